@@ -261,13 +261,14 @@ def _plain_logprobs(logits, ids, temperature, top_n):
     weighted = torch.where(e > 0.0, e * y, 0.0).sum(-1)
     out["entropy"] = torch.where(z[:, 0] > 0.0, log_z[:, 0] - weighted / z[:, 0], 0.0)
     if top_n:
-        # by value, the lowest token among equals: one whole number that is in that order
+        # by value, the lowest token among equals: one whole number that is in that order; -1 where no token is left
         bits = (x + 0.0).view(torch.int32).long()
         order = torch.where(bits >= 0, bits, -2 ** 31 - 1 - bits)     # (the bits of a negative number fall as it rises)
         key = order * 2 ** 20 + (2 ** 20 - 1 - torch.arange(x.shape[1], device="cuda"))
         best = 2 ** 20 - 1 - (key.topk(top_n, dim=-1).values & (2 ** 20 - 1))
-        out["top_ids"] = best.int()
-        out["top_logprobs"] = torch.where(z > 0.0, y.gather(1, best) - log_z, -math.inf)
+        mass = x.gather(1, best) > -math.inf
+        out["top_ids"] = torch.where(mass, best, -1).int()
+        out["top_logprobs"] = torch.where(mass, y.gather(1, best) - log_z, -math.inf)
     return out
 
 
