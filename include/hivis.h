@@ -358,6 +358,59 @@ int hivis_verify_noalloc(int B, int k, int vocab, const int32_t* draft_ids, cons
                          int logits_dtype, const int32_t* rows_before, int32_t* out_accept,
                          int32_t* out_next, int32_t* out_kv_len, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * A key/value cache held in 4 bits, in the caller's buffers.  None of the calls needs a context or a workspace, allocates
+ * or keeps anything; calls on different streams that do not write the same rows may overlap.  (The paper has no
+ * counterpart: its drafter keeps 16-bit rows.)
+ * Per row, KV head and group of HIVIS_KV4_GROUP channels: m = the group's smallest value rounded down to bf16, s = (the
+ * largest - m) / 15 rounded up to bf16, and per channel the integer n in 0..15 nearest to (x - m) / s, the lower one on a
+ * tie (0 where s = 0).  The channel stands for m + s n, at most s / 2 from x.  A group that holds a NaN or an infinity, or
+ * whose range overflows, stands for NaN.  5 bits a value: 0.3125 of a bf16 cache.
+ * The buffers' inner order is the library's own; rows are independent of one another.
+ *   k_codes, v_codes   n_slots * n_kv_heads * max_len * head_dim / 2 bytes each
+ *   k_params, v_params n_slots * n_kv_heads * max_len * head_dim / 32 * 4 bytes each                                  */
+#define HIVIS_KV4_GROUP 32
+#define HIVIS_KV4_MAX_QUERIES 64     /* query rows per sequence in one call          */
+#define HIVIS_KV4_MAX_MASK 1024      /* rows that a mask covers                      */
+typedef struct {
+    uint32_t struct_size;            /* sizeof(hivis_kv4_cache), checked             */
+    int n_slots, n_kv_heads;
+    int head_dim;                    /* 64 or 128                                    */
+    int max_len;                     /* rows per slot, a multiple of 32 up to 2^28     */
+    void *k_codes, *v_codes, *k_params, *v_params;
+} hivis_kv4_cache;
+
+/* Quantise rows into the cache.  Packed as in hivis_prefill: sequence b owns rows [cu_seqlens_host[b], cu_seqlens_host[b+1])
+ * (none is allowed) of k and v, [total, n_kv_heads * head_dim] in `dtype` (HIVIS_F32 | HIVIS_BF16) with `ld` elements from
+ * one row to the next, and puts them at cache rows start_rows[b].. (int32 [B], device) of its slot.  Rows that would lie
+ * outside [0, max_len) are dropped, all rows of a sequence if its start lies there; other rows of the cache stay as they
+ * are.  Keys are stored as given: rotate them first.
+ * Errors: ARG, SHAPE (head_dim, max_len, ld not a multiple of 8), DTYPE, CAPACITY (B > HIVIS_MAX_BATCH, more than max_len
+ * rows for a sequence), CUDA; the text is available from hivis_last_error(NULL).                                      */
+int hivis_kv4_append(const hivis_kv4_cache* cache, int B, const int* seq_slots_host, const int32_t* cu_seqlens_host,
+                     const int32_t* start_rows, const void* k, const void* v, int dtype, int64_t ld, void* stream);
+
+/* The values that cache rows stand for, widened to fp32: rows start_rows[b].. of each listed slot into rows
+ * [cu_seqlens_host[b], cu_seqlens_host[b+1]) of out_k and out_v, [total, n_kv_heads * head_dim].  Output rows whose cache
+ * row would lie outside [0, max_len) are left as they are.  Errors as for hivis_kv4_append.                           */
+int hivis_kv4_read(const hivis_kv4_cache* cache, int B, const int* seq_slots_host, const int32_t* cu_seqlens_host,
+                   const int32_t* start_rows, float* out_k, float* out_v, void* stream);
+
+/* Attention of n_q query rows per sequence over its cached rows: out = softmax(scale * q K^T) V per query head, head h on
+ * KV head h / (n_q_heads / n_kv_heads).  rows[b] (int32 [B], device; read as 0 or max_len where it lies outside) counts the
+ * slot's rows including those of the queries.
+ *   mask NULL: causal.  The queries sit on the last n_q rows: query i sees rows [0, rows[b] - n_q + i].
+ *   mask (uint32 [B, n_q, ceil(mask_rows / 32)]): a draft tree, or anything else over the last mask_rows rows: query i sees
+ *   rows [0, rows[b] - mask_rows), and row rows[b] - mask_rows + j iff bit j % 32 of word j / 32 is set.
+ * A query that sees no row gets zeros.  Rows that a query does not see do not touch its result, whatever they hold.
+ * q [B * n_q, n_q_heads * head_dim] and out likewise in `dtype` (HIVIS_F32 | HIVIS_BF16), q_ld and out_ld elements from one
+ * row to the next.  The result does not depend on anything but the arguments: sums are made in one order.
+ * Errors: ARG, SHAPE (n_q_heads not a multiple of n_kv_heads, q_ld or out_ld not a multiple of 8), DTYPE, CAPACITY (B, n_q >
+ * HIVIS_KV4_MAX_QUERIES, mask_rows > HIVIS_KV4_MAX_MASK), CUDA; the text is available from hivis_last_error(NULL).    */
+int hivis_kv4_attention(const hivis_kv4_cache* cache, int B, const int* seq_slots_host, const int32_t* rows, int n_q,
+                        int n_q_heads, const void* q, int dtype, int64_t q_ld, float scale, const uint32_t* mask,
+                        int mask_rows, void* out, int64_t out_ld, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,7 +18,8 @@ EXPORTS = ("hivis_init", "hivis_destroy", "hivis_prefill", "hivis_draft", "hivis
            "hivis_get_kv_len", "hivis_set_kv_len", "hivis_read_kv", "hivis_debug_tap", "hivis_step_bytes",
            "hivis_launch_count", "hivis_last_error", "hivis_profile_begin", "hivis_profile_end", "hivis_set_option",
            "hivis_status", "hivis_verify_noalloc", "hivis_read_phase_times", "hivis_draft_tree", "hivis_verify_tree", "hivis_verify_sampled", "hivis_draft_sampled",
-           "hivis_set_kv_len_batch")
+           "hivis_set_kv_len_batch", "hivis_kv4_append", "hivis_kv4_read", "hivis_kv4_attention")
+HIVIS_KV4_GROUP, HIVIS_KV4_MAX_QUERIES, HIVIS_KV4_MAX_MASK = 32, 64, 1024
 HIVIS_OPT_CHAIN_KERNEL = 0
 HIVIS_OPT_TC_KERNEL = 1
 HIVIS_OPT_WAIT_LIMIT_US = 2
@@ -50,6 +51,12 @@ _WNAMES = ("embed", "lm_head", "fc", "norm1", "wq", "wk", "wv", "bq", "bk", "bv"
 
 class hivis_weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in _WNAMES]
+
+
+class hivis_kv4_cache(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_slots", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("max_len", C.c_int), ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_params", C.c_void_p),
+                ("v_params", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -85,6 +92,10 @@ def _load() -> C.CDLL:
     L.hivis_draft_tree.argtypes = [vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]
     L.hivis_verify_tree.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp]
     L.hivis_read_phase_times.argtypes = [vp, vp, C.c_longlong, ip, ip, vp]
+    cp = C.POINTER(hivis_kv4_cache)
+    L.hivis_kv4_append.argtypes = [cp, i32, ip, ip, vp, vp, vp, i32, C.c_int64, vp]
+    L.hivis_kv4_read.argtypes = [cp, i32, ip, ip, vp, vp, vp, vp]
+    L.hivis_kv4_attention.argtypes = [cp, i32, ip, vp, i32, i32, vp, i32, C.c_int64, C.c_float, vp, i32, vp, C.c_int64, vp]
     L.hivis_last_error.argtypes = [vp]
     L.hivis_last_error.restype = C.c_char_p
     for n in EXPORTS:
@@ -109,6 +120,14 @@ def _ptr(t) -> Optional[int]:
     if isinstance(t, int):
         return t
     assert t.is_cuda and t.is_contiguous(), "expected a contiguous CUDA tensor"
+    return t.data_ptr()
+
+
+def _row_ptr(t) -> Optional[int]:
+    """As _ptr, for a tensor whose rows (first dimension) may lie apart."""
+    if t is None or isinstance(t, int):
+        return t
+    assert t.is_cuda and (t.is_contiguous() or t[0].is_contiguous()), "expected a CUDA tensor with contiguous rows"
     return t.data_ptr()
 
 
@@ -186,6 +205,23 @@ def hivis_verify_noalloc(B, k, vocab, draft_ids, target_logits, logits_dtype, ro
     _check(lib.hivis_verify_noalloc(int(B), int(k), int(vocab), _ptr(draft_ids), _ptr(target_logits),
                                     int(logits_dtype), _ptr(rows_before), _ptr(out_accept), _ptr(out_next),
                                     _ptr(out_kv_len), _stream(stream)))
+
+
+def hivis_kv4_append(cache, B, seq_slots, cu_seqlens, start_rows, k, v, dtype, ld, stream=None):
+    _check(lib.hivis_kv4_append(C.byref(cache), int(B), _ints(seq_slots), _ints(cu_seqlens), _ptr(start_rows), _row_ptr(k),
+                                _row_ptr(v), int(dtype), int(ld), _stream(stream)))
+
+
+def hivis_kv4_read(cache, B, seq_slots, cu_seqlens, start_rows, out_k, out_v, stream=None):
+    _check(lib.hivis_kv4_read(C.byref(cache), int(B), _ints(seq_slots), _ints(cu_seqlens), _ptr(start_rows), _ptr(out_k),
+                              _ptr(out_v), _stream(stream)))
+
+
+def hivis_kv4_attention(cache, B, seq_slots, rows, n_q, n_q_heads, q, dtype, q_ld, scale, mask, mask_rows, out, out_ld,
+                        stream=None):
+    _check(lib.hivis_kv4_attention(C.byref(cache), int(B), _ints(seq_slots), _ptr(rows), int(n_q), int(n_q_heads), _row_ptr(q),
+                                   int(dtype), int(q_ld), float(scale), _ptr(mask), int(mask_rows), _row_ptr(out), int(out_ld),
+                                   _stream(stream)))
 
 
 def hivis_reset(ctx, slot, stream=None):
@@ -419,3 +455,98 @@ class Drafter:
 
     def launch_count(self):
         return hivis_launch_count(self.ctx)
+
+
+def _dtype(t) -> int:
+    """HIVIS_F32 or HIVIS_BF16, whichever a tensor's element type is."""
+    import torch
+    if t.dtype == torch.bfloat16:
+        return HIVIS_BF16
+    if t.dtype == torch.float32:
+        return HIVIS_F32
+    raise TypeError(f"expected a bfloat16 or float32 tensor, not {t.dtype}")
+
+
+class Kv4Cache:
+    """A key/value cache held in 4 bits (include/hivis.h: hivis_kv4_cache) for `n_slots` sequences of up to `max_len` rows
+    (rounded up to a multiple of 32).  Rows hold [n_kv_heads, head_dim] keys and values."""
+
+    def __init__(self, n_slots: int, n_kv_heads: int, head_dim: int, max_len: int, device=None):
+        import torch
+        self.torch = torch
+        self.dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        if self.dev.index is None:
+            self.dev = torch.device("cuda", torch.cuda.current_device())
+        self.n_slots, self.n_kv_heads, self.head_dim = int(n_slots), int(n_kv_heads), int(head_dim)
+        self.max_len = (int(max_len) + 31) // 32 * 32
+        rows = (self.n_slots, self.n_kv_heads, self.max_len)
+        self.codes = [torch.zeros(rows + (self.head_dim // 2,), dtype=torch.uint8, device=self.dev) for _ in range(2)]
+        self.params = [torch.zeros(rows + (self.head_dim // HIVIS_KV4_GROUP,), dtype=torch.int32, device=self.dev) for _ in range(2)]
+        self.c = hivis_kv4_cache(C.sizeof(hivis_kv4_cache), self.n_slots, self.n_kv_heads, self.head_dim, self.max_len,
+                                 *[t.data_ptr() for t in self.codes + self.params])
+
+    def _here(self, *tensors):
+        """Whether the cache's device is the current one; every tensor has to be on it."""
+        for t in tensors:
+            if t is not None and t.device != self.dev:
+                raise ValueError(f"the cache is on {self.dev}, a tensor on {t.device}")
+        return self.torch.cuda.current_device() == self.dev.index
+
+    def _rows(self, t, n_heads, name, n_rows=None):
+        """[rows, heads, head_dim] with rows that may lie apart -> elements from one row to the next."""
+        if t.dim() != 3 or t.shape[1] != n_heads or t.shape[2] != self.head_dim or (n_rows is not None and t.shape[0] != n_rows):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({n_rows if n_rows is not None else 'rows'}, {n_heads}, {self.head_dim})")
+        if t.numel() and (t.stride(2) != 1 or (n_heads > 1 and t.stride(1) != self.head_dim)):
+            raise ValueError(f"the rows of {name} are not contiguous")
+        return t.stride(0) if t.shape[0] > 1 else n_heads * self.head_dim
+
+    def _per_sequence(self, t, B, name):
+        if t.dtype != self.torch.int32 or t.dim() != 1 or t.shape[0] != B:
+            raise ValueError(f"{name} must be an int32 tensor of {B} entries")
+
+    def append(self, k, v, cu_seqlens, start_rows, slots=None):
+        """Rows [cu_seqlens[b], cu_seqlens[b + 1]) of k and v ([total, n_kv_heads, head_dim], bf16 or fp32) become rows
+        start_rows[b].. (int32 tensor) of slot slots[b] (default b)."""
+        if not self._here(k, v, start_rows):
+            with self.torch.cuda.device(self.dev):
+                return self.append(k, v, cu_seqlens, start_rows, slots)
+        B, total = len(cu_seqlens) - 1, int(cu_seqlens[-1])
+        self._per_sequence(start_rows, B, "start_rows")
+        ld = self._rows(k, self.n_kv_heads, "k", total)
+        if self._rows(v, self.n_kv_heads, "v", total) != ld or v.dtype != k.dtype:
+            raise ValueError("k and v must have the same type and row stride")
+        hivis_kv4_append(self.c, B, slots, cu_seqlens, start_rows, k.data_ptr(), v.data_ptr(), _dtype(k), ld)
+
+    def read(self, cu_seqlens, start_rows, slots=None):
+        """-> (k, v) fp32 [total, n_kv_heads, head_dim]: what rows start_rows[b].. of the slots stand for."""
+        if not self._here(start_rows):
+            with self.torch.cuda.device(self.dev):
+                return self.read(cu_seqlens, start_rows, slots)
+        t, B = self.torch, len(cu_seqlens) - 1
+        self._per_sequence(start_rows, B, "start_rows")
+        shape = (int(cu_seqlens[-1]), self.n_kv_heads, self.head_dim)
+        k = t.empty(shape, dtype=t.float32, device=self.dev)
+        v = t.empty(shape, dtype=t.float32, device=self.dev)
+        hivis_kv4_read(self.c, B, slots, cu_seqlens, start_rows, k, v)
+        return k, v
+
+    def attention(self, q, rows, n_q=1, scale=None, mask=None, mask_rows=0, slots=None, out=None):
+        """q [B * n_q, n_q_heads, head_dim] (bf16 or fp32) over the slots' first rows[b] rows (int32 tensor) -> the same shape
+        and type.  Causal over the last n_q rows, or by `mask` (int32 [B, n_q, ceil(mask_rows / 32)]) over the last mask_rows."""
+        if not self._here(q, rows, mask, out):
+            with self.torch.cuda.device(self.dev):
+                return self.attention(q, rows, n_q, scale, mask, mask_rows, slots, out)
+        t, B = self.torch, rows.shape[0]
+        self._per_sequence(rows, B, "rows")
+        heads = q.shape[1] if q.dim() == 3 else 0
+        q_ld = self._rows(q, heads, "q", B * int(n_q))
+        if out is None:
+            out = t.empty(q.shape, dtype=q.dtype, device=self.dev)
+        elif out.dtype != q.dtype:
+            raise ValueError("out must have the type of q")
+        out_ld = self._rows(out, heads, "out", B * int(n_q))
+        if mask is not None and (mask.dtype != t.int32 or tuple(mask.shape) != (B, int(n_q), (int(mask_rows) + 31) // 32) or not mask.is_contiguous()):
+            raise ValueError("mask must be a contiguous int32 tensor [B, n_q, ceil(mask_rows / 32)]")
+        hivis_kv4_attention(self.c, B, slots, rows, n_q, heads, q.data_ptr(), _dtype(q), q_ld,
+                            self.head_dim ** -0.5 if scale is None else scale, mask, mask_rows, out.data_ptr(), out_ld)
+        return out

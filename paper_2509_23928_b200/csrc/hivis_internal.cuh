@@ -12,6 +12,8 @@
 typedef __nv_bfloat16 bf16;
 typedef unsigned long long u64;
 
+void hivis_set_global_error(const char* msg);   // text of a failed call that has no context
+
 #define HIVIS_MAX_DEVICES 64   // per-device caches of function attributes are indexed by device ordinal
 
 // ---------------------------------------------------------------------------------------------

@@ -1,0 +1,90 @@
+// A key/value cache held in 4 bits: the format, shared by the kernels that write, read and attend over it.
+//
+// Per cache row, KV head and group of 32 channels: m = the smallest value rounded down to bf16, s = (the largest - m) / 15
+// rounded up to bf16, and per channel the integer n in 0..15 nearest to (x - m) / s (the lower one on a tie); the channel
+// stands for m + s n.  Rounded this way round, m and m + 15 s enclose the group, so no value is off by more than s / 2.
+// A group that holds a NaN or an infinity, or whose range overflows, gets m = s = NaN.
+//
+// Parameters: one 32-bit word per group, s in the upper half and m in the lower (each is widened with one instruction),
+// [slot][KV head][row][group].
+// Codes: [slot][KV head][row] of dh / 2 bytes, in the order in which mma.m16n8k16 wants them as its A operand, so that the
+// attention takes them from memory to the tensor core with a mask and a shift:
+//   K  (A = keys: 16 rows x 16 channels).  A row is four chunks of dh / 8 bytes, chunk c for the lanes with lane % 4 = c; word w
+//      of a chunk holds channels 32 w + 8 c + i, nibble i.
+//   V  (A = values transposed: 16 channels x 16 rows).  A register holds one channel of two neighbouring rows, so rows 2 p and
+//      2 p + 1 share dh / 4 words: word u = (dh / 32) g + w holds channels 32 w + 4 g + i, nibble i of the even row in the lower
+//      half and of the odd row in the upper half.  A row owns whole 16-bit halves: writing it leaves its neighbour alone.
+#pragma once
+#include "hivis_internal.cuh"
+
+#include <cuda_fp16.h>
+
+struct Kv4View {
+    unsigned char *k_codes, *v_codes;
+    uint32_t *k_params, *v_params;
+    int n_slots, Hkv, max_len, dh;
+};
+#define KV4_GROUP 32
+
+// first row of a head, in rows: the codes are dh / 2 bytes and the parameters dh / 32 words a row on
+__device__ __forceinline__ long long kv4_row0(const Kv4View& c, int slot, int h) {
+    return ((long long)slot * c.Hkv + h) * c.max_len;
+}
+
+__device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ float kv4_min(uint32_t w) { return __uint_as_float(w << 16); }
+
+// Parameters of a group whose smallest and largest value are lo and hi.  Every step rounds towards the outside, and a number
+// that is exact before the last step stays exact: what comes out is the definition's m and s.
+__device__ __forceinline__ uint32_t kv4_params(float lo, float hi, bool finite) {
+    const bf16 m = __float2bfloat16_rd(lo);
+    const bf16 s = __float2bfloat16_ru(__fdiv_ru(__fsub_ru(hi, __bfloat162float(m)), 15.f));
+    const uint32_t w = ((uint32_t)__bfloat16_as_ushort(s) << 16) | __bfloat16_as_ushort(m);
+    const bool ok = finite && fabsf(__bfloat162float(m)) < INFINITY && __bfloat162float(s) < INFINITY;
+    return ok ? w : 0x7FC07FC0u;
+}
+
+// The code of x, decided without error.  x - m may need more than 24 bits: e is what d = x - m lost.  r = d - n s is exact (n s
+// has 12 bits, and the difference no bit below d's last), and so are the comparisons with s / 2, a multiple of d's last bit.
+__device__ __forceinline__ unsigned kv4_code_exact(float x, float m, float s) {
+    if (!(s > 0.f)) return 0u;
+    float d = x - m;
+    const float bb = d - x;
+    float e = (x - (d - bb)) - (m + bb);
+    if (s < 1e-30f) { d *= 0x1p96f; e *= 0x1p96f; s *= 0x1p96f; }      // (the quotient is the same)
+    float n = rintf(d / s);
+    const float r = fmaf(-n, s, d), half = 0.5f * s;
+    if (r > half || (r == half && e > 0.f)) n += 1.f;
+    else if (r < -half || (r == -half && e <= 0.f)) n -= 1.f;
+    return (unsigned)fminf(fmaxf(n, 0.f), 15.f);
+}
+
+// Codes of 8 values as 8 nibbles.  t = (x - m) / s comes from a product with the reciprocal, off by less than 2^-18; where it is
+// nearer than 2^-17 to a tie the exact form decides.
+__device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t params) {
+    const float m = kv4_min(params), s = kv4_scale(params);
+    uint32_t w = 0u;
+    if (s >= 1e-30f) {
+        const float inv = 1.f / s;
+        bool near = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float t = (x[i] - m) * inv;
+            const float u = t + 12582912.f;                 // 1.5 * 2^23: the nearest integer in the low bits
+            near |= fabsf(t - (u - 12582912.f)) > 0.5f - 0x1p-17f;
+            w |= (__float_as_uint(u) & 15u) << (4 * i);
+        }
+        if (!near) return w;
+        w = 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w |= kv4_code_exact(x[i], m, s) << (4 * i);
+    return w;
+}
+
+// Where the 8 codes of channels [32 w + 8 c, + 8) of a row go.  K: one word.  V: the lower four nibbles into the row's half of
+// word (dh / 32) (2 c) + w of its pair of rows, the upper four into word (dh / 32) (2 c + 1) + w.
+__device__ __forceinline__ long long kv4_k_offset(int dh, long long row, int w, int c) { return row * (dh / 2) + c * (dh / 8) + w * 4; }
+__device__ __forceinline__ long long kv4_v_offset(int dh, long long row, int w, int g) {
+    return (row & ~1ll) * (dh / 2) + ((dh / 32) * g + w) * 4 + (row & 1) * 2;
+}

@@ -10,7 +10,6 @@
 
 #include "hivis_internal.cuh"
 
-void hivis_set_global_error(const char* msg);   // text later returned by hivis_last_error(NULL)
 
 #define NOALLOC_ROWS (HIVIS_MAX_BATCH * (HIVIS_MAX_K + 1))
 #define NOALLOC_CHUNK 8192   // logits per CTA

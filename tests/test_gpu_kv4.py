@@ -1,0 +1,422 @@
+"""The 4-bit cache against its definition in 64 bits: rows in, rows out, and the attention over them."""
+import math
+
+import numpy as np
+import pytest
+
+from tests import kv4_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _to(x, dtype):
+    t = _torch()
+    return t.from_numpy(np.ascontiguousarray(x, np.float32)).to(t.bfloat16 if dtype == "bf16" else t.float32).cuda()
+
+
+def _np(x):
+    return x.float().cpu().numpy().astype(np.float64)
+
+
+def _ints(x):
+    return _torch().tensor([int(i) for i in x], dtype=_torch().int32, device="cuda")
+
+
+def _bytes(cache):
+    return [x.cpu().numpy().copy() for x in cache.codes + cache.params]
+
+
+def _cache(*a):
+    from paper_2509_23928_b200 import Kv4Cache
+    return Kv4Cache(*a)
+
+
+def _starts(n):
+    return [0] + [int(x) for x in np.cumsum(n)]
+
+
+# ---------------------------------------------------------------------------------------------- rows in, rows out
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh,heads,counts,start", [
+    (128, 3, [1], [0]), (128, 3, [1], [7]), (64, 5, [1, 1, 1], [0, 1, 30]), (128, 2, [2, 3, 16, 33, 0, 5], [1, 0, 15, 31, 4, 59]),
+    (64, 1, [64, 17, 1, 40], [0, 47, 63, 1]), (128, 32, [3, 2], [0, 61]),
+])
+def test_rows_are_held_as_the_format_says(dtype, dh, heads, counts, start):
+    t = _torch()
+    rng = np.random.default_rng(5)
+    cu = _starts(counts)
+    B, total = len(counts), cu[-1]
+    cache = _cache(B + 1, heads, dh, 64)
+    slots = list(range(B, 0, -1))                                    # any order; slot 0 is not listed
+    k, v = (_to(rng.standard_normal((total, heads, dh)) * 3 + rng.standard_normal((1, heads, dh)), dtype) for _ in range(2))
+    before = _bytes(cache)
+    cache.append(k, v, cu, _ints(start), slots)
+    k2, v2 = cache.read(cu, _ints(start), slots)
+    t.cuda.synchronize()
+    for got, x in ((k2, k), (v2, v)):
+        want = ref.values(*ref.quantise(_np(x)))
+        # m + s n is one fp32 operation on exact numbers: half a step of fp32
+        assert np.all(np.abs(_np(got) - want) <= 2.0 ** -24 * np.abs(want))
+    # nothing else has moved: the rows written are the only ones that differ from the start
+    for a, z in zip(before, _bytes(cache)):
+        touched = np.zeros(a.shape[:3], bool)
+        for b in range(B):
+            touched[slots[b], :, start[b]:start[b] + counts[b]] = True
+        if a.dtype == np.uint8:                                      # (a row's V codes lie in its pair's rows)
+            pair = touched.reshape(touched.shape[0], touched.shape[1], -1, 2).any(-1)
+            touched = np.repeat(pair, 2, axis=2)
+        assert np.array_equal(a[~touched], z[~touched])
+
+
+def test_a_row_at_a_time_is_the_same_as_all_at_once():
+    t = _torch()
+    rng = np.random.default_rng(6)
+    k, v = (_to(rng.standard_normal((45, 2, 128)), "bf16") for _ in range(2))
+    whole, single = _cache(1, 2, 128, 64), _cache(1, 2, 128, 64)
+    whole.append(k, v, [0, 45], _ints([3]))
+    for i in rng.permutation(45):
+        single.append(k[i:i + 1], v[i:i + 1], [0, 1], _ints([3 + i]))
+    t.cuda.synchronize()
+    for a, b in zip(_bytes(whole), _bytes(single)):
+        assert np.array_equal(a, b)
+
+
+def test_rows_behind_the_cache_are_dropped():
+    t = _torch()
+    rng = np.random.default_rng(7)
+    k, v = (_to(rng.standard_normal((40, 2, 64)), "bf16") for _ in range(2))
+    cache = _cache(4, 2, 64, 32)
+    before = _bytes(cache)
+    cache.append(k, v, [0, 10, 20, 30, 40], _ints([27, -1, 32, 2 ** 31 - 1]))
+    t.cuda.synchronize()
+    for a, z in zip(before, _bytes(cache)):
+        assert np.array_equal(a[1:], z[1:]) and np.array_equal(a[0, :, :26], z[0, :, :26])
+    got, _ = cache.read([0, 5], _ints([27]))
+    want = ref.values(*ref.quantise(_np(k[:5])))
+    assert np.all(np.abs(_np(got) - want) <= 2.0 ** -24 * np.abs(want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_groups_that_are_hard_to_hold(dtype):
+    """Ties, equal values, zeros of both signs, one far value, denormals, the ends of the range, and what is not finite."""
+    rng = np.random.default_rng(8)
+    rows = []
+    for step in (1.0, 0.5, 3.0, 2.0 ** -100, 2.0 ** 90):
+        # whole and half steps above the smallest value, both ends among them: every half is a tie
+        g = rng.integers(0, 31, 32) * 0.5
+        g[0], g[1] = 0.0, 15.0
+        rows.append((g + 1.0) * step)
+    rows.append(np.full(32, 0.3))
+    rows.append(np.zeros(32))
+    rows.append(np.where(np.arange(32) % 2, 0.0, -0.0))
+    rows.append(np.where(np.arange(32) == 5, 1e4, rng.standard_normal(32)))
+    rows.append(np.where(np.arange(32) == 5, 1.0, -1e-20 * np.arange(32)))
+    rows.append(rng.standard_normal(32) * 1e-39)
+    rows.append(rng.standard_normal(32) * 2.0 ** -133)
+    rows.append(np.linspace(-1.5e38, 1.6e38, 32))
+    rows.append(np.where(np.arange(32) == 9, np.nan, 1.0))
+    rows.append(np.where(np.arange(32) == 9, np.inf, 1.0))
+    rows.append(np.where(np.arange(32) == 9, -np.inf, 1.0))
+    rows.append(np.where(np.arange(32) % 2, -3e38, 3e38))           # the range overflows
+    x = np.stack(rows).astype(np.float32)
+    k = _to(x[:, None].repeat(2, 1).reshape(len(rows), 1, 64), dtype)
+    cache = _cache(1, 1, 64, 32)
+    cache.append(k, k.flip(0).contiguous(), [0, len(rows)], _ints([1]))
+    got_k, got_v = cache.read([0, len(rows)], _ints([1]))
+    want = ref.values(*ref.quantise(_np(k)))
+    for got, w in ((got_k, want), (got_v, want[::-1])):
+        g = got.cpu().numpy().astype(np.float64)
+        assert np.array_equal(np.isnan(g), np.isnan(w))
+        d = np.abs(g - w)
+        # (half a step of fp32, which below its normal numbers is 2^-150)
+        assert np.all(d[~np.isnan(d)] <= np.maximum(2.0 ** -24 * np.abs(w), 2.0 ** -150)[~np.isnan(d)])
+
+
+def test_many_values_take_the_nearest_code():
+    """A million fp32 values: the short form of the division must never decide what it cannot see."""
+    rng = np.random.default_rng(9)
+    x = rng.standard_normal((2048, 4, 128)) * np.exp(rng.uniform(-5, 5, (2048, 4, 1)))
+    k, v = _to(x, "f32"), _to(np.round(x, 2), "bf16").float()
+    cache = _cache(1, 4, 128, 2048)
+    cache.append(k, v, [0, 2048], _ints([0]))
+    got_k, got_v = cache.read([0, 2048], _ints([0]))
+    for got, src in ((got_k, k), (got_v, v)):
+        want = ref.values(*ref.quantise(src.cpu().numpy().astype(np.float64)))
+        assert np.all(np.abs(_np(got) - want) <= 2.0 ** -24 * np.abs(want))
+
+
+def test_rows_with_a_stride():
+    t = _torch()
+    rng = np.random.default_rng(10)
+    both = _to(rng.standard_normal((21, 5 * 64)), "bf16")           # q | k | v of one projection, say
+    k, v = both[:, 64:192].view(21, 2, 64), both[:, 192:].view(21, 2, 64)
+    cache = _cache(1, 2, 64, 32)
+    cache.append(k, v, [0, 21], _ints([4]))
+    got_k, got_v = cache.read([0, 21], _ints([4]))
+    t.cuda.synchronize()
+    for got, x in ((got_k, k), (got_v, v)):
+        want = ref.values(*ref.quantise(_np(x)))
+        assert np.all(np.abs(_np(got) - want) <= 2.0 ** -24 * np.abs(want))
+
+
+# ---------------------------------------------------------------------------------------------- attention
+class Filled:
+    """A cache with rows in it, what they stand for, and queries."""
+
+    def __init__(self, dtype, dh, Hkv, G, lens, n_q, seed=0, max_len=None, slots=None, q_std=1.5, fill=None, spread=0.0):
+        rng = np.random.default_rng(seed)
+        self.rng, self.dtype, self.lens, self.n_q, self.dh, self.Hkv, self.G = rng, dtype, list(lens), n_q, dh, Hkv, G
+        B = len(lens)
+        self.slots = slots
+        self.cache = _cache(B if slots is None else max(slots) + 1, Hkv, dh, max_len or max(max(lens), 1))
+        if fill is not None:                                          # what lies in the cache where no row was put
+            for x in self.cache.codes + self.cache.params:
+                x.fill_(fill)
+        total = sum(lens)
+        k = rng.standard_normal((total, Hkv, dh)) + 2.0 * rng.standard_normal((1, Hkv, dh))
+        v = rng.standard_normal((total, Hkv, dh)) * np.exp(spread * rng.uniform(-1, 1, (total, Hkv, 1)))
+        self.k, self.v = _to(k, dtype), _to(v, dtype)
+        self.q = _to(rng.standard_normal((B * n_q, Hkv * G, dh)) * q_std, dtype)
+        self.rows = _ints(lens)
+
+    def put(self):
+        self.cache.append(self.k, self.v, _starts(self.lens), _ints([0] * len(self.lens)), self.slots)
+
+    def check(self, out, mask=None, mask_rows=0):
+        cu = _starts(self.lens)
+        got, q = _np(out).reshape(len(self.lens), self.n_q, self.Hkv * self.G, self.dh), _np(self.q).reshape(len(self.lens), self.n_q, -1, self.dh)
+        scale = self.dh ** -0.5
+        for b, L in enumerate(self.lens):
+            kq, vq = ref.quantise(_np(self.k[cu[b]:cu[b + 1]])), ref.quantise(_np(self.v[cu[b]:cu[b + 1]]))
+            see = ref.visible(L, self.n_q, None if mask is None else mask[b], mask_rows)
+            want, reach, big = ref.attention(q[b], kq, vq, scale, see)
+            if self.dtype == "bf16":
+                # the result's rounding; the probabilities' to fp16, 2^-11 of each, and as much for scores, sums and exponentials
+                tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * reach
+            else:
+                # queries and probabilities to 22 bits, exponentials and sums to fp32; a score is off by that much of its terms
+                tol = 2.0 ** -20 * reach * (1.0 + big[..., None])
+            d = np.abs(got[b] - want)
+            assert np.all(d <= tol + 1e-30), (b, L, float((d / (tol + 1e-30)).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh,Hkv,G", [(64, 4, 1), (128, 2, 1), (128, 1, 7), (64, 1, 8), (128, 1, 5), (64, 2, 3)])
+@pytest.mark.parametrize("n_q", [1, 3, 8])
+def test_attention_over_uneven_sequences(dtype, dh, Hkv, G, n_q):
+    f = Filled(dtype, dh, Hkv, G, [0, 1, 2, 15, 16, 17, 31, 33, 64, 65, 130, 511], n_q, seed=dh + G + n_q)
+    f.put()
+    f.check(f.cache.attention(f.q, f.rows, n_q=n_q))
+
+
+@pytest.mark.parametrize("dtype,dh,Hkv,G,n_q", [("bf16", 128, 2, 7, 17), ("bf16", 64, 1, 8, 61), ("f32", 128, 1, 1, 33), ("bf16", 128, 1, 16, 5),
+                                                ("f32", 64, 1, 40, 2)])
+def test_attention_with_many_columns(dtype, dh, Hkv, G, n_q):
+    f = Filled(dtype, dh, Hkv, G, [700, 5, 64], n_q, seed=3)
+    f.put()
+    f.check(f.cache.attention(f.q, f.rows, n_q=n_q))
+
+
+def _words(mask):
+    t = _torch()
+    B, n_q, T = mask.shape
+    w = (T + 31) // 32
+    bits = np.zeros((B, n_q, w * 32), np.uint32)
+    bits[..., :T] = mask
+    return t.from_numpy((bits.reshape(B, n_q, w, 32) << np.arange(32, dtype=np.uint32)).sum(-1, dtype=np.uint32).view(np.int32)).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_q,mask_rows,lens", [(1, 1, [1, 40]), (5, 5, [5, 3, 200]), (10, 51, [60, 51, 20, 333]), (61, 61, [61, 100, 10]),
+                                                (16, 241, [300, 241, 240]), (3, 1024, [40, 1100])])
+def test_attention_under_a_tree_mask(dtype, n_q, mask_rows, lens):
+    f = Filled(dtype, 128, 2, 2, lens, n_q, seed=n_q)
+    f.put()
+    mask = f.rng.random((len(lens), n_q, mask_rows)) < 0.4
+    mask[:, 0] = False                                               # a query that sees nothing of the last rows
+    mask[0, -1] = True
+    f.check(f.cache.attention(f.q, f.rows, n_q=n_q, mask=_words(mask), mask_rows=mask_rows), mask, mask_rows)
+
+
+@pytest.mark.parametrize("fill", [0xFF, 0x7F, 0x00])
+def test_what_lies_behind_the_rows_does_not_matter(fill):
+    """Rows that were never written (NaN, infinite and zero parameters), and rows that a query does not see, holding NaN."""
+    t = _torch()
+    f = Filled("bf16", 128, 2, 3, [1, 18, 47, 80], 4, seed=11, fill=fill, max_len=96)
+    f.put()
+    out = f.cache.attention(f.q, f.rows, n_q=4)
+    f.check(out)
+    # the sequence's last row is NaN: only the last query sees it
+    cu = _starts(f.lens)
+    bad = t.full((4, 2, 128), math.nan, dtype=t.bfloat16, device="cuda")
+    f.cache.append(bad, bad, [0, 1, 2, 3, 4], _ints([n - 1 for n in f.lens]))
+    again = f.cache.attention(f.q, f.rows, n_q=4).view(4, 4, 6, 128)
+    out = out.view(4, 4, 6, 128)
+    assert t.equal(again[:, :3], out[:, :3])
+    assert bool(again[:, 3].isnan().all())
+    assert cu[-1] == 146
+
+
+def test_infinite_rows_that_are_masked_by_a_tree():
+    t = _torch()
+    f = Filled("bf16", 64, 1, 8, [70], 2, seed=12)
+    f.v[66] = math.inf
+    f.k[67] = math.nan
+    f.put()
+    mask = np.ones((1, 2, 10), bool)
+    mask[0, :, 6] = mask[0, :, 7] = False                            # rows 66 and 67
+    out = f.cache.attention(f.q, f.rows, n_q=2, mask=_words(mask), mask_rows=10)
+    f.k[67], f.v[66] = 0.0, 0.0
+    f.check(out, mask, 10)
+    assert bool(t.isfinite(out).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_queries_and_values_of_any_size(dtype):
+    """Queries from 2^-60 to flat-out certain, values whose rows differ by factors of a thousand."""
+    for q_std, spread in ((2.0 ** -60, 0.0), (30.0, 0.0), (1.0, 3.5), (8.0, 3.5)):
+        f = Filled(dtype, 128, 1, 4, [257, 40], 2, seed=13, q_std=q_std, spread=spread)
+        f.put()
+        f.check(f.cache.attention(f.q, f.rows, n_q=2))
+
+
+@pytest.mark.parametrize("scale_v", [1e-30, 1e-6, 1e6, 1e30])
+def test_values_of_any_magnitude(scale_v):
+    f = Filled("bf16", 128, 1, 1, [300], 1, seed=14)
+    f.v *= scale_v
+    f.put()
+    f.check(f.cache.attention(f.q, f.rows))
+
+
+def test_scores_that_keep_rising():
+    """Every row beats all before it by a little: the maximum is raised late, and often."""
+    t = _torch()
+    for slope in (0.02, 0.5, 3.0):
+        f = Filled("bf16", 64, 1, 1, [900], 1, seed=15)
+        d = t.nn.functional.normalize(f.q[0, 0].float(), dim=0)
+        f.k[:, 0] = (f.k[:, 0].float() * 0.1 + t.arange(900, device="cuda")[:, None] * slope * 8.0 / float(f.q[0, 0].float().norm()) * d).bfloat16()
+        f.put()
+        f.check(f.cache.attention(f.q, f.rows))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_slots_and_an_output_of_the_callers(dtype):
+    t = _torch()
+    f = Filled(dtype, 64, 2, 4, [100, 37, 5], 2, seed=16, slots=[5, 0, 3], max_len=160)
+    f.put()
+    wide = t.zeros((6, 1024), dtype=f.q.dtype, device="cuda")
+    wide[:, 256:768] = f.q.reshape(6, 512)
+    out = t.full((6, 640), 7.0, dtype=f.q.dtype, device="cuda")
+    got = f.cache.attention(wide[:, 256:768].view(6, 8, 64), f.rows, n_q=2, slots=[5, 0, 3], out=out[:, :512].view(6, 8, 64))
+    f.check(got)
+    assert bool((out[:, 512:] == 7.0).all())
+
+
+@pytest.mark.parametrize("B,Hkv,G,dh,lens", [(1, 1, 8, 64, [20001]), (2, 4, 7, 128, [9000, 4097]), (64, 1, 1, 64, list(range(1, 65)))])
+def test_long_and_many(B, Hkv, G, dh, lens):
+    f = Filled("bf16", dh, Hkv, G, lens, 1, seed=17)
+    f.put()
+    f.check(f.cache.attention(f.q, f.rows))
+
+
+def test_row_counts_outside_the_cache_are_read_as_its_ends():
+    t = _torch()
+    f = Filled("bf16", 128, 1, 2, [64, 64], 1, seed=18, max_len=64)
+    f.put()
+    out = f.cache.attention(f.q, _ints([-5, 1000]))
+    whole = f.cache.attention(f.q, _ints([64, 64]))
+    assert bool((out[0] == 0).all()) and t.equal(out[1], whole[1])
+
+
+def test_the_same_call_gives_the_same_bits():
+    t = _torch()
+    f = Filled("bf16", 128, 4, 7, [3000, 777], 3, seed=19)
+    f.put()
+    first = f.cache.attention(f.q, f.rows, n_q=3)
+    for _ in range(5):
+        assert t.equal(f.cache.attention(f.q, f.rows, n_q=3), first)
+
+
+def test_a_cache_of_more_than_four_gigabytes():
+    t = _torch()
+    cache = _cache(40, 32, 128, 65536)                               # 5.4 GB of codes for the keys alone
+    rng = np.random.default_rng(20)
+    k, v = (_to(rng.standard_normal((50, 32, 128)), "bf16") for _ in range(2))
+    q = _to(rng.standard_normal((1, 32, 128)), "bf16")
+    small = _cache(1, 32, 128, 65536)
+    cache.append(k, v, [0, 50], _ints([0]), [39])
+    small.append(k, v, [0, 50], _ints([0]))
+    assert t.equal(cache.attention(q, _ints([50]), slots=[39]), small.attention(q, _ints([50])))
+    cache.append(k, v, [0, 50], _ints([65536 - 50]), [38])
+    got, _ = cache.read([0, 50], _ints([65536 - 50]), [38])
+    want, _ = small.read([0, 50], _ints([0]))
+    assert t.equal(got, want)
+
+
+def test_captured_calls_replay_with_new_inputs():
+    t = _torch()
+    f = Filled("bf16", 128, 2, 4, [50, 90], 1, seed=21, max_len=128)
+    f.put()
+    out = t.empty_like(f.q)
+    k_new, v_new, start = f.k[:2].clone(), f.v[:2].clone(), _ints([50, 90])
+    rows = _ints([51, 91])
+
+    def step():
+        f.cache.append(k_new, v_new, [0, 1, 2], start)
+        f.cache.attention(f.q, rows, out=out)
+
+    side = t.cuda.Stream()
+    side.wait_stream(t.cuda.current_stream())
+    with t.cuda.stream(side):
+        step()
+    t.cuda.current_stream().wait_stream(side)
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        step()
+    for i in range(3):
+        k_new.copy_(f.k[2 + 2 * i:4 + 2 * i])
+        v_new.copy_(f.v[2 + 2 * i:4 + 2 * i])
+        graph.replay()
+        got = out.clone()
+        step()
+        assert t.equal(got, out)
+        start += 1
+        rows += 1
+
+
+def test_two_streams_at_once():
+    t = _torch()
+    f = Filled("bf16", 128, 4, 2, [2000, 1500], 2, seed=22)
+    f.put()
+    want = f.cache.attention(f.q, f.rows, n_q=2)
+    streams = [t.cuda.Stream() for _ in range(2)]
+    got = []
+    t.cuda.synchronize()
+    for i in range(20):
+        with t.cuda.stream(streams[i % 2]):
+            got.append(f.cache.attention(f.q, f.rows, n_q=2))
+    t.cuda.synchronize()
+    assert all(t.equal(g, want) for g in got)
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    t = _torch()
+    cache = _cache(2, 2, 64, 32)
+    k = t.zeros((4, 2, 64), dtype=t.bfloat16, device="cuda")
+    q = t.zeros((2, 4, 64), dtype=t.bfloat16, device="cuda")
+    rows = _ints([3, 3])
+    for call in (lambda: cache.append(k, k.float(), [0, 4], _ints([0])), lambda: cache.append(k, k, [0, 3], _ints([0])),
+                 lambda: cache.append(k.transpose(1, 2), k.transpose(1, 2), [0, 4], _ints([0])),
+                 lambda: cache.append(k, k, [0, 4], _ints([0, 0])), lambda: cache.append(k.cpu(), k, [0, 4], _ints([0])),
+                 lambda: cache.attention(q, rows.long()), lambda: cache.attention(q[:1], rows), lambda: cache.attention(q, rows, n_q=2),
+                 lambda: cache.attention(q, rows, mask=t.zeros((2, 1, 1), dtype=t.int32, device="cuda"), mask_rows=33),
+                 lambda: cache.attention(q, rows, out=t.zeros((2, 4, 64), device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        cache.append(k.half(), k.half(), [0, 4], _ints([0]))
