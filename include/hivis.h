@@ -359,16 +359,15 @@ int hivis_verify_noalloc(int B, int k, int vocab, const int32_t* draft_ids, cons
                          int32_t* out_next, int32_t* out_kv_len, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
- * A key/value cache held in 4 bits, in the caller's buffers.  None of the calls needs a context or a workspace, allocates
+ * A key/value cache held in 4 bits, in a buffer of the caller's.  None of the calls needs a context or a workspace, allocates
  * or keeps anything; calls on different streams that do not write the same rows may overlap.  (The paper has no
  * counterpart: its drafter keeps 16-bit rows.)
  * Per row, KV head and group of HIVIS_KV4_GROUP channels: m = the group's smallest value rounded down to bf16, s = (the
  * largest - m) / 15 rounded up to bf16, and per channel the integer n in 0..15 nearest to (x - m) / s, the lower one on a
  * tie (0 where s = 0).  The channel stands for m + s n, at most s / 2 from x.  A group that holds a NaN or an infinity, or
  * whose range overflows, stands for NaN.  5 bits a value: 0.3125 of a bf16 cache.
- * The buffers' inner order is the library's own; rows are independent of one another.
- *   k_codes, v_codes   n_slots * n_kv_heads * max_len * head_dim / 2 bytes each
- *   k_params, v_params n_slots * n_kv_heads * max_len * head_dim / 32 * 4 bytes each                                  */
+ * The buffer holds n_slots * n_kv_heads * max_len * head_dim * 5 / 4 bytes (keys and values); its inner order is the
+ * library's own, and a row can be written without touching others.                                                 */
 #define HIVIS_KV4_GROUP 32
 #define HIVIS_KV4_MAX_QUERIES 64     /* query rows per sequence in one call          */
 #define HIVIS_KV4_MAX_MASK 1024      /* rows that a mask covers                      */
@@ -377,7 +376,7 @@ typedef struct {
     int n_slots, n_kv_heads;
     int head_dim;                    /* 64 or 128                                    */
     int max_len;                     /* rows per slot, a multiple of 32 up to 2^28     */
-    void *k_codes, *v_codes, *k_params, *v_params;
+    void* data;                      /* device buffer, 16-byte aligned               */
 } hivis_kv4_cache;
 
 /* Quantise rows into the cache.  Packed as in hivis_prefill: sequence b owns rows [cu_seqlens_host[b], cu_seqlens_host[b+1])

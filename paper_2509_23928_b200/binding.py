@@ -55,8 +55,7 @@ class hivis_weights(C.Structure):
 
 class hivis_kv4_cache(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("n_slots", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
-                ("max_len", C.c_int), ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_params", C.c_void_p),
-                ("v_params", C.c_void_p)]
+                ("max_len", C.c_int), ("data", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -479,11 +478,9 @@ class Kv4Cache:
             self.dev = torch.device("cuda", torch.cuda.current_device())
         self.n_slots, self.n_kv_heads, self.head_dim = int(n_slots), int(n_kv_heads), int(head_dim)
         self.max_len = (int(max_len) + 31) // 32 * 32
-        rows = (self.n_slots, self.n_kv_heads, self.max_len)
-        self.codes = [torch.zeros(rows + (self.head_dim // 2,), dtype=torch.uint8, device=self.dev) for _ in range(2)]
-        self.params = [torch.zeros(rows + (self.head_dim // HIVIS_KV4_GROUP,), dtype=torch.int32, device=self.dev) for _ in range(2)]
+        self.data = torch.zeros(self.n_slots * self.n_kv_heads * self.max_len * self.head_dim * 5 // 4, dtype=torch.uint8, device=self.dev)
         self.c = hivis_kv4_cache(C.sizeof(hivis_kv4_cache), self.n_slots, self.n_kv_heads, self.head_dim, self.max_len,
-                                 *[t.data_ptr() for t in self.codes + self.params])
+                                 self.data.data_ptr())
 
     def _here(self, *tensors):
         """Whether the cache's device is the current one; every tensor has to be on it."""

@@ -97,20 +97,23 @@ __device__ __forceinline__ void kv4_store_row(const Kv4View& c, const Kv4Place& 
     const uint32_t other = __shfl_xor_sync(0xffffffffu, vw, LR);
     const bool both = __shfl_xor_sync(0xffffffffu, live ? 1 : 0, LR) != 0 && live;
     if (!live) return;
-    const long long r0 = kv4_row0(c, p.slot, p.h), row = r0 + p.row;
-    *(uint32_t*)(c.k_codes + kv4_k_offset(DH, row, p.w, p.c)) = kw;
+    unsigned char* tile = kv4_tile(c, p.slot, p.h, p.row);
+    const int r = p.row % KV4_TILE;
+    *(uint32_t*)(tile + kv4_k_at(DH, r, p.w, p.c)) = kw;
     if (p.c == 0) {
-        c.k_params[row * (DH / 32) + p.w] = kp;
-        c.v_params[row * (DH / 32) + p.w] = vp;
+        *(uint16_t*)(tile + kv4_s_at(DH, 0, r, p.w)) = (uint16_t)(kp >> 16);
+        *(uint16_t*)(tile + kv4_m_at(DH, 0, r, p.w)) = (uint16_t)kp;
+        *(uint16_t*)(tile + kv4_s_at(DH, 1, r, p.w)) = (uint16_t)(vp >> 16);
+        *(uint16_t*)(tile + kv4_m_at(DH, 1, r, p.w)) = (uint16_t)vp;
     }
     const bool odd = (p.row & 1) != 0;
     if (both) {
         // the pair's words are whole: the even row's lane writes the first, the odd row's the second
         const uint32_t word = odd ? ((other >> 16) | (vw & 0xFFFF0000u)) : ((vw & 0xFFFFu) | (other << 16));
-        *(uint32_t*)(c.v_codes + kv4_v_offset(DH, row & ~1ll, p.w, 2 * p.c + (odd ? 1 : 0))) = word;
+        *(uint32_t*)(tile + kv4_v_at(DH, r & ~1, p.w, 2 * p.c + (odd ? 1 : 0))) = word;
     } else {
-        *(uint16_t*)(c.v_codes + kv4_v_offset(DH, row, p.w, 2 * p.c)) = (uint16_t)vw;
-        *(uint16_t*)(c.v_codes + kv4_v_offset(DH, row, p.w, 2 * p.c + 1)) = (uint16_t)(vw >> 16);
+        *(uint16_t*)(tile + kv4_v_at(DH, r, p.w, 2 * p.c)) = (uint16_t)vw;
+        *(uint16_t*)(tile + kv4_v_at(DH, r, p.w, 2 * p.c + 1)) = (uint16_t)(vw >> 16);
     }
 }
 
@@ -134,11 +137,13 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ K
     pdl_trigger();
     const Kv4Place p = kv4_place<DH>(a);
     if (p.packed < 0) return;
-    const long long row = kv4_row0(a.c, p.slot, p.h) + p.row;
-    const uint32_t kp = a.c.k_params[row * (DH / 32) + p.w], vp = a.c.v_params[row * (DH / 32) + p.w];
-    const uint32_t kw = *(const uint32_t*)(a.c.k_codes + kv4_k_offset(DH, row, p.w, p.c));
-    const uint32_t v0 = *(const uint16_t*)(a.c.v_codes + kv4_v_offset(DH, row, p.w, 2 * p.c));
-    const uint32_t v1 = *(const uint16_t*)(a.c.v_codes + kv4_v_offset(DH, row, p.w, 2 * p.c + 1));
+    const unsigned char* tile = kv4_tile(a.c, p.slot, p.h, p.row);
+    const int r = p.row % KV4_TILE;
+    auto half = [&](int at) { return (uint32_t)*(const uint16_t*)(tile + at); };
+    const uint32_t kp = (half(kv4_s_at(DH, 0, r, p.w)) << 16) | half(kv4_m_at(DH, 0, r, p.w));
+    const uint32_t vp = (half(kv4_s_at(DH, 1, r, p.w)) << 16) | half(kv4_m_at(DH, 1, r, p.w));
+    const uint32_t kw = *(const uint32_t*)(tile + kv4_k_at(DH, r, p.w, p.c));
+    const uint32_t v0 = half(kv4_v_at(DH, r, p.w, 2 * p.c)), v1 = half(kv4_v_at(DH, r, p.w, 2 * p.c + 1));
     const uint32_t vw = v0 | (v1 << 16);
     float k[8], v[8];
 #pragma unroll
@@ -157,19 +162,22 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ K
 // ------------------------------------------------------------------------------------------------ attention
 // For each KV head the queries of all its rows and query heads are the columns of one problem: S^T = K Q^T and O^T = V^T P^T with
 // the cache as the A operand of mma.m16n8k16 (16 keys, or 16 channels) and eight queries as B, so that one query costs no more
-// than eight.  For bf16 codes reach the tensor core as fp16 subnormals (n 2^-24: a mask, no conversion), every second nibble as 16 n with
-// its query, or its output, scaled by 1/16.  Scales stay outside: per group of 32 channels S = sum s_g (q_g . n) + m_g sum(q_g),
-// and O_g = sum_r (p_r s_rg) n_r + sum_r p_r m_rg, the second sums in fp32 beside the products.
+// than eight.  For bf16 codes reach the tensor core as fp16 subnormals (n 2^-24: a mask, no conversion), every second nibble as 16 n
+// with its query, or its output, scaled by 1/16.  Scales stay outside: per group of 32 channels S = sum s_g (q_g . n) + m_g sum(q_g),
+// and O_g = sum_r (p_r s_rg) n_r + sum_r p_r m_rg.  The second sum of S is one more product, of the m as they are stored (bf16)
+// and sum(q_g) in three bf16 parts.
 //
 // Precision.  bf16 queries are exact in fp16 once their row is scaled by a power of two (what is below 2^-29 of the row's largest
 // is rounded there); probabilities are rounded to fp16's 11 bits, 2^-12 of each, which the 2^-9 of the bf16 result hides.  fp32
 // queries and their probabilities go in as two fp16 numbers (22 bits), the codes as whole numbers, and the products of 16 rows are
 // added up in fp32 outside the tensor core.
 //
-// A cluster of up to 16 CTAs shares one (sequence, KV head, block of columns); a warp takes every (4 * CTAs)-th tile of 16 rows and
-// keeps its own maximum, sum and output.  They are joined in shared memory, then over the cluster, always in the same order.
-#define KV4_WARPS 4
+// A cluster of up to 16 CTAs shares one (sequence, KV head, block of columns); a warp takes every (warps of the cluster)-th tile of
+// 16 rows, which one bulk copy brings into its own ring of four, and keeps its own maximum, sum and output.  They are joined in
+// shared memory, then over the cluster, always in the same order.
 #define KV4_MAX_CLUSTER 16
+#define KV4_STAGES 4
+#define KV4_WAIT_LIMIT (1 << 22)     // polls of a copy's barrier before a warp gives up (each may suspend for a while)
 
 struct Kv4AttnArgs {
     Kv4View c;
@@ -186,39 +194,48 @@ struct Kv4AttnArgs {
     int n_blocks;              // blocks of 8 NT columns
 };
 
+__device__ __forceinline__ uint32_t kv4_saddr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool kv4_wait(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < KV4_WAIT_LIMIT; ++i) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+// one tile into shared memory; the barrier's phase ends when it is there (one lane)
+__device__ __forceinline__ void kv4_fetch(uint32_t dst, const unsigned char* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 template <int Q>
-struct Kv4Tile {               // a lane's part of 16 rows: chunk lane % 4 of the keys lane / 4 and lane / 4 + 8; chunk lane / 4 of the
-    uint32_t k0[Q], k1[Q], v0[Q], v1[Q];        // pairs of values lane % 4 and lane % 4 + 4; the parameters of its two keys' rows
-    uint32_t kp0[Q], kp1[Q], vp0[Q], vp1[Q];
-};
-template <int Q>
-__device__ __forceinline__ void kv4_ld(const void* p, uint32_t (&w)[Q]) {
+__device__ __forceinline__ void kv4_lds(const unsigned char* p, uint32_t (&w)[Q]) {
     if constexpr (Q == 4) {
-        const uint4 x = ld_stream((const uint4*)p);
+        const uint4 x = *(const uint4*)p;
         w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
     } else {
-        const uint2 x = __ldg((const uint2*)p);
+        const uint2 x = *(const uint2*)p;
         w[0] = x.x; w[1] = x.y;
     }
-}
-template <int DH>
-__device__ __forceinline__ void kv4_load_tile(const Kv4View& c, long long row, int lane, Kv4Tile<DH / 32>& t) {
-    constexpr int Q = DH / 32, RB = DH / 2, CH = DH / 8;
-    const int g = lane >> 2, l = lane & 3;
-    kv4_ld<Q>(c.k_codes + (row + g) * RB + l * CH, t.k0);
-    kv4_ld<Q>(c.k_codes + (row + g + 8) * RB + l * CH, t.k1);
-    kv4_ld<Q>(c.k_params + (row + g) * Q, t.kp0);
-    kv4_ld<Q>(c.k_params + (row + g + 8) * Q, t.kp1);
-    kv4_ld<Q>(c.v_codes + (row + 2 * l) * RB + g * CH, t.v0);
-    kv4_ld<Q>(c.v_codes + (row + 2 * l + 8) * RB + g * CH, t.v1);
-    kv4_ld<Q>(c.v_params + (row + g) * Q, t.vp0);
-    kv4_ld<Q>(c.v_params + (row + g + 8) * Q, t.vp1);
 }
 
 __device__ __forceinline__ void kv4_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the first of a sum
+__device__ __forceinline__ void kv4_mma0(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void kv4_mma0_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t kv4_half2(float x, float y) {
     const __half2 h = __floats2half2_rn(x, y);
@@ -230,6 +247,14 @@ __device__ __forceinline__ uint32_t kv4_transpose(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
+__device__ __forceinline__ float kv4_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 2^e, -126 <= e <= 127
+__device__ __forceinline__ float kv4_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
 // Nibbles 0 and 4 of a word as n, nibbles 1 and 5 as 16 n, two fp16 numbers: subnormal ones (of 2^-24) by a mask alone, or whole ones.
 // The tensor core lines products up by their factors' exponent fields, and a subnormal's is ten bits above its value: sums of
 // subnormal products keep about 2^-16 of themselves (measured: 1.9e-5), too few for fp32 results.
@@ -248,24 +273,54 @@ __device__ __forceinline__ uint32_t kv4_hi(uint32_t w) {
     return *(const uint32_t*)&h;
 }
 
-// ---- the state of a warp: running maximum, sum and output of its columns
-template <int DH, int NT>
-struct Kv4State {
-    float m[NT][2], l[NT][2];          // of columns 2 (lane % 4) and + 1 of every block of eight; l: this lane's rows only
-    float o[NT][DH / 16][4];           // V^T P^T, scaled by R and the codes' unit
-    float mn[NT][DH / 32][2];          // sum of p m per group, this lane's rows only
-    float R;                           // power of two that brings the values' scales to 2^5 .. 2^6
+// a column's four channels from ch on: the sum of its rows over the sum of their weights
+template <typename T>
+__device__ __forceinline__ void kv4_put(const Kv4AttnArgs& a, int b, int h, int j, int ch, int dh, const float4& o, float l) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;                    // nothing visible: zeros
+    const long long at = (long long)(b * a.n_q + j / a.G) * a.out_ld + (h * a.G + j % a.G) * dh + ch;
+    if constexpr (sizeof(T) == 2) {
+        const __nv_bfloat162 u = __floats2bfloat162_rn(o.x * inv, o.y * inv), v = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+        *(uint2*)((bf16*)a.out + at) = make_uint2(*(const unsigned*)&u, *(const unsigned*)&v);
+    } else {
+        *(float4*)((float*)a.out + at) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    }
+}
+
+// The number bf16 w's half h (0 lower, 1 upper) stands for.
+__device__ __forceinline__ float kv4_bf(uint32_t w, int h) { return h ? bf16_hi(w) : bf16_lo(w); }
+
+#define KV4_NOTHING -1e30f     // the running maximum of a column that has seen no row
+
+// ---- what a warp keeps: the queries, and the running maximum, sum and output of its columns
+template <int DH, int NT, bool SPLIT>
+struct Kv4Warp {
+    static constexpr int Q = DH / 32;
+    uint32_t q[NT][2 * Q][2];                   // B fragments of the queries
+    uint32_t ql[SPLIT ? NT : 1][2 * Q][2];      // fp32: what the first rounding left
+    uint32_t qm[SPLIT ? 1 : NT][2];             // B fragment of sum(q_g) in bf16 parts
+    float qs[SPLIT ? NT : 1][Q][2];             // fp32: sum(q_g) of columns 2 (lane % 4) and + 1
+    float fq[NT][2];                            // of those columns: what a sum is to be multiplied with
+    float m[NT][2], l[NT][2];                   // l: this lane's rows only
+    float o[NT][2 * Q][4];                      // V^T P^T, scaled by R and the codes' unit
+    float mn[NT][Q][2];                         // sum of p m per group, this lane's rows only
+    float R;                                    // power of two that brings the values' scales below 2^6
+    uint32_t r_limit;                           // the bf16 scale from which on R is too large
 };
 
-template <int DH, int NT>
-__device__ __forceinline__ void kv4_rescale(Kv4State<DH, NT>& st, int t, float f0, float f1) {
-#pragma unroll
-    for (int i = 0; i < DH / 16; ++i) { st.o[t][i][0] *= f0; st.o[t][i][1] *= f1; st.o[t][i][2] *= f0; st.o[t][i][3] *= f1; }
-#pragma unroll
-    for (int w = 0; w < DH / 32; ++w) { st.mn[t][w][0] *= f0; st.mn[t][w][1] *= f1; }
-    st.l[t][0] *= f0;
-    st.l[t][1] *= f1;
-}
+// How far the maximum may fall behind: p < 2^8, so that p s R < 2^14 stays inside fp16.
+#define KV4_LAZY 8.f
+
+struct Kv4Sight {              // which rows the columns see
+    int nrows, n_q, mask_rows;
+    const uint32_t* mask;      // of the sequence; nullable
+    int mask_words;
+    __device__ __forceinline__ bool operator()(int r, int i) const {
+        if (!mask) return r <= nrows - n_q + i;
+        const int k = r - (nrows - mask_rows);
+        return k < 0 || (r < nrows && ((mask[(long long)i * mask_words + (k >> 5)] >> (k & 31)) & 1u));
+    }
+};
+
 __device__ __forceinline__ float kv4_max_rows(float x) {       // over the lanes that hold other rows of the same columns
     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
@@ -277,38 +332,190 @@ __device__ __forceinline__ float kv4_sum_rows(float x) {
     return x + __shfl_xor_sync(0xffffffffu, x, 16);
 }
 
+// One tile of 16 rows from `row` on.  EDGE: some of them are not for every column, or not there at all.
+template <int DH, int NT, bool SPLIT, bool EDGE>
+__device__ __forceinline__ void kv4_rows16(Kv4Warp<DH, NT, SPLIT>& st, const unsigned char* tile, int row, int lane, int j0, int G,
+                                           const Kv4Sight& sight) {
+    constexpr int Q = DH / 32, CH = DH / 8, H = Q / 2;
+    const int g = lane >> 2, c = lane & 3;
+    const int r0 = row + g, r1 = r0 + 8;                          // this lane's rows
+    uint32_t p0[Q], p1[Q];                                        // s of the groups two by two, then m
+    kv4_lds<Q>(tile + 16 * DH + g * CH, p0);
+    kv4_lds<Q>(tile + 17 * DH + g * CH, p1);
+    float s[NT][4];
+    {
+        uint32_t k0[Q], k1[Q];
+        kv4_lds<Q>(tile + g * (DH / 2) + c * CH, k0);
+        kv4_lds<Q>(tile + (g + 8) * (DH / 2) + c * CH, k1);
+        if constexpr (!SPLIT) {
+            // the lane's columns of A: the m of groups 2 c and 2 c + 1, the groups over and over again
+            const uint32_t m0 = H == 2 && (c & 1) ? p0[H + 1] : p0[H], m1 = H == 2 && (c & 1) ? p1[H + 1] : p1[H];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) kv4_mma0_bf16(s[n], m0, m1, m0, m1, st.qm[n][0], st.qm[n][1]);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        }
+#pragma unroll
+        for (int w = 0; w < Q; ++w) {
+            const uint32_t x0 = k0[w], x1 = k1[w], y0 = x0 >> 8, y1 = x1 >> 8;
+            const uint32_t f0 = kv4_lo<SPLIT>(x0), f1 = kv4_lo<SPLIT>(x1), f2 = kv4_hi<SPLIT>(x0), f3 = kv4_hi<SPLIT>(x1);
+            const uint32_t h0 = kv4_lo<SPLIT>(y0), h1 = kv4_lo<SPLIT>(y1), h2 = kv4_hi<SPLIT>(y0), h3 = kv4_hi<SPLIT>(y1);
+            const float sc0 = kv4_bf(p0[w >> 1], w & 1), sc1 = kv4_bf(p1[w >> 1], w & 1);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float d[4];
+                kv4_mma0(d, f0, f1, f2, f3, st.q[n][2 * w][0], st.q[n][2 * w][1]);
+                kv4_mma(d, h0, h1, h2, h3, st.q[n][2 * w + 1][0], st.q[n][2 * w + 1][1]);
+                if constexpr (SPLIT) {
+                    kv4_mma(d, f0, f1, f2, f3, st.ql[n][2 * w][0], st.ql[n][2 * w][1]);
+                    kv4_mma(d, h0, h1, h2, h3, st.ql[n][2 * w + 1][0], st.ql[n][2 * w + 1][1]);
+                    const float mn0 = kv4_bf(p0[H + (w >> 1)], w & 1), mn1 = kv4_bf(p1[H + (w >> 1)], w & 1);
+                    s[n][0] = fmaf(mn0, st.qs[n][w][0], s[n][0]);
+                    s[n][1] = fmaf(mn0, st.qs[n][w][1], s[n][1]);
+                    s[n][2] = fmaf(mn1, st.qs[n][w][0], s[n][2]);
+                    s[n][3] = fmaf(mn1, st.qs[n][w][1], s[n][3]);
+                }
+                s[n][0] = fmaf(sc0, d[0], s[n][0]);
+                s[n][1] = fmaf(sc0, d[1], s[n][1]);
+                s[n][2] = fmaf(sc1, d[2], s[n][2]);
+                s[n][3] = fmaf(sc1, d[3], s[n][3]);
+            }
+        }
+    }
+    // ---- scores above the running maximum, in powers of two
+    float p[NT][4], top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (EDGE)
+                if (!sight(e < 2 ? r0 : r1, min((j0 + 8 * n + 2 * c + (e & 1)) / G, sight.n_q - 1))) s[n][e] = -INFINITY;
+            p[n][e] = fmaf(s[n][e], st.fq[n][e & 1], -st.m[n][e & 1]);
+            top = fmaxf(top, p[n][e]);
+        }
+    }
+    if (__any_sync(0xffffffffu, top > KV4_LAZY)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float m = fmaxf(st.m[n][e], kv4_max_rows(fmaxf(s[n][e] * st.fq[n][e], s[n][e + 2] * st.fq[n][e])));
+                const float f = kv4_exp2(st.m[n][e] - m);
+                st.m[n][e] = m;
+                p[n][e] = fmaf(s[n][e], st.fq[n][e], -m);
+                p[n][e + 2] = fmaf(s[n][e + 2], st.fq[n][e], -m);
+                st.l[n][e] *= f;
+#pragma unroll
+                for (int w = 0; w < Q; ++w) {
+                    st.mn[n][w][e] *= f;
+                    st.o[n][2 * w][e] *= f; st.o[n][2 * w][e + 2] *= f;
+                    st.o[n][2 * w + 1][e] *= f; st.o[n][2 * w + 1][e + 2] *= f;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[n][e] = kv4_exp2(p[n][e]);
+        st.l[n][0] += p[n][0] + p[n][2];
+        st.l[n][1] += p[n][1] + p[n][3];
+    }
+    // ---- the values
+    kv4_lds<Q>(tile + 18 * DH + g * CH, p0);
+    kv4_lds<Q>(tile + 19 * DH + g * CH, p1);
+    if constexpr (EDGE) {
+        // what lies behind the last row is anything at all
+#pragma unroll
+        for (int w = 0; w < Q; ++w) {
+            if (r0 >= sight.nrows) p0[w] = 0u;
+            if (r1 >= sight.nrows) p1[w] = 0u;
+        }
+    }
+    {
+        // R follows the largest scale, by halves of words (no scale is negative; a NaN's is above all)
+        uint32_t big = 0u;
+#pragma unroll
+        for (int w = 0; w < H; ++w) big = __vmaxu2(big, __vmaxu2(p0[w], p1[w]));
+        if (__any_sync(0xffffffffu, max(big >> 16, big & 0xFFFFu) >= st.r_limit)) {
+            uint32_t fin = 0u;                                      // (rows that hold a NaN decide nothing)
+#pragma unroll
+            for (int w = 0; w < Q; ++w) {
+                const uint32_t u0 = (p0[w >> 1] >> (16 * (w & 1))) & 0xFFFFu, u1 = (p1[w >> 1] >> (16 * (w & 1))) & 0xFFFFu;
+                if (u0 < 0x7F80u) fin = max(fin, u0);
+                if (u1 < 0x7F80u) fin = max(fin, u1);
+            }
+            fin = __reduce_max_sync(0xffffffffu, fin);
+            const int e = min(max((int)(fin >> 7) - 127, -114), 114);       // scales are below 2^(e + 1)
+            const float R = kv4_pow2(5 - e);
+            if (R < st.R) {
+                const float f = R / st.R;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2 * Q; ++i)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) st.o[n][i][t] *= f;
+                st.R = R;
+                st.r_limit = (uint32_t)(e + 1 + 127) << 7;
+            }
+        }
+    }
+    uint32_t v0[Q], v1[Q];
+    kv4_lds<Q>(tile + 8 * DH + c * DH + g * CH, v0);
+    kv4_lds<Q>(tile + 8 * DH + (c + 4) * DH + g * CH, v1);
+#pragma unroll
+    for (int w = 0; w < Q; ++w) {
+        const float a0 = kv4_bf(p0[w >> 1], w & 1), a1 = kv4_bf(p1[w >> 1], w & 1);
+        const float mn0 = kv4_bf(p0[H + (w >> 1)], w & 1), mn1 = kv4_bf(p1[H + (w >> 1)], w & 1);
+        const uint32_t x0 = v0[w], x1 = v1[w], y0 = x0 >> 8, y1 = x1 >> 8;
+        const uint32_t f0 = kv4_lo<SPLIT>(x0), f1 = kv4_hi<SPLIT>(x0), f2 = kv4_lo<SPLIT>(x1), f3 = kv4_hi<SPLIT>(x1);
+        const uint32_t g0 = kv4_lo<SPLIT>(y0), g1 = kv4_hi<SPLIT>(y0), g2 = kv4_lo<SPLIT>(y1), g3 = kv4_hi<SPLIT>(y1);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float ps[4] = {p[n][0] * st.R * a0, p[n][1] * st.R * a0, p[n][2] * st.R * a1, p[n][3] * st.R * a1};
+            if constexpr (EDGE) {
+                // a column that does not see the row takes nothing of it, not even a NaN
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (p[n][e] == 0.f) ps[e] = 0.f;
+                st.mn[n][w][0] += (p[n][0] == 0.f ? 0.f : p[n][0] * mn0) + (p[n][2] == 0.f ? 0.f : p[n][2] * mn1);
+                st.mn[n][w][1] += (p[n][1] == 0.f ? 0.f : p[n][1] * mn0) + (p[n][3] == 0.f ? 0.f : p[n][3] * mn1);
+            } else {
+                st.mn[n][w][0] = fmaf(p[n][0], mn0, fmaf(p[n][2], mn1, st.mn[n][w][0]));
+                st.mn[n][w][1] = fmaf(p[n][1], mn0, fmaf(p[n][3], mn1, st.mn[n][w][1]));
+            }
+            const uint32_t h0 = kv4_half2(ps[0], ps[1]), h1 = kv4_half2(ps[2], ps[3]);
+            const uint32_t b0 = kv4_transpose(h0), b1 = kv4_transpose(h1);
+            if constexpr (SPLIT) {
+                const float2 w0 = kv4_unhalf2(h0), w1 = kv4_unhalf2(h1);
+                const uint32_t c0 = kv4_transpose(kv4_half2(ps[0] - w0.x, ps[1] - w0.y)), c1 = kv4_transpose(kv4_half2(ps[2] - w1.x, ps[3] - w1.y));
+                float d[4], u[4];
+                kv4_mma0(d, f0, f1, f2, f3, c0, c1);
+                kv4_mma(d, f0, f1, f2, f3, b0, b1);
+                kv4_mma0(u, g0, g1, g2, g3, c0, c1);
+                kv4_mma(u, g0, g1, g2, g3, b0, b1);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    st.o[n][2 * w][e] += d[e];
+                    st.o[n][2 * w + 1][e] += u[e];
+                }
+            } else {
+                kv4_mma(st.o[n][2 * w], f0, f1, f2, f3, b0, b1);
+                kv4_mma(st.o[n][2 * w + 1], g0, g1, g2, g3, b0, b1);
+            }
+        }
+    }
+}
+
+// The queries as B fragments: column lane / 4 of every block of eight, channels 32 w + 8 (lane % 4) + 0..7 of every group.
 template <int DH, int NT, typename T>
-__global__ void __launch_bounds__(KV4_WARPS * 32) kv4_attn_kernel(const __grid_constant__ Kv4AttnArgs a) {
-    constexpr int Q = DH / 32, NB = 8 * NT, LDO = DH + 4;
+__device__ __forceinline__ void kv4_load_queries(Kv4Warp<DH, NT, sizeof(T) == 4>& st, const Kv4AttnArgs& a, int b, int h, int j0, int lane) {
     constexpr bool SPLIT = sizeof(T) == 4;
-    constexpr float UNIT = SPLIT ? 1.f : 0x1p-24f;     // what a code of 1 is to the tensor core
-    constexpr float LAZY = 8.f;        // the running maximum is raised once a score is above it by 2^8 (see the state's R: p s R < 2^14)
-    extern __shared__ float sm[];
-    float* sO = sm;                                 // [warp][column][LDO]
-    float* sM = sO + KV4_WARPS * NB * LDO;          // [warp][column]
-    float* sL = sM + KV4_WARPS * NB;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    const int b = blockIdx.z, h = blockIdx.y / a.n_blocks, j0 = (blockIdx.y % a.n_blocks) * NB;
-    const int rank = blockIdx.x, S = gridDim.x;     // (a cluster is the x extent of the grid)
-    pdl_wait();
-    pdl_trigger();
-    const int nrows = min(max(a.rows[b], 0), a.c.max_len);
-    const int i_first = j0 / a.G, i_last = min(j0 + NB, a.ncol) - 1 < 0 ? 0 : (min(j0 + NB, a.ncol) - 1) / a.G;
-    // rows [0, clear) are visible to every column of the block, rows from `end` on to none
-    const int clear = max(0, a.mask ? nrows - a.mask_rows : nrows - a.n_q + i_first + 1);
-    const int end = max(0, a.mask ? nrows : nrows - a.n_q + i_last + 1);
-    const int ntile = (end + 15) >> 4;
-    const long long row0 = kv4_row0(a.c, a.sl.slot[b], h);
-
-    int t = rank * KV4_WARPS + warp;
-    const int step = S * KV4_WARPS;
-    Kv4Tile<Q> tile;
-    if (t < ntile) kv4_load_tile<DH>(a.c, row0 + t * 16, lane, tile);
-
-    // ---- queries: column lane / 4 of every block of eight, channels 32 w + 8 (lane % 4) + 0..7 of every group
-    uint32_t qb[NT][2 * Q][2], ql[SPLIT ? NT : 1][2 * Q][2];
-    float fq[NT][2], qs[NT][Q][2];      // of columns 2 c and 2 c + 1: what a sum is to be multiplied with; sum of q per group
-    int ci[NT][2];                      // query row of those columns
+    constexpr int Q = DH / 32;
+    constexpr float UNIT = SPLIT ? 1.f : 0x1p-24f;                // what a code of 1 is to the tensor core
+    const int g = lane >> 2, c = lane & 3;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int j = j0 + 8 * n + g;
@@ -327,8 +534,9 @@ __global__ void __launch_bounds__(KV4_WARPS * 32) kv4_attn_kernel(const __grid_c
         }
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        const int e = mx > 0.f ? min(max(ilogbf(mx), -100), 100) : 0;
-        const float up = scalbnf(1.f, 14 - e);
+        // the row's largest number to 2^14 .. 2^15 (a row of zeros, or below 2^-100, or beyond 2^100, as far as that goes)
+        const int e = mx > 0.f ? min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 100) : 0;
+        const float up = kv4_pow2(14 - e);
         float sum[Q];
 #pragma unroll
         for (int w = 0; w < Q; ++w) {
@@ -344,12 +552,12 @@ __global__ void __launch_bounds__(KV4_WARPS * 32) kv4_attn_kernel(const __grid_c
                     const float2 back = kv4_unhalf2(hi);
                     const float f = r ? 0.0625f : 1.f;
                     sum[w] += back.x + back.y;
-                    qb[n][2 * w + s][r] = kv4_half2(back.x * f, back.y * f);
+                    st.q[n][2 * w + s][r] = kv4_half2(back.x * f, back.y * f);
                     if constexpr (SPLIT) {
                         const uint32_t lo = kv4_half2(y[2 * r] - back.x, y[2 * r + 1] - back.y);
                         const float2 bl = kv4_unhalf2(lo);
                         sum[w] += bl.x + bl.y;
-                        ql[n][2 * w + s][r] = kv4_half2(bl.x * f, bl.y * f);
+                        st.ql[n][2 * w + s][r] = kv4_half2(bl.x * f, bl.y * f);
                     }
                 }
             }
@@ -357,185 +565,135 @@ __global__ void __launch_bounds__(KV4_WARPS * 32) kv4_attn_kernel(const __grid_c
             sum[w] += __shfl_xor_sync(0xffffffffu, sum[w], 2);
             sum[w] *= UNIT;                                       // in the unit of the products
         }
-        const float f = scalbnf(a.scale_log2, e - 14) * (1.f / UNIT);
+        if constexpr (!SPLIT) {
+            // sum(q_g) = hi + mid + lo, eight bits each.  Rows 2 c, 2 c + 1 of B: groups 2 (c % (Q / 2)) and + 1, part c / (Q / 2) (four
+            // groups: lo comes in rows 2 c + 8, 2 c + 9 of c = 0, 1; two groups: c = 3 has nothing)
+            float part[Q][3];
+#pragma unroll
+            for (int w = 0; w < Q; ++w) {
+                part[w][0] = __bfloat162float(__float2bfloat16_rn(sum[w]));
+                part[w][1] = __bfloat162float(__float2bfloat16_rn(sum[w] - part[w][0]));
+                part[w][2] = sum[w] - part[w][0] - part[w][1];
+            }
+            auto pair = [](float x, float y) {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+                return *(const uint32_t*)&v;
+            };
+            if constexpr (Q == 4) {
+                const uint32_t b00 = pair(part[0][0], part[1][0]), b01 = pair(part[2][0], part[3][0]);
+                const uint32_t b10 = pair(part[0][1], part[1][1]), b11 = pair(part[2][1], part[3][1]);
+                const uint32_t b20 = pair(part[0][2], part[1][2]), b21 = pair(part[2][2], part[3][2]);
+                st.qm[n][0] = c == 0 ? b00 : c == 1 ? b01 : c == 2 ? b10 : b11;
+                st.qm[n][1] = c == 0 ? b20 : c == 1 ? b21 : 0u;
+            } else {
+                const uint32_t b0 = pair(part[0][0], part[1][0]), b1 = pair(part[0][1], part[1][1]), b2 = pair(part[0][2], part[1][2]);
+                st.qm[n][0] = c == 0 ? b0 : c == 1 ? b1 : c == 2 ? b2 : 0u;
+                st.qm[n][1] = 0u;
+            }
+        }
+        const float f = kv4_pow2(e - 14) * (1.f / UNIT) * a.scale_log2;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int from = (2 * c + s) * 4;                     // a lane with lane / 4 = 2 c + s
-            fq[n][s] = __shfl_sync(0xffffffffu, f, from);
+            st.fq[n][s] = __shfl_sync(0xffffffffu, f, from);
+            if constexpr (SPLIT) {
 #pragma unroll
-            for (int w = 0; w < Q; ++w) qs[n][w][s] = __shfl_sync(0xffffffffu, sum[w], from);
-            const int jc = j0 + 8 * n + 2 * c + s;
-            ci[n][s] = jc < a.ncol ? jc / a.G : 0;
+                for (int w = 0; w < Q; ++w) st.qs[n][w][s] = __shfl_sync(0xffffffffu, sum[w], from);
+            }
         }
     }
+}
 
-    Kv4State<DH, NT> st;
+// Shared memory: the warps' rings, and over them, once they are used up, [warp][column][DH + 4] outputs, maxima and sums.
+template <int DH, int NT>
+__host__ __device__ constexpr size_t kv4_smem(int warps) {
+    const size_t ring = (size_t)warps * KV4_STAGES * kv4_tile_bytes(DH), join = sizeof(float) * 8 * NT * (warps * (DH + 4 + 2) + 2);
+    return ring > join ? ring : join;
+}
+
+template <int DH, int NT, typename T, int WARPS, int CTAS>
+__global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid_constant__ Kv4AttnArgs a) {
+    constexpr bool SPLIT = sizeof(T) == 4;
+    constexpr int Q = DH / 32, NB = 8 * NT, LDO = DH + 4, TB = kv4_tile_bytes(DH);
+    constexpr float UNIT = SPLIT ? 1.f : 0x1p-24f;
+    extern __shared__ __align__(128) unsigned char kv4_sm[];
+    __shared__ u64 bars[WARPS][KV4_STAGES];
+    float* sO = (float*)kv4_sm;                     // [warp][column][LDO]
+    float* sM = sO + WARPS * NB * LDO;              // [warp][column]
+    float* sL = sM + WARPS * NB;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int b = blockIdx.z, h = blockIdx.y / a.n_blocks, j0 = (blockIdx.y % a.n_blocks) * NB;
+    const int rank = blockIdx.x, S = gridDim.x;     // (a cluster is the x extent of the grid)
+    const uint32_t bar = kv4_saddr(bars[warp]), ring = kv4_saddr(kv4_sm) + warp * KV4_STAGES * TB;
+    if (lane < KV4_STAGES) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + lane * 8) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");
+    __syncwarp();
+    pdl_wait();
+    pdl_trigger();
+    Kv4Sight sight;
+    sight.nrows = min(max(a.rows[b], 0), a.c.max_len);
+    sight.n_q = a.n_q; sight.mask_rows = a.mask_rows; sight.mask_words = a.mask_words;
+    sight.mask = a.mask ? a.mask + (long long)b * a.n_q * a.mask_words : nullptr;
+    const int i_first = j0 / a.G, i_last = (min(j0 + NB, a.ncol) - 1) / a.G;
+    // rows [0, clear) are visible to every column of the block, rows from `end` on to none
+    const int clear = max(0, a.mask ? sight.nrows - a.mask_rows : sight.nrows - a.n_q + i_first + 1);
+    const int end = max(0, a.mask ? sight.nrows : sight.nrows - a.n_q + i_last + 1);
+    const int ntile = (end + KV4_TILE - 1) / KV4_TILE, nfull = clear / KV4_TILE;
+    const unsigned char* base = kv4_tile(a.c, a.sl.slot[b], h, 0);
+    const int first = rank * WARPS + warp, step = S * WARPS;
+
+    const unsigned char* next = base + (long long)first * TB;
+    int ahead = first;                              // the next tile to be fetched
+#pragma unroll
+    for (int i = 0; i < KV4_STAGES; ++i) {
+        if (ahead < ntile && lane == 0) kv4_fetch(ring + i * TB, next, TB, bar + i * 8);
+        ahead += step;
+        next += (long long)step * TB;
+    }
+    Kv4Warp<DH, NT, SPLIT> st;
+    kv4_load_queries<DH, NT, T>(st, a, b, h, j0, lane);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            st.m[n][s] = -INFINITY;
+            st.m[n][s] = KV4_NOTHING;
             st.l[n][s] = 0.f;
 #pragma unroll
             for (int w = 0; w < Q; ++w) st.mn[n][w][s] = 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < DH / 16; ++i)
+        for (int i = 0; i < 2 * Q; ++i)
 #pragma unroll
             for (int s = 0; s < 4; ++s) st.o[n][i][s] = 0.f;
     }
-    st.R = 0x1p120f;
+    st.R = 0x1p119f;
+    st.r_limit = (uint32_t)(127 - 113) << 7;
 
-    for (; t < ntile; t += step) {
-        Kv4Tile<Q> cur = tile;
-        if (t + step < ntile) kv4_load_tile<DH>(a.c, row0 + (t + step) * 16, lane, tile);
-        const int r0 = t * 16 + g, r1 = r0 + 8;                   // this lane's rows
-        const bool edge = t * 16 + 16 > clear;                    // some row is not for every column
-        if (edge) {
-            // what lies behind the last row is anything at all
-#pragma unroll
-            for (int w = 0; w < Q; ++w) {
-                if (r0 >= nrows) cur.kp0[w] = cur.vp0[w] = 0u;
-                if (r1 >= nrows) cur.kp1[w] = cur.vp1[w] = 0u;
-            }
-        }
-        // ---- scores
-        float s[NT][4];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-#pragma unroll
-        for (int w = 0; w < Q; ++w) {
-            const uint32_t x0 = cur.k0[w], x1 = cur.k1[w], y0 = x0 >> 8, y1 = x1 >> 8;
-            const uint32_t f0 = kv4_lo<SPLIT>(x0), f1 = kv4_lo<SPLIT>(x1), f2 = kv4_hi<SPLIT>(x0), f3 = kv4_hi<SPLIT>(x1);
-            const uint32_t h0 = kv4_lo<SPLIT>(y0), h1 = kv4_lo<SPLIT>(y1), h2 = kv4_hi<SPLIT>(y0), h3 = kv4_hi<SPLIT>(y1);
-            const float sc0 = kv4_scale(cur.kp0[w]), sc1 = kv4_scale(cur.kp1[w]), mn0 = kv4_min(cur.kp0[w]), mn1 = kv4_min(cur.kp1[w]);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float d[4] = {0.f, 0.f, 0.f, 0.f};
-                kv4_mma(d, f0, f1, f2, f3, qb[n][2 * w][0], qb[n][2 * w][1]);
-                kv4_mma(d, h0, h1, h2, h3, qb[n][2 * w + 1][0], qb[n][2 * w + 1][1]);
-                if constexpr (SPLIT) {
-                    kv4_mma(d, f0, f1, f2, f3, ql[n][2 * w][0], ql[n][2 * w][1]);
-                    kv4_mma(d, h0, h1, h2, h3, ql[n][2 * w + 1][0], ql[n][2 * w + 1][1]);
-                }
-                s[n][0] = fmaf(mn0, qs[n][w][0], fmaf(sc0, d[0], s[n][0]));
-                s[n][1] = fmaf(mn0, qs[n][w][1], fmaf(sc0, d[1], s[n][1]));
-                s[n][2] = fmaf(mn1, qs[n][w][0], fmaf(sc1, d[2], s[n][2]));
-                s[n][3] = fmaf(mn1, qs[n][w][1], fmaf(sc1, d[3], s[n][3]));
-            }
-        }
-        bool raise = edge;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[n][e] *= fq[n][e & 1];
-                if (edge) {
-                    const int r = e < 2 ? r0 : r1, i = ci[n][e & 1];
-                    bool see;
-                    if (!a.mask) {
-                        see = r <= nrows - a.n_q + i;
-                    } else {
-                        const int k = r - (nrows - a.mask_rows);
-                        see = k < 0 || (r < nrows && ((a.mask[((long long)b * a.n_q + i) * a.mask_words + (k >> 5)] >> (k & 31)) & 1u));
-                    }
-                    if (!see) s[n][e] = -INFINITY;
-                }
-                raise |= s[n][e] > st.m[n][e & 1] + LAZY;
-            }
-        }
-        if (__any_sync(0xffffffffu, raise)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float f[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float m = fmaxf(st.m[n][e], kv4_max_rows(fmaxf(s[n][e], s[n][e + 2])));
-                    f[e] = m == st.m[n][e] ? 1.f : exp2f(st.m[n][e] - m);
-                    st.m[n][e] = m;
-                }
-                kv4_rescale<DH, NT>(st, n, f[0], f[1]);
-            }
-        }
-        // ---- the values' scales, as multiples of 1 / R
-        {
-            uint32_t top = 0u;
-#pragma unroll
-            for (int w = 0; w < Q; ++w) top = max(top, max(cur.vp0[w], cur.vp1[w]));
-            if (__any_sync(0xffffffffu, top >= __float_as_uint(64.f / st.R))) {
-                uint32_t fin = 0u;                                  // (rows that hold a NaN decide nothing)
-#pragma unroll
-                for (int w = 0; w < Q; ++w) {
-                    if (cur.vp0[w] < 0x7F800000u) fin = max(fin, cur.vp0[w]);
-                    if (cur.vp1[w] < 0x7F800000u) fin = max(fin, cur.vp1[w]);
-                }
-                fin = __reduce_max_sync(0xffffffffu, fin);
-                const float R = __uint_as_float((uint32_t)(127 + 5 + 127 - min(max((int)(fin >> 23), 12), 250)) << 23);
-                if (R < st.R) {
-                    const float f = R / st.R;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < DH / 16; ++i)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) st.o[n][i][e] *= f;
-                    st.R = R;
-                }
-            }
-        }
-        // ---- probabilities, and the part of the output that the codes do not carry
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float m = st.m[n][e & 1];
-                s[n][e] = exp2f(s[n][e] - (m == -INFINITY ? 0.f : m));
-            }
-            st.l[n][0] += s[n][0] + s[n][2];
-            st.l[n][1] += s[n][1] + s[n][3];
-        }
-#pragma unroll
-        for (int w = 0; w < Q; ++w) {
-            const float a0 = kv4_scale(cur.vp0[w]) * st.R, a1 = kv4_scale(cur.vp1[w]) * st.R, mn0 = kv4_min(cur.vp0[w]), mn1 = kv4_min(cur.vp1[w]);
-            const uint32_t x0 = cur.v0[w], x1 = cur.v1[w], y0 = x0 >> 8, y1 = x1 >> 8;
-            const uint32_t f0 = kv4_lo<SPLIT>(x0), f1 = kv4_hi<SPLIT>(x0), f2 = kv4_lo<SPLIT>(x1), f3 = kv4_hi<SPLIT>(x1);
-            const uint32_t g0 = kv4_lo<SPLIT>(y0), g1 = kv4_hi<SPLIT>(y0), g2 = kv4_lo<SPLIT>(y1), g3 = kv4_hi<SPLIT>(y1);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float p[4] = {s[n][0] * a0, s[n][1] * a0, s[n][2] * a1, s[n][3] * a1};
-                if (edge) {
-                    // a column that does not see the row takes nothing of it, not even a NaN
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (s[n][e] == 0.f) p[e] = 0.f;
-                    st.mn[n][w][0] += (s[n][0] == 0.f ? 0.f : s[n][0] * mn0) + (s[n][2] == 0.f ? 0.f : s[n][2] * mn1);
-                    st.mn[n][w][1] += (s[n][1] == 0.f ? 0.f : s[n][1] * mn0) + (s[n][3] == 0.f ? 0.f : s[n][3] * mn1);
-                } else {
-                    st.mn[n][w][0] = fmaf(s[n][0], mn0, fmaf(s[n][2], mn1, st.mn[n][w][0]));
-                    st.mn[n][w][1] = fmaf(s[n][1], mn0, fmaf(s[n][3], mn1, st.mn[n][w][1]));
-                }
-                const uint32_t h0 = kv4_half2(p[0], p[1]), h1 = kv4_half2(p[2], p[3]);
-                const uint32_t b0 = kv4_transpose(h0), b1 = kv4_transpose(h1);
-                if constexpr (SPLIT) {
-                    const float2 w0 = kv4_unhalf2(h0), w1 = kv4_unhalf2(h1);
-                    const uint32_t c0 = kv4_transpose(kv4_half2(p[0] - w0.x, p[1] - w0.y)), c1 = kv4_transpose(kv4_half2(p[2] - w1.x, p[3] - w1.y));
-                    float d[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
-                    kv4_mma(d, f0, f1, f2, f3, c0, c1);
-                    kv4_mma(d, f0, f1, f2, f3, b0, b1);
-                    kv4_mma(u, g0, g1, g2, g3, c0, c1);
-                    kv4_mma(u, g0, g1, g2, g3, b0, b1);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        st.o[n][2 * w][e] += d[e];
-                        st.o[n][2 * w + 1][e] += u[e];
-                    }
-                } else {
-                    kv4_mma(st.o[n][2 * w], f0, f1, f2, f3, b0, b1);
-                    kv4_mma(st.o[n][2 * w + 1], g0, g1, g2, g3, b0, b1);
-                }
-            }
-        }
+    bool ok = true;
+    uint32_t stage = 0, parity = 0;
+    for (int t = first; t < ntile; t += step) {
+        ok = kv4_wait(bar + stage * 8, parity);
+        if (!ok) break;
+        const unsigned char* tile = kv4_sm + (warp * KV4_STAGES + stage) * TB;
+        if (t < nfull) kv4_rows16<DH, NT, SPLIT, false>(st, tile, t * KV4_TILE, lane, j0, a.G, sight);
+        else kv4_rows16<DH, NT, SPLIT, true>(st, tile, t * KV4_TILE, lane, j0, a.G, sight);
+        __syncwarp();
+        if (ahead < ntile && lane == 0) kv4_fetch(ring + stage * TB, next, TB, bar + stage * 8);
+        ahead += step;
+        next += (long long)step * TB;
+        if (++stage == KV4_STAGES) { stage = 0; parity ^= 1u; }
     }
+    if (!ok) {
+        // a copy has not come: what is in flight is waited for once more, and the result is NaN
+        for (int i = 0; i < KV4_STAGES; ++i) {
+            kv4_wait(bar + stage * 8, parity);
+            if (++stage == KV4_STAGES) { stage = 0; parity ^= 1u; }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) st.l[n][0] = st.l[n][1] = __uint_as_float(0x7FC00000u);
+    }
+    __syncthreads();                                // every ring is used up
 
     // ---- this warp's columns to shared memory: maximum, sum, output
     const float down = (1.f / UNIT) / st.R;
@@ -559,82 +717,66 @@ __global__ void __launch_bounds__(KV4_WARPS * 32) kv4_attn_kernel(const __grid_c
             }
         }
     __syncthreads();
-    // ---- the four warps of the CTA, into the first one's place
+    // ---- the warps of the CTA, into the first one's place
     const int cols = min(NB, a.ncol - j0);
-    for (int i = tid; i < cols * (DH / 4); i += KV4_WARPS * 32) {
+    for (int i = tid; i < cols * (DH / 4); i += WARPS * 32) {
         const int col = i / (DH / 4), ch = (i % (DH / 4)) * 4;
-        float m = -INFINITY;
+        float m = KV4_NOTHING, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < KV4_WARPS; ++w) m = fmaxf(m, sM[w * NB + col]);
+        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, sM[w * NB + col]);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < KV4_WARPS; ++w) {
-            const float mw = sM[w * NB + col];
-            if (mw == -INFINITY && m > -INFINITY) continue;        // (nothing seen; where every warp saw nothing all is zero)
-            const float f = m == mw ? 1.f : exp2f(mw - m);
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = kv4_exp2(sM[w * NB + col] - m);
             const float4 x = *(const float4*)(sO + (w * NB + col) * LDO + ch);
+            l = fmaf(sL[w * NB + col], f, l);
             o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
         }
-        *(float4*)(sO + col * LDO + ch) = o;
-    }
-    __syncthreads();
-    if (tid < cols) {
-        float m = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < KV4_WARPS; ++w) m = fmaxf(m, sM[w * NB + tid]);
-#pragma unroll
-        for (int w = 0; w < KV4_WARPS; ++w) {
-            const float mw = sM[w * NB + tid];
-            if (mw > -INFINITY || mw != mw) l = fmaf(sL[w * NB + tid], m == mw ? 1.f : exp2f(mw - m), l);
+        if (S == 1) {
+            kv4_put<T>(a, b, h, j0 + col, ch, DH, o, l);
+        } else {
+            *(float4*)(sO + col * LDO + ch) = o;
+            // (maxima and sums for the cluster go behind those of the warps, which other threads still read)
+            if (ch == 0) {
+                sM[2 * WARPS * NB + col] = m;
+                sM[2 * WARPS * NB + NB + col] = l;
+            }
         }
-        sM[tid] = m;
-        sL[tid] = l;
     }
-    cg::cluster_group cluster = cg::this_cluster();
-    if (S > 1) cluster.sync();
-    else __syncthreads();
+    if (S == 1) return;
     // ---- the CTAs of the cluster: each writes its share of the columns' channels
-    for (int i = rank * KV4_WARPS * 32 + tid; i < cols * (DH / 4); i += S * KV4_WARPS * 32) {
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    const float* cM = sM + 2 * WARPS * NB;
+    for (int i = rank * WARPS * 32 + tid; i < cols * (DH / 4); i += S * WARPS * 32) {
         const int col = i / (DH / 4), ch = (i % (DH / 4)) * 4;
-        float m = -INFINITY;
-        for (int r = 0; r < S; ++r) m = fmaxf(m, *(S > 1 ? cluster.map_shared_rank(sM + col, r) : sM + col));
-        float l = 0.f;
+        float m = KV4_NOTHING, l = 0.f;
+        for (int r = 0; r < S; ++r) m = fmaxf(m, *cluster.map_shared_rank(cM + col, r));
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int r = 0; r < S; ++r) {
-            const float mr = *(S > 1 ? cluster.map_shared_rank(sM + col, r) : sM + col);
-            const float lr = *(S > 1 ? cluster.map_shared_rank(sL + col, r) : sL + col);
-            const float4 x = *(const float4*)(S > 1 ? cluster.map_shared_rank(sO + col * LDO + ch, r) : sO + col * LDO + ch);
-            if (mr == -INFINITY && m > -INFINITY) continue;
-            const float f = m == mr ? 1.f : exp2f(mr - m);
-            l = fmaf(lr, f, l);
+            const float f = kv4_exp2(*cluster.map_shared_rank(cM + col, r) - m);
+            const float4 x = *(const float4*)cluster.map_shared_rank(sO + col * LDO + ch, r);
+            l = fmaf(*cluster.map_shared_rank(cM + NB + col, r), f, l);
             o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;                // nothing visible: zeros
-        const int j = j0 + col;
-        const long long at = (long long)(b * a.n_q + j / a.G) * a.out_ld + (h * a.G + j % a.G) * DH + ch;
-        if constexpr (sizeof(T) == 2) {
-            const __nv_bfloat162 u = __floats2bfloat162_rn(o.x * inv, o.y * inv), v = __floats2bfloat162_rn(o.z * inv, o.w * inv);
-            *(uint2*)((bf16*)a.out + at) = make_uint2(*(const unsigned*)&u, *(const unsigned*)&v);
-        } else {
-            *(float4*)((float*)a.out + at) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        }
+        kv4_put<T>(a, b, h, j0 + col, ch, DH, o, l);
     }
-    if (S > 1) cluster.sync();          // nobody leaves while its shared memory may still be read
+    cluster.sync();          // nobody leaves while its shared memory may still be read
 }
 
-// CTAs per (sequence, KV head, block of columns): a power of two, so many that the GPU's SMs have about four CTAs each, but not
-// more than there are tiles of 16 rows for their warps at the cache's full length.
-static int kv4_cluster(int units, int max_len, int num_sms) {
-    int s = 1;
-    while (s < KV4_MAX_CLUSTER && units * s < 4 * num_sms && s * 2 * KV4_WARPS * 16 <= max_len) s *= 2;
-    return s;
+// CTAs per (sequence, KV head, block of columns): as many as the GPU holds at once, but no more than the cache's full length has
+// tiles for their warps.
+static int kv4_cluster(int units, int max_len, int warps, int resident) {
+    const int most = max_len / (KV4_TILE * warps), want = resident / units;
+    const int s = want < most ? want : most;
+    return s < 1 ? 1 : s > KV4_MAX_CLUSTER ? KV4_MAX_CLUSTER : s;
 }
 
-template <int DH, int NT, typename T>
+template <int DH, int NT, typename T, int WARPS, int CTAS>
 static cudaError_t kv4_launch_attn(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
     constexpr int NB = 8 * NT;
-    const size_t smem = sizeof(float) * KV4_WARPS * NB * (DH + 4 + 2);
-    auto kernel = kv4_attn_kernel<DH, NT, T>;
+    constexpr size_t smem = kv4_smem<DH, NT>(WARPS);
+    auto kernel = kv4_attn_kernel<DH, NT, T, WARPS, CTAS>;
     static bool attr_set[HIVIS_MAX_DEVICES] = {false};
     if (dev < 0 || dev >= HIVIS_MAX_DEVICES || !attr_set[dev]) {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -643,10 +785,10 @@ static cudaError_t kv4_launch_attn(Kv4AttnArgs& a, int dev, int num_sms, cudaStr
         if (dev >= 0 && dev < HIVIS_MAX_DEVICES) attr_set[dev] = true;
     }
     a.n_blocks = (a.ncol + NB - 1) / NB;
-    const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, num_sms);
+    const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, WARPS, num_sms * CTAS);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)S, (unsigned)(a.c.Hkv * a.n_blocks), (unsigned)a.sl.n);
-    cfg.blockDim = dim3(KV4_WARPS * 32);
+    cfg.blockDim = dim3(WARPS * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2] = {};
@@ -662,8 +804,8 @@ static cudaError_t kv4_launch_attn(Kv4AttnArgs& a, int dev, int num_sms, cudaStr
 
 template <int DH, typename T>
 static cudaError_t kv4_launch_attn_n(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
-    if (a.ncol <= 8) return kv4_launch_attn<DH, 1, T>(a, dev, num_sms, st);
-    return kv4_launch_attn<DH, 2, T>(a, dev, num_sms, st);
+    if (a.ncol <= 8) return kv4_launch_attn<DH, 1, T, 4, sizeof(T) == 4 ? 2 : 4>(a, dev, num_sms, st);
+    return kv4_launch_attn<DH, 2, T, 4, sizeof(T) == 4 ? 2 : 3>(a, dev, num_sms, st);
 }
 
 // ------------------------------------------------------------------------------------------------ C entries
@@ -684,9 +826,7 @@ static int kv4_check(const char* who, const hivis_kv4_cache* cache, int B, const
     if (cache->n_kv_heads < 1 || cache->n_kv_heads > 65535 || cache->n_slots < 1) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: n_kv_heads or n_slots out of range", who);
     if (cache->max_len < 32 || cache->max_len % 32 || cache->max_len > (1 << 28))
         KV4_FAIL(HIVIS_ERR_SHAPE, "%s: max_len must be a positive multiple of 32, at most 2^28", who);
-    if (!cache->k_codes || !cache->v_codes || !cache->k_params || !cache->v_params) KV4_FAIL(HIVIS_ERR_ARG, "%s: null buffer in the cache", who);
-    if (kv4_misaligned(cache->k_codes) || kv4_misaligned(cache->v_codes) || kv4_misaligned(cache->k_params) || kv4_misaligned(cache->v_params))
-        KV4_FAIL(HIVIS_ERR_ARG, "%s: a cache buffer is not 16-byte aligned", who);
+    if (!cache->data || kv4_misaligned(cache->data)) KV4_FAIL(HIVIS_ERR_ARG, "%s: the cache's buffer is null or not 16-byte aligned", who);
     if (B < 1 || B > HIVIS_MAX_BATCH) KV4_FAIL(HIVIS_ERR_CAPACITY, "%s: B=%d outside [1,%d]", who, B, HIVIS_MAX_BATCH);
     sl->n = B;
     for (int b = 0; b < B; ++b) {
@@ -696,10 +836,7 @@ static int kv4_check(const char* who, const hivis_kv4_cache* cache, int B, const
             if (sl->slot[i] == s) KV4_FAIL(HIVIS_ERR_ARG, "%s: slot %d listed twice", who, s);
         sl->slot[b] = s;
     }
-    c->k_codes = (unsigned char*)cache->k_codes;
-    c->v_codes = (unsigned char*)cache->v_codes;
-    c->k_params = (uint32_t*)cache->k_params;
-    c->v_params = (uint32_t*)cache->v_params;
+    c->data = (unsigned char*)cache->data;
     c->n_slots = cache->n_slots; c->Hkv = cache->n_kv_heads; c->max_len = cache->max_len; c->dh = cache->head_dim;
     return HIVIS_OK;
 }

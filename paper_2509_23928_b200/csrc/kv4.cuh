@@ -5,10 +5,10 @@
 // stands for m + s n.  Rounded this way round, m and m + 15 s enclose the group, so no value is off by more than s / 2.
 // A group that holds a NaN or an infinity, or whose range overflows, gets m = s = NaN.
 //
-// Parameters: one 32-bit word per group, s in the upper half and m in the lower (each is widened with one instruction),
-// [slot][KV head][row][group].
-// Codes: [slot][KV head][row] of dh / 2 bytes, in the order in which mma.m16n8k16 wants them as its A operand, so that the
-// attention takes them from memory to the tensor core with a mask and a shift:
+// Rows lie in tiles of 16, [slot][KV head][row / 16], 20 dh bytes each, so that one copy brings everything the attention needs of 16
+// rows: the codes of K (16 rows of dh / 2 bytes), those of V, then per row s and m of K's groups (dh / 32 bf16 numbers each), then V's.
+// Codes are in the order in which mma.m16n8k16 wants them as its A operand, so that the attention takes them from memory to the
+// tensor core with a mask and a shift:
 //   K  (A = keys: 16 rows x 16 channels).  A row is four chunks of dh / 8 bytes, chunk c for the lanes with lane % 4 = c; word w
 //      of a chunk holds channels 32 w + 8 c + i, nibble i.
 //   V  (A = values transposed: 16 channels x 16 rows).  A register holds one channel of two neighbouring rows, so rows 2 p and
@@ -20,17 +20,19 @@
 #include <cuda_fp16.h>
 
 struct Kv4View {
-    unsigned char *k_codes, *v_codes;
-    uint32_t *k_params, *v_params;
+    unsigned char* data;
     int n_slots, Hkv, max_len, dh;
 };
 #define KV4_GROUP 32
+#define KV4_TILE 16
+__host__ __device__ __forceinline__ constexpr int kv4_tile_bytes(int dh) { return 20 * dh; }
 
-// first row of a head, in rows: the codes are dh / 2 bytes and the parameters dh / 32 words a row on
-__device__ __forceinline__ long long kv4_row0(const Kv4View& c, int slot, int h) {
-    return ((long long)slot * c.Hkv + h) * c.max_len;
+// the tile of a head that holds `row`
+__device__ __forceinline__ unsigned char* kv4_tile(const Kv4View& c, int slot, int h, int row) {
+    return c.data + (((long long)slot * c.Hkv + h) * (c.max_len / KV4_TILE) + row / KV4_TILE) * kv4_tile_bytes(c.dh);
 }
 
+// A group's parameters in one word: s in the upper half, m in the lower.
 __device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float kv4_min(uint32_t w) { return __uint_as_float(w << 16); }
 
@@ -82,9 +84,9 @@ __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t par
     return w;
 }
 
-// Where the 8 codes of channels [32 w + 8 c, + 8) of a row go.  K: one word.  V: the lower four nibbles into the row's half of
-// word (dh / 32) (2 c) + w of its pair of rows, the upper four into word (dh / 32) (2 c + 1) + w.
-__device__ __forceinline__ long long kv4_k_offset(int dh, long long row, int w, int c) { return row * (dh / 2) + c * (dh / 8) + w * 4; }
-__device__ __forceinline__ long long kv4_v_offset(int dh, long long row, int w, int g) {
-    return (row & ~1ll) * (dh / 2) + ((dh / 32) * g + w) * 4 + (row & 1) * 2;
-}
+// Offsets in a tile, r = row % 16.  The 8 codes of channels [32 w + 8 c, + 8): K, one word; V, the lower four nibbles into the row's
+// half of word g = 2 c of the group, the upper four into that of g = 2 c + 1.  Parameters of group w (which: 0 K, 1 V).
+__device__ __forceinline__ int kv4_k_at(int dh, int r, int w, int c) { return r * (dh / 2) + c * (dh / 8) + w * 4; }
+__device__ __forceinline__ int kv4_v_at(int dh, int r, int w, int g) { return 8 * dh + (r & ~1) * (dh / 2) + ((dh / 32) * g + w) * 4 + (r & 1) * 2; }
+__device__ __forceinline__ int kv4_s_at(int dh, int which, int r, int w) { return (16 + 2 * which) * dh + r * (dh / 8) + 2 * w; }
+__device__ __forceinline__ int kv4_m_at(int dh, int which, int r, int w) { return kv4_s_at(dh, which, r, w) + dh / 16; }

@@ -27,8 +27,15 @@ def _ints(x):
     return _torch().tensor([int(i) for i in x], dtype=_torch().int32, device="cuda")
 
 
+def _all_rows(cache):
+    """[K, V], each [slots, max_len, heads, dh]: what every row of the cache stands for, written or not."""
+    n, L = cache.n_slots, cache.max_len
+    k, v = cache.read([L * i for i in range(n + 1)], _ints([0] * n))
+    return [x.cpu().numpy().reshape(n, L, cache.n_kv_heads, cache.head_dim) for x in (k, v)]
+
+
 def _bytes(cache):
-    return [x.cpu().numpy().copy() for x in cache.codes + cache.params]
+    return [cache.data.cpu().numpy().copy()]
 
 
 def _cache(*a):
@@ -54,7 +61,9 @@ def test_rows_are_held_as_the_format_says(dtype, dh, heads, counts, start):
     cache = _cache(B + 1, heads, dh, 64)
     slots = list(range(B, 0, -1))                                    # any order; slot 0 is not listed
     k, v = (_to(rng.standard_normal((total, heads, dh)) * 3 + rng.standard_normal((1, heads, dh)), dtype) for _ in range(2))
-    before = _bytes(cache)
+    old = _to(rng.standard_normal((64 * (B + 1), heads, dh)), "bf16")
+    cache.append(old, old, [64 * i for i in range(B + 2)], _ints([0] * (B + 1)))
+    before = _all_rows(cache)
     cache.append(k, v, cu, _ints(start), slots)
     k2, v2 = cache.read(cu, _ints(start), slots)
     t.cuda.synchronize()
@@ -62,14 +71,11 @@ def test_rows_are_held_as_the_format_says(dtype, dh, heads, counts, start):
         want = ref.values(*ref.quantise(_np(x)))
         # m + s n is one fp32 operation on exact numbers: half a step of fp32
         assert np.all(np.abs(_np(got) - want) <= 2.0 ** -24 * np.abs(want))
-    # nothing else has moved: the rows written are the only ones that differ from the start
-    for a, z in zip(before, _bytes(cache)):
-        touched = np.zeros(a.shape[:3], bool)
-        for b in range(B):
-            touched[slots[b], :, start[b]:start[b] + counts[b]] = True
-        if a.dtype == np.uint8:                                      # (a row's V codes lie in its pair's rows)
-            pair = touched.reshape(touched.shape[0], touched.shape[1], -1, 2).any(-1)
-            touched = np.repeat(pair, 2, axis=2)
+    # nothing else has moved
+    touched = np.zeros((B + 1, 64), bool)
+    for b in range(B):
+        touched[slots[b], start[b]:start[b] + counts[b]] = True
+    for a, z in zip(before, _all_rows(cache)):
         assert np.array_equal(a[~touched], z[~touched])
 
 
@@ -91,11 +97,11 @@ def test_rows_behind_the_cache_are_dropped():
     rng = np.random.default_rng(7)
     k, v = (_to(rng.standard_normal((40, 2, 64)), "bf16") for _ in range(2))
     cache = _cache(4, 2, 64, 32)
-    before = _bytes(cache)
+    before = _all_rows(cache)
     cache.append(k, v, [0, 10, 20, 30, 40], _ints([27, -1, 32, 2 ** 31 - 1]))
     t.cuda.synchronize()
-    for a, z in zip(before, _bytes(cache)):
-        assert np.array_equal(a[1:], z[1:]) and np.array_equal(a[0, :, :26], z[0, :, :26])
+    for a, z in zip(before, _all_rows(cache)):
+        assert np.array_equal(a[1:], z[1:]) and np.array_equal(a[0, :27], z[0, :27])
     got, _ = cache.read([0, 5], _ints([27]))
     want = ref.values(*ref.quantise(_np(k[:5])))
     assert np.all(np.abs(_np(got) - want) <= 2.0 ** -24 * np.abs(want))
@@ -175,8 +181,7 @@ class Filled:
         self.slots = slots
         self.cache = _cache(B if slots is None else max(slots) + 1, Hkv, dh, max_len or max(max(lens), 1))
         if fill is not None:                                          # what lies in the cache where no row was put
-            for x in self.cache.codes + self.cache.params:
-                x.fill_(fill)
+            self.cache.data.fill_(fill)
         total = sum(lens)
         k = rng.standard_normal((total, Hkv, dh)) + 2.0 * rng.standard_normal((1, Hkv, dh))
         v = rng.standard_normal((total, Hkv, dh)) * np.exp(spread * rng.uniform(-1, 1, (total, Hkv, 1)))

@@ -8,8 +8,7 @@ P = 0x10000                      # an address that is aligned and never read
 
 def _cache(**kw):
     from paper_2509_23928_b200.binding import hivis_kv4_cache
-    base = dict(struct_size=C.sizeof(hivis_kv4_cache), n_slots=4, n_kv_heads=2, head_dim=64, max_len=64, k_codes=P, v_codes=P,
-                k_params=P, v_params=P)
+    base = dict(struct_size=C.sizeof(hivis_kv4_cache), n_slots=4, n_kv_heads=2, head_dim=64, max_len=64, data=P)
     base.update(kw)
     return hivis_kv4_cache(**base)
 
@@ -36,8 +35,8 @@ def _attend(cache, B=2, slots=None, rows=P, n_q=1, heads=4, q=P, dtype=1, q_ld=2
 
 @pytest.mark.parametrize("kw,code", [
     (dict(struct_size=8), -1), (dict(head_dim=96), -2), (dict(head_dim=32), -2), (dict(n_kv_heads=0), -2), (dict(n_slots=0), -2),
-    (dict(max_len=0), -2), (dict(max_len=33), -2), (dict(max_len=2 ** 28 + 32), -2), (dict(k_codes=None), -1), (dict(v_codes=None), -1),
-    (dict(k_params=P + 8), -1), (dict(v_params=P + 4), -1), (dict(n_kv_heads=70000), -2),
+    (dict(max_len=0), -2), (dict(max_len=33), -2), (dict(max_len=2 ** 28 + 32), -2), (dict(data=None), -1),
+    (dict(data=P + 8), -1), (dict(n_kv_heads=70000), -2),
 ])
 def test_a_bad_cache_is_refused_by_every_call(kw, code):
     from paper_2509_23928_b200 import hivis_last_error
