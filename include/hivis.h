@@ -410,6 +410,26 @@ int hivis_kv4_attention(const hivis_kv4_cache* cache, int B, const int* seq_slot
                         int n_q_heads, const void* q, int dtype, int64_t q_ld, float scale, const uint32_t* mask,
                         int mask_rows, void* out, int64_t out_ld, void* stream);
 
+/* Log-probabilities of rows of logits: what a server returns for the tokens a verification committed, and what tells how
+ * sure a draft is.  (The paper has no counterpart.)  Needs no context or workspace and keeps nothing; each logit is read once.
+ * logits [n_rows, vocab] in logits_dtype (HIVIS_F32 | HIVIS_BF16), ld >= vocab elements from one row to the next (any number:
+ * rows need not be aligned); p = softmax(row / temperature).
+ *   ids (int32 [n_rows, n_ids], with n_ids > 0): out_logprobs fp32 [n_rows, n_ids] = log p of each; -infinity for a token
+ *   without mass and for an id outside [0, vocab).
+ *   out_entropy (nullable, fp32 [n_rows]): -sum p log p, in nats.
+ *   out_top_ids int32, out_top_logprobs fp32 [n_rows, top_n] (with top_n > 0): the most probable tokens, largest logit
+ *   first, the lowest id among equals; -1 and -infinity where no token with mass is left.
+ * A row without any mass (every logit -infinity): log-probabilities -infinity, entropy 0, no alternatives.  A row that holds
+ * a NaN or +infinity: NaN; its alternatives are tokens that are not NaN.  Sums are made in one order.
+ * Errors: CAPACITY (n_ids > HIVIS_LOGPROBS_MAX_IDS, top_n > HIVIS_LOGPROBS_MAX_TOP), SHAPE (vocab, ld), DTYPE, ARG, CUDA; the
+ * text is available from hivis_last_error(NULL).                                                                     */
+#define HIVIS_LOGPROBS_MAX_IDS 32
+#define HIVIS_LOGPROBS_MAX_TOP 32
+#define HIVIS_LOGPROBS_MAX_VOCAB (1 << 28)
+int hivis_logprobs(int n_rows, int vocab, const void* logits, int logits_dtype, int64_t ld, float temperature,
+                   const int32_t* ids, int n_ids, int top_n, float* out_logprobs, float* out_entropy,
+                   int32_t* out_top_ids, float* out_top_logprobs, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

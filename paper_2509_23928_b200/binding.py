@@ -3,7 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, Optional, Sequence
+from typing import Dict, NamedTuple, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libhivis.so")
@@ -18,7 +18,8 @@ EXPORTS = ("hivis_init", "hivis_destroy", "hivis_prefill", "hivis_draft", "hivis
            "hivis_get_kv_len", "hivis_set_kv_len", "hivis_read_kv", "hivis_debug_tap", "hivis_step_bytes",
            "hivis_launch_count", "hivis_last_error", "hivis_profile_begin", "hivis_profile_end", "hivis_set_option",
            "hivis_status", "hivis_verify_noalloc", "hivis_read_phase_times", "hivis_draft_tree", "hivis_verify_tree", "hivis_verify_sampled", "hivis_draft_sampled",
-           "hivis_set_kv_len_batch", "hivis_kv4_append", "hivis_kv4_read", "hivis_kv4_attention")
+           "hivis_set_kv_len_batch", "hivis_kv4_append", "hivis_kv4_read", "hivis_kv4_attention",
+           "hivis_logprobs")
 HIVIS_KV4_GROUP, HIVIS_KV4_MAX_QUERIES, HIVIS_KV4_MAX_MASK = 32, 64, 1024
 HIVIS_OPT_CHAIN_KERNEL = 0
 HIVIS_OPT_TC_KERNEL = 1
@@ -95,6 +96,7 @@ def _load() -> C.CDLL:
     L.hivis_kv4_append.argtypes = [cp, i32, ip, ip, vp, vp, vp, i32, C.c_int64, vp]
     L.hivis_kv4_read.argtypes = [cp, i32, ip, ip, vp, vp, vp, vp]
     L.hivis_kv4_attention.argtypes = [cp, i32, ip, vp, i32, i32, vp, i32, C.c_int64, C.c_float, vp, i32, vp, C.c_int64, vp]
+    L.hivis_logprobs.argtypes = [i32, i32, vp, i32, C.c_int64, C.c_float, vp, i32, i32, vp, vp, vp, vp, vp]
     L.hivis_last_error.argtypes = [vp]
     L.hivis_last_error.restype = C.c_char_p
     for n in EXPORTS:
@@ -221,6 +223,13 @@ def hivis_kv4_attention(cache, B, seq_slots, rows, n_q, n_q_heads, q, dtype, q_l
     _check(lib.hivis_kv4_attention(C.byref(cache), int(B), _ints(seq_slots), _ptr(rows), int(n_q), int(n_q_heads), _row_ptr(q),
                                    int(dtype), int(q_ld), float(scale), _ptr(mask), int(mask_rows), _row_ptr(out), int(out_ld),
                                    _stream(stream)))
+
+
+def hivis_logprobs(n_rows, vocab, logits, logits_dtype, ld, temperature, ids, n_ids, top_n, out_logprobs, out_entropy=None,
+                   out_top_ids=None, out_top_logprobs=None, stream=None):
+    _check(lib.hivis_logprobs(int(n_rows), int(vocab), _row_ptr(logits), int(logits_dtype), int(ld), float(temperature), _ptr(ids),
+                              int(n_ids), int(top_n), _ptr(out_logprobs), _ptr(out_entropy), _ptr(out_top_ids),
+                              _ptr(out_top_logprobs), _stream(stream)))
 
 
 def hivis_reset(ctx, slot, stream=None):
@@ -547,3 +556,37 @@ class Kv4Cache:
         hivis_kv4_attention(self.c, B, slots, rows, n_q, heads, q.data_ptr(), _dtype(q), q_ld,
                             self.head_dim ** -0.5 if scale is None else scale, mask, mask_rows, out.data_ptr(), out_ld)
         return out
+
+
+class Logprobs(NamedTuple):
+    """What `logprobs` returns; fields that were not asked for are None."""
+    logprobs: "object" = None       # fp32 [n_rows, n_ids]
+    entropy: "object" = None        # fp32 [n_rows]
+    top_ids: "object" = None        # int32 [n_rows, top_n]
+    top_logprobs: "object" = None   # fp32 [n_rows, top_n]
+
+
+def logprobs(logits, ids=None, temperature: float = 1.0, top_n: int = 0, entropy: bool = True) -> Logprobs:
+    """Log-probabilities of `ids` (int32 [n_rows, n_ids]) under softmax(logits / temperature), the rows' entropy and their
+    `top_n` most probable tokens; logits [n_rows, vocab], bf16 or fp32, rows may lie apart.  include/hivis.h: hivis_logprobs."""
+    import torch
+    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1:
+        raise ValueError(f"logits must be [n_rows, vocab] with contiguous rows, not {tuple(logits.shape)}")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor")
+    n, dev = logits.shape[0], logits.device
+    if torch.cuda.current_device() != dev.index:
+        with torch.cuda.device(dev):
+            return logprobs(logits, ids, temperature, top_n, entropy)
+    n_ids = 0
+    if ids is not None:
+        if ids.dtype != torch.int32 or ids.dim() != 2 or ids.shape[0] != n or ids.device != dev or not ids.is_contiguous():
+            raise ValueError("ids must be a contiguous int32 tensor [n_rows, n_ids] beside the logits")
+        n_ids = ids.shape[1]
+    lp = torch.empty((n, n_ids), dtype=torch.float32, device=dev) if n_ids else None
+    h = torch.empty((n,), dtype=torch.float32, device=dev) if entropy else None
+    top = torch.empty((n, top_n), dtype=torch.int32, device=dev) if top_n > 0 else None
+    top_lp = torch.empty((n, top_n), dtype=torch.float32, device=dev) if top_n > 0 else None
+    hivis_logprobs(n, logits.shape[1], logits.data_ptr(), _dtype(logits), logits.stride(0) if n > 1 else logits.shape[1], temperature,
+                   ids if n_ids else None, n_ids, top_n, lp, h, top, top_lp)
+    return Logprobs(lp, h, top, top_lp)
