@@ -465,14 +465,31 @@ class Drafter:
         return hivis_launch_count(self.ctx)
 
 
+_DTYPES = {}
+
+
 def _dtype(t) -> int:
     """HIVIS_F32 or HIVIS_BF16, whichever a tensor's element type is."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: HIVIS_F32, torch.bfloat16: HIVIS_BF16})
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"expected a bfloat16 or float32 tensor, not {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _slots(slots, B):
+    if slots is None:
+        return None
+    if len(slots) != B:
+        raise ValueError(f"{len(slots)} slots for {B} sequences")
+    return _ints(slots)
+
+
+def _raw_stream(index: int) -> int:
+    """The current stream of a device, without a Stream object around it."""
     import torch
-    if t.dtype == torch.bfloat16:
-        return HIVIS_BF16
-    if t.dtype == torch.float32:
-        return HIVIS_F32
-    raise TypeError(f"expected a bfloat16 or float32 tensor, not {t.dtype}")
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 class Kv4Cache:
@@ -490,71 +507,81 @@ class Kv4Cache:
         self.data = torch.zeros(self.n_slots * self.n_kv_heads * self.max_len * self.head_dim * 5 // 4, dtype=torch.uint8, device=self.dev)
         self.c = hivis_kv4_cache(C.sizeof(hivis_kv4_cache), self.n_slots, self.n_kv_heads, self.head_dim, self.max_len,
                                  self.data.data_ptr())
+        self._ref, self._scale = C.byref(self.c), self.head_dim ** -0.5
 
-    def _here(self, *tensors):
-        """Whether the cache's device is the current one; every tensor has to be on it."""
+    # (The checks below are written for few Python operations: on short sequences the host is what a call waits for.)
+    def _elsewhere(self, *tensors):
+        """Whether the cache's device is not the current one; every tensor has to be on it."""
         for t in tensors:
-            if t is not None and t.device != self.dev:
+            if t is not None and t.get_device() != self.dev.index:
                 raise ValueError(f"the cache is on {self.dev}, a tensor on {t.device}")
-        return self.torch.cuda.current_device() == self.dev.index
+        return self.torch.cuda.current_device() != self.dev.index
 
-    def _rows(self, t, n_heads, name, n_rows=None):
-        """[rows, heads, head_dim] with rows that may lie apart -> elements from one row to the next."""
-        if t.dim() != 3 or t.shape[1] != n_heads or t.shape[2] != self.head_dim or (n_rows is not None and t.shape[0] != n_rows):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({n_rows if n_rows is not None else 'rows'}, {n_heads}, {self.head_dim})")
-        if t.numel() and (t.stride(2) != 1 or (n_heads > 1 and t.stride(1) != self.head_dim)):
-            raise ValueError(f"the rows of {name} are not contiguous")
-        return t.stride(0) if t.shape[0] > 1 else n_heads * self.head_dim
+    def _row_stride(self, t, n_heads, n_rows, name):
+        """[n_rows, n_heads, head_dim] with rows that may lie apart -> elements from one row to the next."""
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 3 or shape[0] != n_rows or shape[1] != n_heads or shape[2] != self.head_dim:
+            raise ValueError(f"{name} has shape {tuple(shape)}, expected {(n_rows, n_heads, self.head_dim)}")
+        if stride[2] != 1 or (n_heads > 1 and stride[1] != self.head_dim):
+            if t.numel():
+                raise ValueError(f"the rows of {name} are not contiguous")
+        return stride[0] if n_rows > 1 else n_heads * self.head_dim
 
-    def _per_sequence(self, t, B, name):
-        if t.dtype != self.torch.int32 or t.dim() != 1 or t.shape[0] != B:
-            raise ValueError(f"{name} must be an int32 tensor of {B} entries")
+    def _counts(self, t, B, name):
+        if t.dtype is not self.torch.int32 or t.shape != (B,) or (B > 1 and t.stride(0) != 1):
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {B} entries")
+        return t.data_ptr()
 
     def append(self, k, v, cu_seqlens, start_rows, slots=None):
         """Rows [cu_seqlens[b], cu_seqlens[b + 1]) of k and v ([total, n_kv_heads, head_dim], bf16 or fp32) become rows
         start_rows[b].. (int32 tensor) of slot slots[b] (default b)."""
-        if not self._here(k, v, start_rows):
+        if self._elsewhere(k, v, start_rows):
             with self.torch.cuda.device(self.dev):
                 return self.append(k, v, cu_seqlens, start_rows, slots)
         B, total = len(cu_seqlens) - 1, int(cu_seqlens[-1])
-        self._per_sequence(start_rows, B, "start_rows")
-        ld = self._rows(k, self.n_kv_heads, "k", total)
-        if self._rows(v, self.n_kv_heads, "v", total) != ld or v.dtype != k.dtype:
+        ld = self._row_stride(k, self.n_kv_heads, total, "k")
+        if self._row_stride(v, self.n_kv_heads, total, "v") != ld or v.dtype is not k.dtype:
             raise ValueError("k and v must have the same type and row stride")
-        hivis_kv4_append(self.c, B, slots, cu_seqlens, start_rows, k.data_ptr(), v.data_ptr(), _dtype(k), ld)
+        _check(lib.hivis_kv4_append(self._ref, B, _slots(slots, B), _ints(cu_seqlens), self._counts(start_rows, B, "start_rows"), k.data_ptr(),
+                                    v.data_ptr(), _dtype(k), ld, _raw_stream(self.dev.index)))
 
     def read(self, cu_seqlens, start_rows, slots=None):
         """-> (k, v) fp32 [total, n_kv_heads, head_dim]: what rows start_rows[b].. of the slots stand for."""
-        if not self._here(start_rows):
+        if self._elsewhere(start_rows):
             with self.torch.cuda.device(self.dev):
                 return self.read(cu_seqlens, start_rows, slots)
         t, B = self.torch, len(cu_seqlens) - 1
-        self._per_sequence(start_rows, B, "start_rows")
         shape = (int(cu_seqlens[-1]), self.n_kv_heads, self.head_dim)
         k = t.empty(shape, dtype=t.float32, device=self.dev)
         v = t.empty(shape, dtype=t.float32, device=self.dev)
-        hivis_kv4_read(self.c, B, slots, cu_seqlens, start_rows, k, v)
+        _check(lib.hivis_kv4_read(self._ref, B, _slots(slots, B), _ints(cu_seqlens), self._counts(start_rows, B, "start_rows"), k.data_ptr(),
+                                  v.data_ptr(), _raw_stream(self.dev.index)))
         return k, v
 
     def attention(self, q, rows, n_q=1, scale=None, mask=None, mask_rows=0, slots=None, out=None):
         """q [B * n_q, n_q_heads, head_dim] (bf16 or fp32) over the slots' first rows[b] rows (int32 tensor) -> the same shape
         and type.  Causal over the last n_q rows, or by `mask` (int32 [B, n_q, ceil(mask_rows / 32)]) over the last mask_rows."""
-        if not self._here(q, rows, mask, out):
+        if self._elsewhere(q, rows, mask, out):
             with self.torch.cuda.device(self.dev):
                 return self.attention(q, rows, n_q, scale, mask, mask_rows, slots, out)
         t, B = self.torch, rows.shape[0]
-        self._per_sequence(rows, B, "rows")
         heads = q.shape[1] if q.dim() == 3 else 0
-        q_ld = self._rows(q, heads, "q", B * int(n_q))
+        q_ld = self._row_stride(q, heads, B * n_q, "q")
+        mask_ptr = None
+        if mask is not None:
+            if mask.dtype is not t.int32 or tuple(mask.shape) != (B, n_q, (mask_rows + 31) // 32) or not mask.is_contiguous():
+                raise ValueError("mask must be a contiguous int32 tensor [B, n_q, ceil(mask_rows / 32)]")
+            mask_ptr = mask.data_ptr()
         if out is None:
             out = t.empty(q.shape, dtype=q.dtype, device=self.dev)
-        elif out.dtype != q.dtype:
-            raise ValueError("out must have the type of q")
-        out_ld = self._rows(out, heads, "out", B * int(n_q))
-        if mask is not None and (mask.dtype != t.int32 or tuple(mask.shape) != (B, int(n_q), (int(mask_rows) + 31) // 32) or not mask.is_contiguous()):
-            raise ValueError("mask must be a contiguous int32 tensor [B, n_q, ceil(mask_rows / 32)]")
-        hivis_kv4_attention(self.c, B, slots, rows, n_q, heads, q.data_ptr(), _dtype(q), q_ld,
-                            self.head_dim ** -0.5 if scale is None else scale, mask, mask_rows, out.data_ptr(), out_ld)
+            out_ld = heads * self.head_dim
+        else:
+            if out.dtype is not q.dtype:
+                raise ValueError("out must have the type of q")
+            out_ld = self._row_stride(out, heads, B * n_q, "out")
+        _check(lib.hivis_kv4_attention(self._ref, B, _slots(slots, B), self._counts(rows, B, "rows"), n_q, heads, q.data_ptr(), _dtype(q), q_ld,
+                                       self._scale if scale is None else scale, mask_ptr, mask_rows, out.data_ptr(), out_ld,
+                                       _raw_stream(self.dev.index)))
         return out
 
 
@@ -570,23 +597,33 @@ def logprobs(logits, ids=None, temperature: float = 1.0, top_n: int = 0, entropy
     """Log-probabilities of `ids` (int32 [n_rows, n_ids]) under softmax(logits / temperature), the rows' entropy and their
     `top_n` most probable tokens; logits [n_rows, vocab], bf16 or fp32, rows may lie apart.  include/hivis.h: hivis_logprobs."""
     import torch
-    if logits.dim() != 2 or logits.stride(1) != 1 and logits.shape[1] > 1:
-        raise ValueError(f"logits must be [n_rows, vocab] with contiguous rows, not {tuple(logits.shape)}")
-    if not logits.is_cuda:
+    shape, stride, index = logits.shape, logits.stride(), logits.get_device()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"logits must be [n_rows, vocab] with contiguous rows, not {tuple(shape)}")
+    if index < 0:
         raise ValueError("logits must be a CUDA tensor")
-    n, dev = logits.shape[0], logits.device
-    if torch.cuda.current_device() != dev.index:
-        with torch.cuda.device(dev):
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
             return logprobs(logits, ids, temperature, top_n, entropy)
+    n, vocab = shape
     n_ids = 0
     if ids is not None:
-        if ids.dtype != torch.int32 or ids.dim() != 2 or ids.shape[0] != n or ids.device != dev or not ids.is_contiguous():
+        if ids.dtype is not torch.int32 or ids.dim() != 2 or ids.shape[0] != n or ids.get_device() != index or not ids.is_contiguous():
             raise ValueError("ids must be a contiguous int32 tensor [n_rows, n_ids] beside the logits")
         n_ids = ids.shape[1]
-    lp = torch.empty((n, n_ids), dtype=torch.float32, device=dev) if n_ids else None
-    h = torch.empty((n,), dtype=torch.float32, device=dev) if entropy else None
-    top = torch.empty((n, top_n), dtype=torch.int32, device=dev) if top_n > 0 else None
-    top_lp = torch.empty((n, top_n), dtype=torch.float32, device=dev) if top_n > 0 else None
-    hivis_logprobs(n, logits.shape[1], logits.data_ptr(), _dtype(logits), logits.stride(0) if n > 1 else logits.shape[1], temperature,
-                   ids if n_ids else None, n_ids, top_n, lp, h, top, top_lp)
+    lp = h = top = top_lp = None
+    p_lp = p_h = p_top = p_top_lp = None
+    dev = logits.device
+    if n_ids:
+        lp = torch.empty((n, n_ids), dtype=torch.float32, device=dev)
+        p_lp = lp.data_ptr()
+    if entropy:
+        h = torch.empty((n,), dtype=torch.float32, device=dev)
+        p_h = h.data_ptr()
+    if top_n > 0:
+        top = torch.empty((n, top_n), dtype=torch.int32, device=dev)
+        top_lp = torch.empty((n, top_n), dtype=torch.float32, device=dev)
+        p_top, p_top_lp = top.data_ptr(), top_lp.data_ptr()
+    _check(lib.hivis_logprobs(n, vocab, logits.data_ptr(), _dtype(logits), stride[0] if n > 1 else vocab, temperature,
+                              ids.data_ptr() if n_ids else None, n_ids, top_n, p_lp, p_h, p_top, p_top_lp, _raw_stream(index)))
     return Logprobs(lp, h, top, top_lp)
