@@ -14,46 +14,50 @@ struct Kv4RowsArgs {
     Kv4View c;
     SlotList sl;
     CuSeqlens cu;              // packed rows: sequence b owns [cu.v[b], cu.v[b + 1])
-    CuSeqlens pairs;           // first pair of rows of each sequence: half its rows and one, whichever way its start is aligned
+    CuSeqlens pairs;           // append: first pair of rows of each sequence: half its rows and one, whichever way its start is aligned
     const int* start;          // [B] cache row of each sequence's first packed row
     const void *k, *v;         // packed rows [.][ld]
     long long ld;
     float *out_k, *out_v;      // read: [.][Hkv * dh]
+    int heads_log2;            // heads side by side in a CTA
 };
 
-// DH / 8 lanes a row: a lane has 8 neighbouring channels, four lanes a group.  Two halves of 2 * DH / 8 lanes take the two rows
-// of a pair, which share the words of their V codes.
+// the entry of a rising list (at most HIVIS_MAX_BATCH of them) that i lies in
+__device__ __forceinline__ int kv4_owner(const CuSeqlens& first, int n, int i) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first.v[mid] <= i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Append: DH / 8 lanes a row, a lane has 8 neighbouring channels, four lanes a group.  Two halves of 2 * DH / 8 lanes take the two
+// rows of a pair, which share the words of their V codes.
 struct Kv4Place {
-    int b, h, slot, w, c;      // sequence, KV head, slot, group, lane of the group
+    int h, slot, w, c;         // KV head, slot, group, lane of the group
     int row, packed;           // cache row; row of the packed input, -1: none
 };
 template <int DH>
 __device__ __forceinline__ Kv4Place kv4_place(const Kv4RowsArgs& a) {
-    constexpr int LR = DH / 8;
+    constexpr int LR = DH / 8, UNITS = 256 / (2 * LR);
     Kv4Place p;
-    const long long t = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    const long long unit = t / (2 * LR);
-    const int l = (int)(t % LR), odd = (int)(t / LR) & 1;
-    const int pair = (int)(unit / a.c.Hkv);
-    p.h = (int)(unit % a.c.Hkv);
+    const int l = threadIdx.x % LR, odd = (threadIdx.x / LR) & 1, unit = threadIdx.x / (2 * LR);
+    p.h = (blockIdx.y << a.heads_log2) + (unit & ((1 << a.heads_log2) - 1));
+    const int pair = blockIdx.x * (UNITS >> a.heads_log2) + (unit >> a.heads_log2);
     p.w = l >> 2;
     p.c = l & 3;
     p.packed = -1;
     p.row = 0;
-    int lo = 0, hi = a.sl.n;                              // the sequence that owns the pair
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.pairs.v[mid] <= pair) lo = mid;
-        else hi = mid;
-    }
-    p.b = lo;
-    p.slot = a.sl.slot[lo];
-    if (pair >= a.pairs.v[a.sl.n]) return p;
-    const int start = a.start[lo], n = a.cu.v[lo + 1] - a.cu.v[lo];
+    const int b = kv4_owner(a.pairs, a.sl.n, pair);
+    p.slot = a.sl.slot[b];
+    if (pair >= a.pairs.v[a.sl.n] || p.h >= a.c.Hkv) return p;
+    const int start = a.start[b], n = a.cu.v[b + 1] - a.cu.v[b];
     if (start < 0 || start >= a.c.max_len) return p;
-    p.row = ((start >> 1) + (pair - a.pairs.v[lo])) * 2 + odd;
+    p.row = ((start >> 1) + (pair - a.pairs.v[b])) * 2 + odd;
     const int i = p.row - start;
-    if (i >= 0 && i < n && p.row < a.c.max_len) p.packed = a.cu.v[lo] + i;
+    if (i >= 0 && i < n && p.row < a.c.max_len) p.packed = a.cu.v[b] + i;
     return p;
 }
 
@@ -71,20 +75,19 @@ __device__ __forceinline__ void kv4_load8(const void* p, long long i, float (&x)
 
 // parameters of the group whose 32 values the four lanes of a quad hold (every lane of the warp takes part)
 __device__ __forceinline__ uint32_t kv4_group_params(const float (&x)[8]) {
-    float lo = x[0], hi = x[0];
-    bool finite = true;
+    float lo = x[0], hi = x[0], zero = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         lo = fminf(lo, x[i]);
         hi = fmaxf(hi, x[i]);
-        finite &= fabsf(x[i]) < INFINITY;
+        zero = fmaf(x[i], 0.f, zero);                       // NaN once a value is not finite
     }
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
         lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
-    const unsigned bad = __ballot_sync(0xffffffffu, !finite);
+    const unsigned bad = __ballot_sync(0xffffffffu, zero != 0.f);
     return kv4_params(lo, hi, ((bad >> (threadIdx.x & 28)) & 15u) == 0u);
 }
 
@@ -131,32 +134,28 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const __grid_constant__
     kv4_store_row<DH>(a.c, p, p.packed >= 0, k, v);
 }
 
+// Read: a lane has four neighbouring channels of a row, so that a warp writes whole lines.
 template <int DH>
 __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ Kv4RowsArgs a) {
+    constexpr int LR = DH / 4, UNITS = 256 / LR;
     pdl_wait();
     pdl_trigger();
-    const Kv4Place p = kv4_place<DH>(a);
-    if (p.packed < 0) return;
-    const unsigned char* tile = kv4_tile(a.c, p.slot, p.h, p.row);
-    const int r = p.row % KV4_TILE;
+    const int l = threadIdx.x % LR, unit = threadIdx.x / LR;
+    const int h = (blockIdx.y << a.heads_log2) + (unit & ((1 << a.heads_log2) - 1));
+    const int j = blockIdx.x * (UNITS >> a.heads_log2) + (unit >> a.heads_log2);
+    if (h >= a.c.Hkv || j >= a.cu.v[a.sl.n]) return;
+    const int b = kv4_owner(a.cu, a.sl.n, j), start = a.start[b];
+    if (start < 0 || start >= a.c.max_len || j - a.cu.v[b] >= a.c.max_len - start) return;
+    const int row = start + (j - a.cu.v[b]), r = row % KV4_TILE, w = l >> 3, c = (l >> 1) & 3, g = l & 7;
+    const unsigned char* tile = kv4_tile(a.c, a.sl.slot[b], h, row);
     auto half = [&](int at) { return (uint32_t)*(const uint16_t*)(tile + at); };
-    const uint32_t kp = (half(kv4_s_at(DH, 0, r, p.w)) << 16) | half(kv4_m_at(DH, 0, r, p.w));
-    const uint32_t vp = (half(kv4_s_at(DH, 1, r, p.w)) << 16) | half(kv4_m_at(DH, 1, r, p.w));
-    const uint32_t kw = *(const uint32_t*)(tile + kv4_k_at(DH, r, p.w, p.c));
-    const uint32_t v0 = half(kv4_v_at(DH, r, p.w, 2 * p.c)), v1 = half(kv4_v_at(DH, r, p.w, 2 * p.c + 1));
-    const uint32_t vw = v0 | (v1 << 16);
-    float k[8], v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        k[i] = fmaf((float)((kw >> (4 * i)) & 15u), kv4_scale(kp), kv4_min(kp));
-        v[i] = fmaf((float)((vw >> (4 * i)) & 15u), kv4_scale(vp), kv4_min(vp));
-    }
-    const long long o = ((long long)p.packed * a.c.Hkv + p.h) * DH + 32 * p.w + 8 * p.c;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        *(float4*)(a.out_k + o + 4 * q) = make_float4(k[4 * q], k[4 * q + 1], k[4 * q + 2], k[4 * q + 3]);
-        *(float4*)(a.out_v + o + 4 * q) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-    }
+    const uint32_t kw = half(kv4_k_at(DH, r, w, c) + 2 * (l & 1)), vw = half(kv4_v_at(DH, r, w, g));
+    const float ks = bf16_lo(half(kv4_s_at(DH, 0, r, w))), km = bf16_lo(half(kv4_m_at(DH, 0, r, w)));
+    const float vs = bf16_lo(half(kv4_s_at(DH, 1, r, w))), vm = bf16_lo(half(kv4_m_at(DH, 1, r, w)));
+    auto value = [](uint32_t codes, int i, float s, float m) { return fmaf((float)((codes >> (4 * i)) & 15u), s, m); };
+    const long long o = ((long long)j * a.c.Hkv + h) * DH + 4 * l;
+    *(float4*)(a.out_k + o) = make_float4(value(kw, 0, ks, km), value(kw, 1, ks, km), value(kw, 2, ks, km), value(kw, 3, ks, km));
+    *(float4*)(a.out_v + o) = make_float4(value(vw, 0, vs, vm), value(vw, 1, vs, vm), value(vw, 2, vs, vm), value(vw, 3, vs, vm));
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -860,12 +859,14 @@ static int kv4_check_rows(const char* who, const hivis_kv4_cache* cache, int B, 
     return HIVIS_OK;
 }
 
-static dim3 kv4_rows_grid(const Kv4RowsArgs& a) {
-    const long long threads = (long long)a.pairs.v[a.sl.n] * a.c.Hkv * (a.c.dh / 4);
-    return dim3((unsigned)((threads + 255) / 256));
-}
-static bool kv4_rows_too_many(const Kv4RowsArgs& a) {
-    return ((long long)a.pairs.v[a.sl.n] * a.c.Hkv * (a.c.dh / 4) + 255) / 256 > 0x7FFFFFFFll;
+// A CTA's `units` places are heads side by side (as many as there are, to a power of two) of neighbouring rows or pairs.
+static bool kv4_rows_grid(Kv4RowsArgs* a, int units, int items, dim3* grid) {
+    a->heads_log2 = 0;
+    while ((1 << a->heads_log2) < units && (1 << a->heads_log2) < a->c.Hkv) a->heads_log2 += 1;
+    const int per = units >> a->heads_log2;
+    const long long y = (a->c.Hkv + (1 << a->heads_log2) - 1) >> a->heads_log2;
+    *grid = dim3((unsigned)(((long long)items + per - 1) / per), (unsigned)y);
+    return y <= 65535;
 }
 
 static int kv4_cuda(const char* who, cudaError_t e) {
@@ -885,9 +886,10 @@ extern "C" int hivis_kv4_append(const hivis_kv4_cache* cache, int B, const int* 
     if (!k || !v) KV4_FAIL(HIVIS_ERR_ARG, "%s: null argument", who);
     if (kv4_misaligned(k) || kv4_misaligned(v)) KV4_FAIL(HIVIS_ERR_ARG, "%s: device pointer not 16-byte aligned", who);
     if (ld % 8 || ld < (int64_t)a.c.Hkv * a.c.dh) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: ld must be a multiple of 8 of at least n_kv_heads * head_dim", who);
-    if (kv4_rows_too_many(a)) KV4_FAIL(HIVIS_ERR_CAPACITY, "%s: too many rows for one call", who);
     a.k = k; a.v = v; a.ld = ld;
-    const dim3 grid = kv4_rows_grid(a), block(256);
+    dim3 grid;
+    const dim3 block(256);
+    if (!kv4_rows_grid(&a, 256 / (a.c.dh / 4), a.pairs.v[B], &grid)) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads", who);
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
     if (dtype == HIVIS_BF16) e = a.c.dh == 128 ? launch_pdl(kv4_append_kernel<128, bf16>, grid, block, 0, st, a) : launch_pdl(kv4_append_kernel<64, bf16>, grid, block, 0, st, a);
@@ -904,9 +906,10 @@ extern "C" int hivis_kv4_read(const hivis_kv4_cache* cache, int B, const int* se
     if (a.cu.v[B] == 0) return HIVIS_OK;
     if (!out_k || !out_v) KV4_FAIL(HIVIS_ERR_ARG, "%s: null argument", who);
     if (kv4_misaligned(out_k) || kv4_misaligned(out_v)) KV4_FAIL(HIVIS_ERR_ARG, "%s: device pointer not 16-byte aligned", who);
-    if (kv4_rows_too_many(a)) KV4_FAIL(HIVIS_ERR_CAPACITY, "%s: too many rows for one call", who);
     a.out_k = out_k; a.out_v = out_v;
-    const dim3 grid = kv4_rows_grid(a), block(256);
+    dim3 grid;
+    const dim3 block(256);
+    if (!kv4_rows_grid(&a, 256 / (a.c.dh / 4), a.cu.v[B], &grid)) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads", who);
     cudaStream_t st = (cudaStream_t)stream;
     return kv4_cuda(who, a.c.dh == 128 ? launch_pdl(kv4_read_kernel<128>, grid, block, 0, st, a) : launch_pdl(kv4_read_kernel<64>, grid, block, 0, st, a));
 }

@@ -1,14 +1,17 @@
 // Log-probabilities of given tokens, entropy and the most probable alternatives of rows of logits, in one pass over them.
 //
-// In powers of two, with y_i = log2(e) / T (x_i - m), m the largest logit so far: log2 p_i = y_i - log2 Z, Z = sum 2^y, and
-// H = log2 Z - W / Z, W = sum 2^y y; raising m by d / (log2(e) / T) turns (Z, W) into (Z f, (W - d Z) f), f = 2^-d.  (The difference
-// comes before the product: logits may be of any size, the type's lowest number as a mask among them.)  A thread keeps
-// (m, Z, W) of its part of a row.  Threads are joined in a CTA and CTAs, up to 16 to a row, in a cluster, always in the same
-// order, in fp32; the row's results are made of the joined sums in fp64.
+// In powers of two, with y_i = log2(e) / T x_i - c: log2 p_i = y_i - log2 Z, Z = sum 2^y, and H = log2 Z - W / Z, W = sum 2^y y, for any
+// c near the largest logit's.  A thread takes c from its first 32 (bf16) or 16 logits and raises it only when later ones are above
+// it by 2^60 - raising by d turns (Z, W) into (Z f, (W - d Z) f), f = 2^-d - so that a logit costs one multiply-add for y, the
+// exponential, and one operation for each sum.  Threads are joined in a CTA and CTAs, up to 16 to a row, in a cluster, always in
+// the same order, in fp32; the row's results are made of the joined sums in fp64.
+// A CTA whose largest logit is so far from zero that y would lose it (|log2(e) / T x| > 2^28: a row of the type's lowest number, say)
+// goes over its part again with y = log2(e) / T (x - max).
 //
-// Alternatives: the n-th largest of the threads' maxima is no larger than the row's n-th largest logit, so only threads whose
-// maximum reaches it look through their part again, and what they find (a few more than n) is sorted as (value, lowest token)
-// keys by one warp.  Where far more logits pass (many equal ones), the n largest are found one after the other instead.
+// Alternatives: a thread remembers its largest logit.  The n-th largest of the threads' maxima is no larger than the n-th largest
+// logit, so only parts of threads whose maximum reaches it are looked through again, a warp to a part, and what they hold (a
+// few more than n) is sorted as (value, lowest token) keys by one warp.  Where far more logits pass (many equal ones), the n
+// largest are found one after the other instead.
 #include <cstdio>
 #include <cstring>
 
@@ -36,57 +39,97 @@ struct LogprobArgs {
     int slice;                    // logits per CTA, a multiple of 8
 };
 
+#define LP_FAR 0x1p28f            // |c| is at most this
+#define LP_RISE 60.f              // y beyond which c is raised
+
 struct LpSum {
-    float m, z, w;                // z = 0: nothing yet, m means nothing
+    float c, z, w;
 };
 __device__ __forceinline__ float lp_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// the sums of a set with another, at least as high, m
-__device__ __forceinline__ LpSum lp_raise(const LpSum& s, float m, float scale) {
-    if (s.z == 0.f) return LpSum{m, 0.f, 0.f};
-    const float d = m == s.m ? 0.f : scale * (m - s.m), f = lp_exp2(-d);
-    return LpSum{m, s.z * f, f > 0.f ? fmaf(-d, s.z, s.w) * f : 0.f};
+// (Z, W) for a reference higher by d
+__device__ __forceinline__ void lp_lower(float& z, float& w, float d) {
+    const float f = lp_exp2(-d);
+    w = f > 0.f ? fmaf(-d, z, w) * f : 0.f;
+    z = z == 0.f ? 0.f : z * f;
 }
-__device__ __forceinline__ float lp_m(const LpSum& s) { return s.z == 0.f ? -INFINITY : s.m; }
 
-// 16 bytes of logits at a time; a vector that is not wholly inside the row is read one by one
+// 16 bytes of logits; a vector that is not wholly inside [lo, hi) is read one by one, with -infinity for what is outside
 template <typename T>
 struct LpVec {
     static constexpr int N = 16 / (int)sizeof(T);
 };
 template <typename T>
-__device__ __forceinline__ void lp_load(const T* row, int i, int lo, int hi, bool vec, float (&x)[LpVec<T>::N]) {
+__device__ __forceinline__ uint4 lp_load(const T* row, int i, int lo, int hi) {
     constexpr int N = LpVec<T>::N;
-    if (vec && i >= lo && i + N <= hi) {
-        const uint4 v = ld_stream((const uint4*)(row + i));
-        if constexpr (N == 8) {
-            x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
-            x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
-        } else {
-            x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
-        }
-    } else {
+    if (i >= lo && i + N <= hi) return ld_stream((const uint4*)(row + i));
+    uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = i + e >= lo && i + e < hi ? load_as_float<T>(row, i + e) : -INFINITY;
+    for (int k = 0; k < 4; ++k) w[k] = N == 8 ? 0xFF80FF80u : 0xFF800000u;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (i + e >= lo && i + e < hi) {
+            if constexpr (N == 8) {
+                const uint32_t x = ((const unsigned short*)row)[i + e];
+                w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | (x << 16) : (w[e / 2] & 0xFFFF0000u) | x;
+            } else {
+                w[e] = ((const uint32_t*)row)[i + e];
+            }
+        }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ void lp_values(const uint4& v, float (&x)[LpVec<T>::N]) {
+    if constexpr (sizeof(T) == 2) {
+        x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
+        x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
+    } else {
+        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
     }
 }
-template <int N>
-__device__ __forceinline__ void lp_add(LpSum& s, float& most, const float (&x)[N], float scale) {
-    float m = x[0];
+
+__device__ __forceinline__ __nv_bfloat162 lp_bf2(uint32_t w) { return *(const __nv_bfloat162*)&w; }
+__device__ __forceinline__ uint32_t lp_w(const __nv_bfloat162& h) { return *(const uint32_t*)&h; }
+// the largest of the numbers of some vectors (NaNs left out)
+template <typename T, int U>
+__device__ __forceinline__ float lp_most(const uint4 (&v)[U]) {
+    if constexpr (sizeof(T) == 2) {
+        __nv_bfloat162 m = __hmax2(__hmax2(lp_bf2(v[0].x), lp_bf2(v[0].y)), __hmax2(lp_bf2(v[0].z), lp_bf2(v[0].w)));
 #pragma unroll
-    for (int e = 1; e < N; ++e) m = fmaxf(m, x[e]);
-    if (m > most) {
-        most = m;
-        s = lp_raise(s, m, scale);
+        for (int u = 1; u < U; ++u) m = __hmax2(m, __hmax2(__hmax2(lp_bf2(v[u].x), lp_bf2(v[u].y)), __hmax2(lp_bf2(v[u].z), lp_bf2(v[u].w))));
+        return fmaxf(bf16_lo(lp_w(m)), bf16_hi(lp_w(m)));
+    } else {
+        float m = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(v[u].x), __uint_as_float(v[u].y))), fmaxf(__uint_as_float(v[u].z), __uint_as_float(v[u].w)));
+        return m;
     }
+}
+// The sums of some vectors' logits.  A logit of -infinity counts as one of -1e30, so that 2^y y is 0 and no NaN.
+template <typename T, int U>
+__device__ __forceinline__ void lp_add(LpSum& s, const uint4 (&v)[U], float scale) {
+    constexpr int N = LpVec<T>::N;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const float y = scale * (x[e] - s.m), p = lp_exp2(y);
-        s.z += p;
-        s.w = fmaf(p, fmaxf(y, -1e30f), s.w);            // (a logit of -infinity adds nothing)
+    for (int u = 0; u < U; ++u) {
+        float x[N];
+        if constexpr (sizeof(T) == 2) {
+            const __nv_bfloat162 low = __float2bfloat162_rn(-1e30f);
+            const uint4 t = make_uint4(lp_w(__hmax2_nan(lp_bf2(v[u].x), low)), lp_w(__hmax2_nan(lp_bf2(v[u].y), low)),
+                                       lp_w(__hmax2_nan(lp_bf2(v[u].z), low)), lp_w(__hmax2_nan(lp_bf2(v[u].w), low)));
+            lp_values<T>(t, x);
+        } else {
+            lp_values<T>(v[u], x);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float y = fmaf(scale, x[e], -s.c), p = lp_exp2(y);
+            s.z += p;
+            s.w = fmaf(p, sizeof(T) == 2 ? y : fmaxf(y, -1e38f), s.w);
+        }
     }
 }
 
@@ -143,13 +186,20 @@ __device__ __forceinline__ u64 lp_select(const u64* cand, int count, int lane) {
     return best;
 }
 
+// What a CTA found out about its part of a row: sums relative to c, and whether some logit is not -infinity.
+struct LpPart {
+    double c;
+    float z, w;
+};
+
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS) logprob_kernel(const __grid_constant__ LogprobArgs a) {
-    constexpr int N = LpVec<T>::N;
-    __shared__ LpSum s_sum[LP_WARPS], s_cta;
-    __shared__ float s_max[LP_WARPS][32];
+__global__ void __launch_bounds__(LP_THREADS, 5) logprob_kernel(const __grid_constant__ LogprobArgs a) {
+    constexpr int N = LpVec<T>::N, U = 4, STRIDE = LP_THREADS * N;
+    __shared__ LpSum s_sum[LP_WARPS];
+    __shared__ float s_most[LP_WARPS], s_max[LP_WARPS][32], s_bar;
+    __shared__ LpPart s_part;
     __shared__ u64 s_cand[LP_CAND], s_top[32], s_red[LP_WARPS];
-    __shared__ int s_count;
+    __shared__ int s_list[LP_THREADS], s_listed, s_count;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int S = gridDim.x, rank = blockIdx.x, r = blockIdx.y + gridDim.y * blockIdx.z;
     pdl_wait();
@@ -159,61 +209,111 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(const __grid_consta
     // vectors start on 16-byte boundaries: `skew` logits before the row's first one belong to the first of them
     const int skew = (int)(((uintptr_t)row & 15u) / sizeof(T));
     const int lo = min(a.V, max(0, rank * a.slice - skew)), hi = rank == S - 1 ? a.V : min(a.V, (rank + 1) * a.slice - skew);
-    const int first = rank * a.slice - skew + tid * N;
+    const int begin = rank * a.slice - skew, first = begin + tid * N;
     // the tokens asked for: their logits are on their way meanwhile
     float asked = -INFINITY;
     if (rank == 0 && warp == 0 && lane < a.n_ids) {
         const int id = a.ids[(long long)r * a.n_ids + lane];
         if (id >= 0 && id < a.V) asked = load_as_float<T>(row, id);
     }
-    LpSum s = {0.f, 0.f, 0.f};
+    LpSum s = {-LP_FAR, 0.f, 0.f};
     float most = -INFINITY;
-    for (int i = first; i < hi; i += 4 * LP_THREADS * N) {
-        float x[4][N];
+    for (int i = first; i < hi; i += U * STRIDE) {
+        uint4 v[U];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) lp_load<T>(row, i + u * LP_THREADS * N, lo, hi, true, x[u]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) lp_add<N>(s, most, x[u], a.scale);
+        for (int u = 0; u < U; ++u) v[u] = lp_load<T>(row, i + u * STRIDE, lo, hi);
+        const float m = lp_most<T>(v);
+        most = fmaxf(most, m);
+        const float c = fminf(fmaxf(a.scale * m, -LP_FAR), LP_FAR);
+        if (c > s.c + (s.z == 0.f ? 0.f : LP_RISE)) {
+            lp_lower(s.z, s.w, c - s.c);
+            s.c = c;
+        }
+        lp_add<T>(s, v, a.scale);
     }
     // ---- the CTA's sums
     {
-        float m = lp_m(s);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        LpSum d = lp_raise(s, m, a.scale);
+        float c = s.z == 0.f ? -INFINITY : s.c, m = most;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            d.z += __shfl_xor_sync(0xffffffffu, d.z, o);
-            d.w += __shfl_xor_sync(0xffffffffu, d.w, o);
+            c = fmaxf(c, __shfl_xor_sync(0xffffffffu, c, o));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         }
-        if (lane == 0) s_sum[warp] = d;
+        if (s.z == 0.f) s.w = 0.f;
+        else lp_lower(s.z, s.w, c - s.c);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
+            s.w += __shfl_xor_sync(0xffffffffu, s.w, o);
+        }
+        if (lane == 0) {
+            s_sum[warp] = LpSum{c, s.z, s.w};
+            s_most[warp] = m;
+        }
     }
     if (TOP) {
         s_max[warp][lane] = lp_sort(most, lane);
-        if (tid == 0) s_count = 0;
+        if (tid == 0) s_count = s_listed = 0;
     }
     __syncthreads();
-    if (tid == 0) {
-        float m = -INFINITY;
-        for (int w = 0; w < LP_WARPS; ++w) m = fmaxf(m, lp_m(s_sum[w]));
-        LpSum d = {m, 0.f, 0.f};
-        for (int w = 0; w < LP_WARPS; ++w) {
-            const LpSum e = lp_raise(s_sum[w], m, a.scale);
-            d.z += e.z;
-            d.w += e.w;
+    float cta_most = s_most[0];
+#pragma unroll
+    for (int w = 1; w < LP_WARPS; ++w) cta_most = fmaxf(cta_most, s_most[w]);
+    const bool far = cta_most > -INFINITY && !(fabsf(a.scale * cta_most) < 0.5f * LP_FAR);
+    if (far) {
+        // relative to the largest logit itself
+        float z = 0.f, w = 0.f;
+        for (int i = first; i < hi; i += STRIDE) {
+            float x[N];
+            lp_values<T>(lp_load<T>(row, i, lo, hi), x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float y = a.scale * (x[e] - cta_most), p = x[e] == cta_most && fabsf(cta_most) < INFINITY ? 1.f : lp_exp2(y);
+                z += p;
+                if (p > 0.f && p < 1.f) w = fmaf(p, y, w);
+            }
         }
-        s_cta = d;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            z += __shfl_xor_sync(0xffffffffu, z, o);
+            w += __shfl_xor_sync(0xffffffffu, w, o);
+        }
+        __syncthreads();                                     // (s_most has been read)
+        if (lane == 0) s_sum[warp] = LpSum{0.f, z, w};
+        __syncthreads();
+    }
+    if (tid == 0) {
+        float c = -INFINITY, z = 0.f, w = 0.f;
+#pragma unroll
+        for (int k = 0; k < LP_WARPS; ++k) c = fmaxf(c, s_sum[k].c);
+#pragma unroll
+        for (int k = 0; k < LP_WARPS; ++k) {
+            LpSum e = s_sum[k];
+            if (e.z == 0.f) continue;
+            lp_lower(e.z, e.w, c - e.c);
+            z += e.z;
+            w += e.w;
+        }
+        s_part = LpPart{far ? (double)a.scale * (double)cta_most : z == 0.f ? -INFINITY : (double)c, z, w};
     }
     if (TOP) {
         // the n-th largest of the threads' maxima
-        float v = s_max[0][lane];
+        if (warp == 1) {
+            float v = s_max[0][lane];
 #pragma unroll
-        for (int w = 1; w < LP_WARPS; ++w) v = lp_merge(v, s_max[w][lane], lane);
-        const float bar = __shfl_sync(0xffffffffu, v, a.top_n - 1);
-        if (most > -INFINITY && most >= bar) {
-            for (int i = first; i < hi; i += LP_THREADS * N) {
+            for (int w = 1; w < LP_WARPS; ++w) v = lp_merge(v, s_max[w][lane], lane);
+            if (lane == a.top_n - 1) s_bar = v;
+        }
+        __syncthreads();
+        const float bar = s_bar;
+        if (most > -INFINITY && most >= bar) s_list[atomicAdd(&s_listed, 1)] = tid;
+        __syncthreads();
+        const int listed = s_listed;
+        for (int k = warp; k < listed; k += LP_WARPS) {
+            const int from = begin + s_list[k] * N;
+            for (int i = from + lane * STRIDE; i < hi; i += 32 * STRIDE) {
                 float x[N];
-                lp_load<T>(row, i, lo, hi, true, x);
+                lp_values<T>(lp_load<T>(row, i, lo, hi), x);
 #pragma unroll
                 for (int e = 0; e < N; ++e)
                     if (x[e] >= bar && x[e] > -INFINITY) {
@@ -234,9 +334,9 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(const __grid_consta
             u64 below = ~0ull;
             for (int k = 0; k < a.top_n; ++k) {
                 u64 best = 0ull;
-                for (int i = first; i < hi; i += LP_THREADS * N) {
+                for (int i = first; i < hi; i += STRIDE) {
                     float x[N];
-                    lp_load<T>(row, i, lo, hi, true, x);
+                    lp_values<T>(lp_load<T>(row, i, lo, hi), x);
 #pragma unroll
                     for (int e = 0; e < N; ++e)
                         if (x[e] >= bar && x[e] > -INFINITY) {
@@ -264,25 +364,29 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(const __grid_consta
     else __syncthreads();
     // ---- the row, by the first warp of the first CTA
     if (rank == 0 && warp == 0) {
-        LpSum d = {0.f, 0.f, 0.f};
-        if (lane < S) d = *(S > 1 ? cluster.map_shared_rank(&s_cta, lane) : &s_cta);
-        float m = lp_m(d);
+        LpPart d = {-INFINITY, 0.f, 0.f};
+        if (lane < S) d = *(S > 1 ? cluster.map_shared_rank(&s_part, lane) : &s_part);
+        double c = d.c;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        d = lp_raise(d, m, a.scale);
+        for (int o = 8; o > 0; o >>= 1) c = fmax(c, __shfl_xor_sync(0xffffffffu, c, o));
+        c = __shfl_sync(0xffffffffu, c, 0);
+        if (d.z == 0.f) d.w = 0.f;
+        else lp_lower(d.z, d.w, (float)(c - d.c));
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
+        for (int o = 8; o > 0; o >>= 1) {
             d.z += __shfl_xor_sync(0xffffffffu, d.z, o);
             d.w += __shfl_xor_sync(0xffffffffu, d.w, o);
         }
+        d.z = __shfl_sync(0xffffffffu, d.z, 0);
+        d.w = __shfl_sync(0xffffffffu, d.w, 0);
         const bool mass = !(d.z == 0.f);                      // (a NaN counts as mass: it has to come out)
         const double ln2 = 0.69314718055994531, log_z = log2((double)d.z), scale = (double)a.scale;
-        auto logprob = [&](float x) { return !mass || x == -INFINITY ? -INFINITY : (float)((scale * ((double)x - (double)m) - log_z) * ln2); };
+        auto logprob = [&](float x) { return !mass || x == -INFINITY ? -INFINITY : (float)((scale * (double)x - c - log_z) * ln2); };
         if (a.out_lp && lane < a.n_ids) a.out_lp[(long long)r * a.n_ids + lane] = logprob(asked);
         if (a.out_h && lane == 0) a.out_h[r] = mass ? (float)((log_z - (double)d.w / (double)d.z) * ln2) : 0.f;
         if (TOP) {
             u64 best = s_top[lane];
-            for (int c = 1; c < S; ++c) best = lp_merge(best, *cluster.map_shared_rank(s_top + lane, c), lane);
+            for (int k = 1; k < S; ++k) best = lp_merge(best, *cluster.map_shared_rank(s_top + lane, k), lane);
             if (lane < a.top_n) {
                 const int id = best ? key_index(best) : -1;
                 a.out_top[(long long)r * a.top_n + lane] = id;

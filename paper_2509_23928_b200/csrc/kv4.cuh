@@ -62,25 +62,31 @@ __device__ __forceinline__ unsigned kv4_code_exact(float x, float m, float s) {
 }
 
 // Codes of 8 values as 8 nibbles.  t = (x - m) / s comes from a product with the reciprocal, off by less than 2^-18; where it is
-// nearer than 2^-17 to a tie the exact form decides.
+// nearer than 2^-17 to a tie (of bf16 values one in a few hundred is one) the exact form decides.
 __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t params) {
     const float m = kv4_min(params), s = kv4_scale(params);
     uint32_t w = 0u;
+    float off = 1.f, inv = 0.f;
     if (s >= 1e-30f) {
-        const float inv = 1.f / s;
-        bool near = false;
+        inv = 1.f / s;
+        off = 0.f;
+#pragma unroll
+        for (int i = 7; i >= 0; --i) {
+            const float t = (x[i] - m) * inv;
+            const float u = t + 12582912.f;                 // 1.5 * 2^23: the nearest integer in the low bits
+            off = fmaxf(off, fabsf(t - (u - 12582912.f)));
+            w = w * 16u + __float_as_uint(u);               // (0x4B400000 above n: together 0x3F400000 in 32 bits)
+        }
+        w -= 0x3F400000u;
+    }
+    if (off > 0.5f - 0x1p-17f) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float t = (x[i] - m) * inv;
-            const float u = t + 12582912.f;                 // 1.5 * 2^23: the nearest integer in the low bits
-            near |= fabsf(t - (u - 12582912.f)) > 0.5f - 0x1p-17f;
-            w |= (__float_as_uint(u) & 15u) << (4 * i);
+            if (!(s >= 1e-30f) || fabsf(t - rintf(t)) > 0.5f - 0x1p-17f)
+                w = (w & ~(15u << (4 * i))) | (kv4_code_exact(x[i], m, s) << (4 * i));
         }
-        if (!near) return w;
-        w = 0u;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w |= kv4_code_exact(x[i], m, s) << (4 * i);
     return w;
 }
 
