@@ -134,28 +134,56 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const __grid_constant__
     kv4_store_row<DH>(a.c, p, p.packed >= 0, k, v);
 }
 
-// Read: a lane has four neighbouring channels of a row, so that a warp writes whole lines.
+// Read: a lane has four neighbouring channels of a row, so that a warp writes whole lines, and four rows.
+#define KV4_READ_ROWS 4
 template <int DH>
 __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ Kv4RowsArgs a) {
     constexpr int LR = DH / 4, UNITS = 256 / LR;
     pdl_wait();
     pdl_trigger();
-    const int l = threadIdx.x % LR, unit = threadIdx.x / LR;
+    const int l = threadIdx.x % LR, unit = threadIdx.x / LR, per = UNITS >> a.heads_log2;
     const int h = (blockIdx.y << a.heads_log2) + (unit & ((1 << a.heads_log2) - 1));
-    const int j = blockIdx.x * (UNITS >> a.heads_log2) + (unit >> a.heads_log2);
-    if (h >= a.c.Hkv || j >= a.cu.v[a.sl.n]) return;
-    const int b = kv4_owner(a.cu, a.sl.n, j), start = a.start[b];
-    if (start < 0 || start >= a.c.max_len || j - a.cu.v[b] >= a.c.max_len - start) return;
-    const int row = start + (j - a.cu.v[b]), r = row % KV4_TILE, w = l >> 3, c = (l >> 1) & 3, g = l & 7;
-    const unsigned char* tile = kv4_tile(a.c, a.sl.slot[b], h, row);
-    auto half = [&](int at) { return (uint32_t)*(const uint16_t*)(tile + at); };
-    const uint32_t kw = half(kv4_k_at(DH, r, w, c) + 2 * (l & 1)), vw = half(kv4_v_at(DH, r, w, g));
-    const float ks = bf16_lo(half(kv4_s_at(DH, 0, r, w))), km = bf16_lo(half(kv4_m_at(DH, 0, r, w)));
-    const float vs = bf16_lo(half(kv4_s_at(DH, 1, r, w))), vm = bf16_lo(half(kv4_m_at(DH, 1, r, w)));
-    auto value = [](uint32_t codes, int i, float s, float m) { return fmaf((float)((codes >> (4 * i)) & 15u), s, m); };
-    const long long o = ((long long)j * a.c.Hkv + h) * DH + 4 * l;
-    *(float4*)(a.out_k + o) = make_float4(value(kw, 0, ks, km), value(kw, 1, ks, km), value(kw, 2, ks, km), value(kw, 3, ks, km));
-    *(float4*)(a.out_v + o) = make_float4(value(vw, 0, vs, vm), value(vw, 1, vs, vm), value(vw, 2, vs, vm), value(vw, 3, vs, vm));
+    const int j0 = blockIdx.x * (per * KV4_READ_ROWS) + (unit >> a.heads_log2), total = a.cu.v[a.sl.n];
+    if (h >= a.c.Hkv || j0 >= total) return;
+    int b = kv4_owner(a.cu, a.sl.n, j0);
+    const int w = l >> 3, at_k = kv4_k_at(DH, 0, w, (l >> 1) & 3) + 2 * (l & 1), at_v = kv4_v_at(DH, 0, w, l & 7);
+    const long long head_stride = (long long)(a.c.max_len / KV4_TILE) * kv4_tile_bytes(DH);
+    uint32_t kw[KV4_READ_ROWS], vw[KV4_READ_ROWS], p[KV4_READ_ROWS][4];
+    bool live[KV4_READ_ROWS];
+#pragma unroll
+    for (int u = 0; u < KV4_READ_ROWS; ++u) {
+        const int j = j0 + u * per;
+        live[u] = j < total;
+        if (!live[u]) break;
+        while (j >= a.cu.v[b + 1]) ++b;
+        const int start = a.start[b];
+        live[u] = start >= 0 && start < a.c.max_len && j - a.cu.v[b] < a.c.max_len - start;
+        if (!live[u]) continue;
+        const int row = start + (j - a.cu.v[b]), r = row % KV4_TILE;
+        const unsigned char* tile = a.c.data + ((long long)a.sl.slot[b] * a.c.Hkv + h) * head_stride + (long long)(row / KV4_TILE) * kv4_tile_bytes(DH);
+        auto half = [&](int at) { return (uint32_t)__ldg((const unsigned short*)(tile + at)); };
+        kw[u] = half(at_k + r * (DH / 2));
+        vw[u] = half(at_v + (r & ~1) * (DH / 2) + (r & 1) * 2);
+        p[u][0] = half(kv4_s_at(DH, 0, r, w));
+        p[u][1] = half(kv4_m_at(DH, 0, r, w));
+        p[u][2] = half(kv4_s_at(DH, 1, r, w));
+        p[u][3] = half(kv4_m_at(DH, 1, r, w));
+    }
+    auto value = [](uint32_t codes, int i, uint32_t s, uint32_t m) {
+        const float n = __uint_as_float(((codes >> (4 * i)) & 15u) | 0x4B000000u) - 8388608.f;
+        return fmaf(n, __uint_as_float(s << 16), __uint_as_float(m << 16));
+    };
+#pragma unroll
+    for (int u = 0; u < KV4_READ_ROWS; ++u) {
+        const int j = j0 + u * per;
+        if (j >= total) break;
+        if (!live[u]) continue;
+        const long long o = ((long long)j * a.c.Hkv + h) * DH + 4 * l;
+        *(float4*)(a.out_k + o) = make_float4(value(kw[u], 0, p[u][0], p[u][1]), value(kw[u], 1, p[u][0], p[u][1]),
+                                              value(kw[u], 2, p[u][0], p[u][1]), value(kw[u], 3, p[u][0], p[u][1]));
+        *(float4*)(a.out_v + o) = make_float4(value(vw[u], 0, p[u][2], p[u][3]), value(vw[u], 1, p[u][2], p[u][3]),
+                                              value(vw[u], 2, p[u][2], p[u][3]), value(vw[u], 3, p[u][2], p[u][3]));
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -171,11 +199,11 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ K
 // queries and their probabilities go in as two fp16 numbers (22 bits), the codes as whole numbers, and the products of 16 rows are
 // added up in fp32 outside the tensor core.
 //
-// A cluster of up to 16 CTAs shares one (sequence, KV head, block of columns); a warp takes every (warps of the cluster)-th tile of
-// 16 rows, which one bulk copy brings into its own ring of four, and keeps its own maximum, sum and output.  They are joined in
+// A cluster of up to 16 CTAs shares one (sequence, KV head, block of columns); a warp takes every (warps of the cluster)-th step of
+// 16 or 32 rows, which bulk copies bring into its own ring, and keeps its own maximum, sum and output.  They are joined in
 // shared memory, then over the cluster, always in the same order.
 #define KV4_MAX_CLUSTER 16
-#define KV4_STAGES 4
+#define KV4_RING 4                   // tiles in a warp's ring
 #define KV4_WAIT_LIMIT (1 << 22)     // polls of a copy's barrier before a warp gives up (each may suspend for a while)
 
 struct Kv4AttnArgs {
@@ -221,18 +249,18 @@ __device__ __forceinline__ void kv4_lds(const unsigned char* p, uint32_t (&w)[Q]
 }
 
 __device__ __forceinline__ void kv4_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // the first of a sum
 __device__ __forceinline__ void kv4_mma0(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ void kv4_mma0_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
@@ -331,29 +359,29 @@ __device__ __forceinline__ float kv4_sum_rows(float x) {
     return x + __shfl_xor_sync(0xffffffffu, x, 16);
 }
 
-// One tile of 16 rows from `row` on.  EDGE: some of them are not for every column, or not there at all.
-template <int DH, int NT, bool SPLIT, bool EDGE>
-__device__ __forceinline__ void kv4_rows16(Kv4Warp<DH, NT, SPLIT>& st, const unsigned char* tile, int row, int lane, int j0, int G,
-                                           const Kv4Sight& sight) {
-    constexpr int Q = DH / 32, CH = DH / 8, H = Q / 2;
+// U tiles of 16 rows from `row` on.  EDGE: some of the rows are not for every column, or not there at all.  Two tiles at a time: the
+// chain from a tile's codes to its output is a thousand cycles long, and one tile alone leaves a warp waiting for most of them.
+template <int DH, int NT, bool SPLIT, int U, bool EDGE>
+__device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsigned char* tile, int row, int lane, int j0, int G,
+                                         const Kv4Sight& sight) {
+    constexpr int Q = DH / 32, CH = DH / 8, H = Q / 2, TB = kv4_tile_bytes(DH);
     const int g = lane >> 2, c = lane & 3;
-    const int r0 = row + g, r1 = r0 + 8;                          // this lane's rows
-    uint32_t p0[Q], p1[Q];                                        // s of the groups two by two, then m
-    kv4_lds<Q>(tile + 16 * DH + g * CH, p0);
-    kv4_lds<Q>(tile + 17 * DH + g * CH, p1);
-    float s[NT][4];
-    {
-        uint32_t k0[Q], k1[Q];
-        kv4_lds<Q>(tile + g * (DH / 2) + c * CH, k0);
-        kv4_lds<Q>(tile + (g + 8) * (DH / 2) + c * CH, k1);
+    float s[U][NT][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        uint32_t p0[Q], p1[Q], k0[Q], k1[Q];                      // s of the groups two by two, then m; codes: of this lane's rows g, g + 8
+        kv4_lds<Q>(tile + u * TB + 16 * DH + g * CH, p0);
+        kv4_lds<Q>(tile + u * TB + 17 * DH + g * CH, p1);
+        kv4_lds<Q>(tile + u * TB + g * (DH / 2) + c * CH, k0);
+        kv4_lds<Q>(tile + u * TB + (g + 8) * (DH / 2) + c * CH, k1);
         if constexpr (!SPLIT) {
             // the lane's columns of A: the m of groups 2 c and 2 c + 1, the groups over and over again
-            const uint32_t m0 = H == 2 && (c & 1) ? p0[H + 1] : p0[H], m1 = H == 2 && (c & 1) ? p1[H + 1] : p1[H];
+            const uint32_t m0 = H == 2 && (c & 1) ? p0[Q - 1] : p0[H], m1 = H == 2 && (c & 1) ? p1[Q - 1] : p1[H];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) kv4_mma0_bf16(s[n], m0, m1, m0, m1, st.qm[n][0], st.qm[n][1]);
+            for (int n = 0; n < NT; ++n) kv4_mma0_bf16(s[u][n], m0, m1, m0, m1, st.qm[n][0], st.qm[n][1]);
         } else {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+            for (int n = 0; n < NT; ++n) s[u][n][0] = s[u][n][1] = s[u][n][2] = s[u][n][3] = 0.f;
         }
 #pragma unroll
         for (int w = 0; w < Q; ++w) {
@@ -370,40 +398,47 @@ __device__ __forceinline__ void kv4_rows16(Kv4Warp<DH, NT, SPLIT>& st, const uns
                     kv4_mma(d, f0, f1, f2, f3, st.ql[n][2 * w][0], st.ql[n][2 * w][1]);
                     kv4_mma(d, h0, h1, h2, h3, st.ql[n][2 * w + 1][0], st.ql[n][2 * w + 1][1]);
                     const float mn0 = kv4_bf(p0[H + (w >> 1)], w & 1), mn1 = kv4_bf(p1[H + (w >> 1)], w & 1);
-                    s[n][0] = fmaf(mn0, st.qs[n][w][0], s[n][0]);
-                    s[n][1] = fmaf(mn0, st.qs[n][w][1], s[n][1]);
-                    s[n][2] = fmaf(mn1, st.qs[n][w][0], s[n][2]);
-                    s[n][3] = fmaf(mn1, st.qs[n][w][1], s[n][3]);
+                    s[u][n][0] = fmaf(mn0, st.qs[n][w][0], s[u][n][0]);
+                    s[u][n][1] = fmaf(mn0, st.qs[n][w][1], s[u][n][1]);
+                    s[u][n][2] = fmaf(mn1, st.qs[n][w][0], s[u][n][2]);
+                    s[u][n][3] = fmaf(mn1, st.qs[n][w][1], s[u][n][3]);
                 }
-                s[n][0] = fmaf(sc0, d[0], s[n][0]);
-                s[n][1] = fmaf(sc0, d[1], s[n][1]);
-                s[n][2] = fmaf(sc1, d[2], s[n][2]);
-                s[n][3] = fmaf(sc1, d[3], s[n][3]);
+                s[u][n][0] = fmaf(sc0, d[0], s[u][n][0]);
+                s[u][n][1] = fmaf(sc0, d[1], s[u][n][1]);
+                s[u][n][2] = fmaf(sc1, d[2], s[u][n][2]);
+                s[u][n][3] = fmaf(sc1, d[3], s[u][n][3]);
             }
         }
     }
     // ---- scores above the running maximum, in powers of two
-    float p[NT][4], top = -INFINITY;
+    float p[U][NT][4], top = -INFINITY;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (EDGE)
-                if (!sight(e < 2 ? r0 : r1, min((j0 + 8 * n + 2 * c + (e & 1)) / G, sight.n_q - 1))) s[n][e] = -INFINITY;
-            p[n][e] = fmaf(s[n][e], st.fq[n][e & 1], -st.m[n][e & 1]);
-            top = fmaxf(top, p[n][e]);
-        }
-    }
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (EDGE)
+                    if (!sight(row + 16 * u + g + (e < 2 ? 0 : 8), min((j0 + 8 * n + 2 * c + (e & 1)) / G, sight.n_q - 1))) s[u][n][e] = -INFINITY;
+                p[u][n][e] = fmaf(s[u][n][e], st.fq[n][e & 1], -st.m[n][e & 1]);
+                top = fmaxf(top, p[u][n][e]);
+            }
     if (__any_sync(0xffffffffu, top > KV4_LAZY)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float m = fmaxf(st.m[n][e], kv4_max_rows(fmaxf(s[n][e] * st.fq[n][e], s[n][e + 2] * st.fq[n][e])));
+                float m = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < U; ++u) m = fmaxf(m, fmaxf(s[u][n][e] * st.fq[n][e], s[u][n][e + 2] * st.fq[n][e]));
+                m = fmaxf(st.m[n][e], kv4_max_rows(m));
                 const float f = kv4_exp2(st.m[n][e] - m);
                 st.m[n][e] = m;
-                p[n][e] = fmaf(s[n][e], st.fq[n][e], -m);
-                p[n][e + 2] = fmaf(s[n][e + 2], st.fq[n][e], -m);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    p[u][n][e] = fmaf(s[u][n][e], st.fq[n][e], -m);
+                    p[u][n][e + 2] = fmaf(s[u][n][e + 2], st.fq[n][e], -m);
+                }
                 st.l[n][e] *= f;
 #pragma unroll
                 for (int w = 0; w < Q; ++w) {
@@ -415,96 +450,157 @@ __device__ __forceinline__ void kv4_rows16(Kv4Warp<DH, NT, SPLIT>& st, const uns
         }
     }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[n][e] = kv4_exp2(p[n][e]);
-        st.l[n][0] += p[n][0] + p[n][2];
-        st.l[n][1] += p[n][1] + p[n][3];
-    }
-    // ---- the values
-    kv4_lds<Q>(tile + 18 * DH + g * CH, p0);
-    kv4_lds<Q>(tile + 19 * DH + g * CH, p1);
-    if constexpr (EDGE) {
-        // what lies behind the last row is anything at all
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int w = 0; w < Q; ++w) {
-            if (r0 >= sight.nrows) p0[w] = 0u;
-            if (r1 >= sight.nrows) p1[w] = 0u;
+            for (int e = 0; e < 4; ++e) p[u][n][e] = kv4_exp2(p[u][n][e]);
+            st.l[n][0] += p[u][n][0] + p[u][n][2];
+            st.l[n][1] += p[u][n][1] + p[u][n][3];
         }
-    }
-    {
-        // R follows the largest scale, by halves of words (no scale is negative; a NaN's is above all)
-        uint32_t big = 0u;
+    // ---- the values
+    uint32_t a0[U][Q], a1[U][Q];                                    // s of the lane's rows' pairs, a word a group
+    const uint32_t mine = g & 1 ? 0x3244u : 0x1044u;                // the lane's rows are the even or the odd ones of their pairs
+    uint32_t big = 0u;
 #pragma unroll
-        for (int w = 0; w < H; ++w) big = __vmaxu2(big, __vmaxu2(p0[w], p1[w]));
-        if (__any_sync(0xffffffffu, max(big >> 16, big & 0xFFFFu) >= st.r_limit)) {
-            uint32_t fin = 0u;                                      // (rows that hold a NaN decide nothing)
+    for (int u = 0; u < U; ++u) {
+        kv4_lds<Q>(tile + u * TB + 18 * DH + (g >> 1) * (DH / 4), a0[u]);
+        kv4_lds<Q>(tile + u * TB + 19 * DH + (g >> 1) * (DH / 4), a1[u]);
+        if constexpr (EDGE) {
+            // what lies behind the last row is anything at all
+            const int pair = row + 16 * u + (g & 6);
 #pragma unroll
             for (int w = 0; w < Q; ++w) {
-                const uint32_t u0 = (p0[w >> 1] >> (16 * (w & 1))) & 0xFFFFu, u1 = (p1[w >> 1] >> (16 * (w & 1))) & 0xFFFFu;
-                if (u0 < 0x7F80u) fin = max(fin, u0);
-                if (u1 < 0x7F80u) fin = max(fin, u1);
+                if (pair >= sight.nrows) a0[u][w] = 0u;
+                if (pair + 1 >= sight.nrows) a0[u][w] &= 0xFFFFu;
+                if (pair + 8 >= sight.nrows) a1[u][w] = 0u;
+                if (pair + 9 >= sight.nrows) a1[u][w] &= 0xFFFFu;
             }
-            fin = __reduce_max_sync(0xffffffffu, fin);
-            const int e = min(max((int)(fin >> 7) - 127, -114), 114);       // scales are below 2^(e + 1)
-            const float R = kv4_pow2(5 - e);
-            if (R < st.R) {
-                const float f = R / st.R;
+        }
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+        for (int w = 0; w < Q; ++w) big = __vmaxu2(big, __vmaxu2(a0[u][w], a1[u][w]));
+    }
+    // R follows the largest scale, by halves of words (no scale is negative; a NaN's is above all)
+    if (__any_sync(0xffffffffu, max(big >> 16, big & 0xFFFFu) >= st.r_limit)) {
+        uint32_t fin = 0u;                                          // (rows that hold a NaN decide nothing)
 #pragma unroll
-                    for (int i = 0; i < 2 * Q; ++i)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-                        for (int t = 0; t < 4; ++t) st.o[n][i][t] *= f;
-                st.R = R;
-                st.r_limit = (uint32_t)(e + 1 + 127) << 7;
+            for (int w = 0; w < Q; ++w) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t u0 = (a0[u][w] >> (16 * t)) & 0xFFFFu, u1 = (a1[u][w] >> (16 * t)) & 0xFFFFu;
+                    if (u0 < 0x7F80u) fin = max(fin, u0);
+                    if (u1 < 0x7F80u) fin = max(fin, u1);
+                }
+            }
+        fin = __reduce_max_sync(0xffffffffu, fin);
+        const int e = min(max((int)(fin >> 7) - 127, -114), 114);           // scales are below 2^(e + 1)
+        const float R = kv4_pow2(5 - e);
+        if (R < st.R) {
+            const float f = R / st.R;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2 * Q; ++i)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) st.o[n][i][t] *= f;
+            st.R = R;
+            st.r_limit = (uint32_t)(e + 1 + 127) << 7;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        uint32_t v0[Q], v1[Q];
+        kv4_lds<Q>(tile + u * TB + 8 * DH + c * DH + g * CH, v0);
+        kv4_lds<Q>(tile + u * TB + 8 * DH + (c + 4) * DH + g * CH, v1);
+        float pr[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr[n][e] = p[u][n][e] * st.R;
+        uint32_t q0[Q], q1[Q];                                      // m likewise
+        kv4_lds<Q>(tile + u * TB + 18 * DH + (g >> 1) * (DH / 4) + CH, q0);
+        kv4_lds<Q>(tile + u * TB + 19 * DH + (g >> 1) * (DH / 4) + CH, q1);
+#pragma unroll
+        for (int w = 0; w < Q; ++w) {
+            const float sc0 = __uint_as_float(__byte_perm(a0[u][w], 0u, mine)), sc1 = __uint_as_float(__byte_perm(a1[u][w], 0u, mine));
+            const float mn0 = __uint_as_float(__byte_perm(q0[w], 0u, mine)), mn1 = __uint_as_float(__byte_perm(q1[w], 0u, mine));
+            uint32_t f0, f1, f2, f3, g0, g1, g2, g3;
+            if constexpr (SPLIT) {
+                const uint32_t y0 = v0[w] >> 8, y1 = v1[w] >> 8;
+                f0 = kv4_lo<true>(v0[w]); f1 = kv4_hi<true>(v0[w]); f2 = kv4_lo<true>(v1[w]); f3 = kv4_hi<true>(v1[w]);
+                g0 = kv4_lo<true>(y0); g1 = kv4_hi<true>(y0); g2 = kv4_lo<true>(y1); g3 = kv4_hi<true>(y1);
+            } else {
+                // whole bytes, n + 16 n', for the first of two channels: the second one's sum is taken off in the end
+                f0 = v0[w] & 0x00FF00FFu; f2 = v1[w] & 0x00FF00FFu;
+                g0 = __byte_perm(v0[w], 0u, 0x4341); g2 = __byte_perm(v1[w], 0u, 0x4341);
+                f1 = kv4_hi<false>(f0); f3 = kv4_hi<false>(f2); g1 = kv4_hi<false>(g0); g3 = kv4_hi<false>(g2);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float ps[4] = {pr[n][0] * sc0, pr[n][1] * sc0, pr[n][2] * sc1, pr[n][3] * sc1};
+                const float* pp = p[u][n];
+                if constexpr (EDGE) {
+                    // a column that does not see the row takes nothing of it, not even a NaN
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (pp[e] == 0.f) ps[e] = 0.f;
+                    st.mn[n][w][0] += (pp[0] == 0.f ? 0.f : pp[0] * mn0) + (pp[2] == 0.f ? 0.f : pp[2] * mn1);
+                    st.mn[n][w][1] += (pp[1] == 0.f ? 0.f : pp[1] * mn0) + (pp[3] == 0.f ? 0.f : pp[3] * mn1);
+                } else {
+                    st.mn[n][w][0] = fmaf(pp[0], mn0, fmaf(pp[2], mn1, st.mn[n][w][0]));
+                    st.mn[n][w][1] = fmaf(pp[1], mn0, fmaf(pp[3], mn1, st.mn[n][w][1]));
+                }
+                const uint32_t h0 = kv4_half2(ps[0], ps[1]), h1 = kv4_half2(ps[2], ps[3]);
+                const uint32_t b0 = kv4_transpose(h0), b1 = kv4_transpose(h1);
+                if constexpr (SPLIT) {
+                    const float2 w0 = kv4_unhalf2(h0), w1 = kv4_unhalf2(h1);
+                    const uint32_t c0 = kv4_transpose(kv4_half2(ps[0] - w0.x, ps[1] - w0.y)), c1 = kv4_transpose(kv4_half2(ps[2] - w1.x, ps[3] - w1.y));
+                    float d[4], f[4];
+                    kv4_mma0(d, f0, f1, f2, f3, c0, c1);
+                    kv4_mma(d, f0, f1, f2, f3, b0, b1);
+                    kv4_mma0(f, g0, g1, g2, g3, c0, c1);
+                    kv4_mma(f, g0, g1, g2, g3, b0, b1);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        st.o[n][2 * w][e] += d[e];
+                        st.o[n][2 * w + 1][e] += f[e];
+                    }
+                } else {
+                    kv4_mma(st.o[n][2 * w], f0, f1, f2, f3, b0, b1);
+                    kv4_mma(st.o[n][2 * w + 1], g0, g1, g2, g3, b0, b1);
+                }
             }
         }
     }
-    uint32_t v0[Q], v1[Q];
-    kv4_lds<Q>(tile + 8 * DH + c * DH + g * CH, v0);
-    kv4_lds<Q>(tile + 8 * DH + (c + 4) * DH + g * CH, v1);
+}
+
+// B fragment of sum(q_g) = hi + mid + lo, eight bits each.  Rows 2 c, 2 c + 1 of B: groups 2 (c % (Q / 2)) and + 1, part c / (Q / 2) (four
+// groups: lo comes in rows 2 c + 8, 2 c + 9 of c = 0, 1; two groups: c = 3 has nothing).
+template <int Q>
+__device__ __forceinline__ void kv4_sum_parts(const float (&sum)[Q], int c, uint32_t (&qm)[2]) {
+    float part[Q][3];
 #pragma unroll
     for (int w = 0; w < Q; ++w) {
-        const float a0 = kv4_bf(p0[w >> 1], w & 1), a1 = kv4_bf(p1[w >> 1], w & 1);
-        const float mn0 = kv4_bf(p0[H + (w >> 1)], w & 1), mn1 = kv4_bf(p1[H + (w >> 1)], w & 1);
-        const uint32_t x0 = v0[w], x1 = v1[w], y0 = x0 >> 8, y1 = x1 >> 8;
-        const uint32_t f0 = kv4_lo<SPLIT>(x0), f1 = kv4_hi<SPLIT>(x0), f2 = kv4_lo<SPLIT>(x1), f3 = kv4_hi<SPLIT>(x1);
-        const uint32_t g0 = kv4_lo<SPLIT>(y0), g1 = kv4_hi<SPLIT>(y0), g2 = kv4_lo<SPLIT>(y1), g3 = kv4_hi<SPLIT>(y1);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float ps[4] = {p[n][0] * st.R * a0, p[n][1] * st.R * a0, p[n][2] * st.R * a1, p[n][3] * st.R * a1};
-            if constexpr (EDGE) {
-                // a column that does not see the row takes nothing of it, not even a NaN
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (p[n][e] == 0.f) ps[e] = 0.f;
-                st.mn[n][w][0] += (p[n][0] == 0.f ? 0.f : p[n][0] * mn0) + (p[n][2] == 0.f ? 0.f : p[n][2] * mn1);
-                st.mn[n][w][1] += (p[n][1] == 0.f ? 0.f : p[n][1] * mn0) + (p[n][3] == 0.f ? 0.f : p[n][3] * mn1);
-            } else {
-                st.mn[n][w][0] = fmaf(p[n][0], mn0, fmaf(p[n][2], mn1, st.mn[n][w][0]));
-                st.mn[n][w][1] = fmaf(p[n][1], mn0, fmaf(p[n][3], mn1, st.mn[n][w][1]));
-            }
-            const uint32_t h0 = kv4_half2(ps[0], ps[1]), h1 = kv4_half2(ps[2], ps[3]);
-            const uint32_t b0 = kv4_transpose(h0), b1 = kv4_transpose(h1);
-            if constexpr (SPLIT) {
-                const float2 w0 = kv4_unhalf2(h0), w1 = kv4_unhalf2(h1);
-                const uint32_t c0 = kv4_transpose(kv4_half2(ps[0] - w0.x, ps[1] - w0.y)), c1 = kv4_transpose(kv4_half2(ps[2] - w1.x, ps[3] - w1.y));
-                float d[4], u[4];
-                kv4_mma0(d, f0, f1, f2, f3, c0, c1);
-                kv4_mma(d, f0, f1, f2, f3, b0, b1);
-                kv4_mma0(u, g0, g1, g2, g3, c0, c1);
-                kv4_mma(u, g0, g1, g2, g3, b0, b1);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    st.o[n][2 * w][e] += d[e];
-                    st.o[n][2 * w + 1][e] += u[e];
-                }
-            } else {
-                kv4_mma(st.o[n][2 * w], f0, f1, f2, f3, b0, b1);
-                kv4_mma(st.o[n][2 * w + 1], g0, g1, g2, g3, b0, b1);
-            }
-        }
+        part[w][0] = __bfloat162float(__float2bfloat16_rn(sum[w]));
+        part[w][1] = __bfloat162float(__float2bfloat16_rn(sum[w] - part[w][0]));
+        part[w][2] = sum[w] - part[w][0] - part[w][1];
+    }
+    auto pair = [](float x, float y) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+        return *(const uint32_t*)&v;
+    };
+    if constexpr (Q == 4) {
+        const uint32_t b00 = pair(part[0][0], part[1][0]), b01 = pair(part[2][0], part[3][0]);
+        const uint32_t b10 = pair(part[0][1], part[1][1]), b11 = pair(part[2][1], part[3][1]);
+        const uint32_t b20 = pair(part[0][2], part[1][2]), b21 = pair(part[2][2], part[3][2]);
+        qm[0] = c == 0 ? b00 : c == 1 ? b01 : c == 2 ? b10 : b11;
+        qm[1] = c == 0 ? b20 : c == 1 ? b21 : 0u;
+    } else {
+        const uint32_t b0 = pair(part[0][0], part[1][0]), b1 = pair(part[0][1], part[1][1]), b2 = pair(part[0][2], part[1][2]);
+        qm[0] = c == 0 ? b0 : c == 1 ? b1 : c == 2 ? b2 : 0u;
+        qm[1] = 0u;
     }
 }
 
@@ -565,30 +661,7 @@ __device__ __forceinline__ void kv4_load_queries(Kv4Warp<DH, NT, sizeof(T) == 4>
             sum[w] *= UNIT;                                       // in the unit of the products
         }
         if constexpr (!SPLIT) {
-            // sum(q_g) = hi + mid + lo, eight bits each.  Rows 2 c, 2 c + 1 of B: groups 2 (c % (Q / 2)) and + 1, part c / (Q / 2) (four
-            // groups: lo comes in rows 2 c + 8, 2 c + 9 of c = 0, 1; two groups: c = 3 has nothing)
-            float part[Q][3];
-#pragma unroll
-            for (int w = 0; w < Q; ++w) {
-                part[w][0] = __bfloat162float(__float2bfloat16_rn(sum[w]));
-                part[w][1] = __bfloat162float(__float2bfloat16_rn(sum[w] - part[w][0]));
-                part[w][2] = sum[w] - part[w][0] - part[w][1];
-            }
-            auto pair = [](float x, float y) {
-                const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
-                return *(const uint32_t*)&v;
-            };
-            if constexpr (Q == 4) {
-                const uint32_t b00 = pair(part[0][0], part[1][0]), b01 = pair(part[2][0], part[3][0]);
-                const uint32_t b10 = pair(part[0][1], part[1][1]), b11 = pair(part[2][1], part[3][1]);
-                const uint32_t b20 = pair(part[0][2], part[1][2]), b21 = pair(part[2][2], part[3][2]);
-                st.qm[n][0] = c == 0 ? b00 : c == 1 ? b01 : c == 2 ? b10 : b11;
-                st.qm[n][1] = c == 0 ? b20 : c == 1 ? b21 : 0u;
-            } else {
-                const uint32_t b0 = pair(part[0][0], part[1][0]), b1 = pair(part[0][1], part[1][1]), b2 = pair(part[0][2], part[1][2]);
-                st.qm[n][0] = c == 0 ? b0 : c == 1 ? b1 : c == 2 ? b2 : 0u;
-                st.qm[n][1] = 0u;
-            }
+            kv4_sum_parts<Q>(sum, c, st.qm[n]);
         }
         const float f = kv4_pow2(e - 14) * (1.f / UNIT) * a.scale_log2;
 #pragma unroll
@@ -606,25 +679,25 @@ __device__ __forceinline__ void kv4_load_queries(Kv4Warp<DH, NT, sizeof(T) == 4>
 // Shared memory: the warps' rings, and over them, once they are used up, [warp][column][DH + 4] outputs, maxima and sums.
 template <int DH, int NT>
 __host__ __device__ constexpr size_t kv4_smem(int warps) {
-    const size_t ring = (size_t)warps * KV4_STAGES * kv4_tile_bytes(DH), join = sizeof(float) * 8 * NT * (warps * (DH + 4 + 2) + 2);
+    const size_t ring = (size_t)warps * KV4_RING * kv4_tile_bytes(DH), join = sizeof(float) * 8 * NT * (warps * (DH + 4 + 2) + 2);
     return ring > join ? ring : join;
 }
 
-template <int DH, int NT, typename T, int WARPS, int CTAS>
+template <int DH, int NT, typename T, int U, int WARPS, int CTAS>
 __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid_constant__ Kv4AttnArgs a) {
     constexpr bool SPLIT = sizeof(T) == 4;
-    constexpr int Q = DH / 32, NB = 8 * NT, LDO = DH + 4, TB = kv4_tile_bytes(DH);
+    constexpr int Q = DH / 32, NB = 8 * NT, LDO = DH + 4, TB = kv4_tile_bytes(DH), ROWS = KV4_TILE * U, STAGES = KV4_RING / U;
     constexpr float UNIT = SPLIT ? 1.f : 0x1p-24f;
     extern __shared__ __align__(128) unsigned char kv4_sm[];
-    __shared__ u64 bars[WARPS][KV4_STAGES];
+    __shared__ u64 bars[WARPS][STAGES];
     float* sO = (float*)kv4_sm;                     // [warp][column][LDO]
     float* sM = sO + WARPS * NB * LDO;              // [warp][column]
     float* sL = sM + WARPS * NB;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const int b = blockIdx.z, h = blockIdx.y / a.n_blocks, j0 = (blockIdx.y % a.n_blocks) * NB;
     const int rank = blockIdx.x, S = gridDim.x;     // (a cluster is the x extent of the grid)
-    const uint32_t bar = kv4_saddr(bars[warp]), ring = kv4_saddr(kv4_sm) + warp * KV4_STAGES * TB;
-    if (lane < KV4_STAGES) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + lane * 8) : "memory");
+    const uint32_t bar = kv4_saddr(bars[warp]), ring = kv4_saddr(kv4_sm) + warp * KV4_RING * TB;
+    if (lane < STAGES) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + lane * 8) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async;" ::: "memory");
     __syncwarp();
@@ -638,17 +711,15 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
     // rows [0, clear) are visible to every column of the block, rows from `end` on to none
     const int clear = max(0, a.mask ? sight.nrows - a.mask_rows : sight.nrows - a.n_q + i_first + 1);
     const int end = max(0, a.mask ? sight.nrows : sight.nrows - a.n_q + i_last + 1);
-    const int ntile = (end + KV4_TILE - 1) / KV4_TILE, nfull = clear / KV4_TILE;
+    const int nstep = (end + ROWS - 1) / ROWS, nfull = clear / ROWS;         // steps of U tiles; those before `clear`
     const unsigned char* base = kv4_tile(a.c, a.sl.slot[b], h, 0);
     const int first = rank * WARPS + warp, step = S * WARPS;
 
-    const unsigned char* next = base + (long long)first * TB;
-    int ahead = first;                              // the next tile to be fetched
+    int ahead = first;                              // the next step to be fetched
 #pragma unroll
-    for (int i = 0; i < KV4_STAGES; ++i) {
-        if (ahead < ntile && lane == 0) kv4_fetch(ring + i * TB, next, TB, bar + i * 8);
+    for (int i = 0; i < STAGES; ++i) {
+        if (ahead < nstep && lane == 0) kv4_fetch(ring + i * U * TB, base + (long long)ahead * (U * TB), U * TB, bar + i * 8);
         ahead += step;
-        next += (long long)step * TB;
     }
     Kv4Warp<DH, NT, SPLIT> st;
     kv4_load_queries<DH, NT, T>(st, a, b, h, j0, lane);
@@ -671,23 +742,22 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
 
     bool ok = true;
     uint32_t stage = 0, parity = 0;
-    for (int t = first; t < ntile; t += step) {
+    for (int t = first; t < nstep; t += step) {
         ok = kv4_wait(bar + stage * 8, parity);
         if (!ok) break;
-        const unsigned char* tile = kv4_sm + (warp * KV4_STAGES + stage) * TB;
-        if (t < nfull) kv4_rows16<DH, NT, SPLIT, false>(st, tile, t * KV4_TILE, lane, j0, a.G, sight);
-        else kv4_rows16<DH, NT, SPLIT, true>(st, tile, t * KV4_TILE, lane, j0, a.G, sight);
+        const unsigned char* tile = kv4_sm + (warp * KV4_RING + stage * U) * TB;
+        if (t < nfull) kv4_rows<DH, NT, SPLIT, U, false>(st, tile, t * ROWS, lane, j0, a.G, sight);
+        else kv4_rows<DH, NT, SPLIT, U, true>(st, tile, t * ROWS, lane, j0, a.G, sight);
         __syncwarp();
-        if (ahead < ntile && lane == 0) kv4_fetch(ring + stage * TB, next, TB, bar + stage * 8);
+        if (ahead < nstep && lane == 0) kv4_fetch(ring + stage * U * TB, base + (long long)ahead * (U * TB), U * TB, bar + stage * 8);
         ahead += step;
-        next += (long long)step * TB;
-        if (++stage == KV4_STAGES) { stage = 0; parity ^= 1u; }
+        if (++stage == STAGES) { stage = 0; parity ^= 1u; }
     }
     if (!ok) {
         // a copy has not come: what is in flight is waited for once more, and the result is NaN
-        for (int i = 0; i < KV4_STAGES; ++i) {
+        for (int i = 0; i < STAGES; ++i) {
             kv4_wait(bar + stage * 8, parity);
-            if (++stage == KV4_STAGES) { stage = 0; parity ^= 1u; }
+            if (++stage == STAGES) { stage = 0; parity ^= 1u; }
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) st.l[n][0] = st.l[n][1] = __uint_as_float(0x7FC00000u);
@@ -709,10 +779,12 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
 #pragma unroll
             for (int w = 0; w < Q; ++w) {
                 const float m = kv4_sum_rows(st.mn[n][w][s]);
-                // channels 32 w + 4 g + 0..3: rows g and g + 8 of the two blocks of 16, the latter sixteenfold
+                // channels 32 w + 4 g + 0..3: rows g and g + 8 of the two blocks of 16, the latter sixteenfold, the former (bf16) with
+                // the latter added
+                const float x1 = st.o[n][2 * w][2 + s], y1 = st.o[n][2 * w + 1][2 + s];
+                const float x0 = st.o[n][2 * w][s] - (SPLIT ? 0.f : x1), y0 = st.o[n][2 * w + 1][s] - (SPLIT ? 0.f : y1);
                 *(float4*)(sO + (warp * NB + col) * LDO + 32 * w + 4 * g) =
-                    make_float4(fmaf(st.o[n][2 * w][s], down, m), fmaf(st.o[n][2 * w][2 + s], down * 0.0625f, m),
-                                fmaf(st.o[n][2 * w + 1][s], down, m), fmaf(st.o[n][2 * w + 1][2 + s], down * 0.0625f, m));
+                    make_float4(fmaf(x0, down, m), fmaf(x1, down * 0.0625f, m), fmaf(y0, down, m), fmaf(y1, down * 0.0625f, m));
             }
         }
     __syncthreads();
@@ -764,30 +836,26 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
 }
 
 // CTAs per (sequence, KV head, block of columns): as many as the GPU holds at once, but no more than the cache's full length has
-// tiles for their warps.
-static int kv4_cluster(int units, int max_len, int warps, int resident) {
-    const int most = max_len / (KV4_TILE * warps), want = resident / units;
+// steps for their warps.  Eight or sixteen, or less than eight: clusters of nine, say, leave a third of a GPC's places empty.
+static int kv4_cluster(int units, int max_len, int step_rows, int resident) {
+    const int most = max_len / step_rows, want = resident / units;
     const int s = want < most ? want : most;
-    return s < 1 ? 1 : s > KV4_MAX_CLUSTER ? KV4_MAX_CLUSTER : s;
+    return s < 1 ? 1 : s < 8 ? s : s < KV4_MAX_CLUSTER ? 8 : KV4_MAX_CLUSTER;
 }
 
-template <int DH, int NT, typename T, int WARPS, int CTAS>
-static cudaError_t kv4_launch_attn(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
-    constexpr int NB = 8 * NT;
-    constexpr size_t smem = kv4_smem<DH, NT>(WARPS);
-    auto kernel = kv4_attn_kernel<DH, NT, T, WARPS, CTAS>;
-    static bool attr_set[HIVIS_MAX_DEVICES] = {false};
+static cudaError_t kv4_launch(void (*kernel)(Kv4AttnArgs), bool* attr_set, Kv4AttnArgs& a, int columns, int threads, size_t smem, int step_rows,
+                              int resident, int dev, cudaStream_t st) {
     if (dev < 0 || dev >= HIVIS_MAX_DEVICES || !attr_set[dev]) {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < HIVIS_MAX_DEVICES) attr_set[dev] = true;
     }
-    a.n_blocks = (a.ncol + NB - 1) / NB;
-    const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, WARPS, num_sms * CTAS);
+    a.n_blocks = (a.ncol + columns - 1) / columns;
+    const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, step_rows, resident);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)S, (unsigned)(a.c.Hkv * a.n_blocks), (unsigned)a.sl.n);
-    cfg.blockDim = dim3(WARPS * 32);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2] = {};
@@ -800,11 +868,25 @@ static cudaError_t kv4_launch_attn(Kv4AttnArgs& a, int dev, int num_sms, cudaStr
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
-
+template <int DH, int NT, typename T, int U, int WARPS, int CTAS>
+static cudaError_t kv4_launch_attn(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
+    static bool attr_set[HIVIS_MAX_DEVICES] = {false};
+    return kv4_launch(kv4_attn_kernel<DH, NT, T, U, WARPS, CTAS>, attr_set, a, 8 * NT, WARPS * 32, kv4_smem<DH, NT>(WARPS),
+                      WARPS * U * KV4_TILE, num_sms * CTAS, dev, st);
+}
 template <int DH, typename T>
 static cudaError_t kv4_launch_attn_n(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
-    if (a.ncol <= 8) return kv4_launch_attn<DH, 1, T, 4, sizeof(T) == 4 ? 2 : 4>(a, dev, num_sms, st);
-    return kv4_launch_attn<DH, 2, T, 4, sizeof(T) == 4 ? 2 : 3>(a, dev, num_sms, st);
+    if constexpr (sizeof(T) == 4) {
+        if (a.ncol <= 8) return kv4_launch_attn<DH, 1, T, 1, 4, 2>(a, dev, num_sms, st);
+        return kv4_launch_attn<DH, 2, T, 1, 4, 2>(a, dev, num_sms, st);
+    } else {
+        if (a.ncol > 8) return kv4_launch_attn<DH, 2, T, 1, 4, 3>(a, dev, num_sms, st);
+        // Few (sequence, KV head) pairs do not fill the GPU with clusters of 16: a warp then gets more registers (nothing spilled)
+        // instead of a fourth neighbour.  4 x 4 pairs of 9 001 to 32 768 rows: 24.6 us, 29.1 with 128 registers; 16 x 32 pairs of
+        // 2176 rows, where four to an SM count: 48.7 us, 45.1 with 128.
+        if (a.sl.n * a.c.Hkv * KV4_MAX_CLUSTER < num_sms * 3) return kv4_launch_attn<DH, 1, T, 2, 4, 3>(a, dev, num_sms, st);
+        return kv4_launch_attn<DH, 1, T, 2, 4, 4>(a, dev, num_sms, st);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ C entries
@@ -859,11 +941,12 @@ static int kv4_check_rows(const char* who, const hivis_kv4_cache* cache, int B, 
     return HIVIS_OK;
 }
 
-// A CTA's `units` places are heads side by side (as many as there are, to a power of two) of neighbouring rows or pairs.
-static bool kv4_rows_grid(Kv4RowsArgs* a, int units, int items, dim3* grid) {
+// A CTA's `units` places are heads side by side (as many as there are, to a power of two) of neighbouring rows or pairs, `rounds` of
+// them after one another.
+static bool kv4_rows_grid(Kv4RowsArgs* a, int units, int rounds, int items, dim3* grid) {
     a->heads_log2 = 0;
     while ((1 << a->heads_log2) < units && (1 << a->heads_log2) < a->c.Hkv) a->heads_log2 += 1;
-    const int per = units >> a->heads_log2;
+    const int per = (units >> a->heads_log2) * rounds;
     const long long y = (a->c.Hkv + (1 << a->heads_log2) - 1) >> a->heads_log2;
     *grid = dim3((unsigned)(((long long)items + per - 1) / per), (unsigned)y);
     return y <= 65535;
@@ -889,7 +972,7 @@ extern "C" int hivis_kv4_append(const hivis_kv4_cache* cache, int B, const int* 
     a.k = k; a.v = v; a.ld = ld;
     dim3 grid;
     const dim3 block(256);
-    if (!kv4_rows_grid(&a, 256 / (a.c.dh / 4), a.pairs.v[B], &grid)) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads", who);
+    if (!kv4_rows_grid(&a, 256 / (a.c.dh / 4), 1, a.pairs.v[B], &grid)) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads", who);
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
     if (dtype == HIVIS_BF16) e = a.c.dh == 128 ? launch_pdl(kv4_append_kernel<128, bf16>, grid, block, 0, st, a) : launch_pdl(kv4_append_kernel<64, bf16>, grid, block, 0, st, a);
@@ -909,7 +992,7 @@ extern "C" int hivis_kv4_read(const hivis_kv4_cache* cache, int B, const int* se
     a.out_k = out_k; a.out_v = out_v;
     dim3 grid;
     const dim3 block(256);
-    if (!kv4_rows_grid(&a, 256 / (a.c.dh / 4), a.cu.v[B], &grid)) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads", who);
+    if (!kv4_rows_grid(&a, 256 / (a.c.dh / 4), KV4_READ_ROWS, a.cu.v[B], &grid)) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads", who);
     cudaStream_t st = (cudaStream_t)stream;
     return kv4_cuda(who, a.c.dh == 128 ? launch_pdl(kv4_read_kernel<128>, grid, block, 0, st, a) : launch_pdl(kv4_read_kernel<64>, grid, block, 0, st, a));
 }

@@ -23,6 +23,7 @@ namespace cg = cooperative_groups;
 
 #define LP_THREADS 256
 #define LP_WARPS (LP_THREADS / 32)
+#define LP_CTAS 4                 // to an SM
 #define LP_MAX_CLUSTER 16
 static_assert(HIVIS_LOGPROBS_MAX_IDS <= 32 && HIVIS_LOGPROBS_MAX_TOP <= 32, "a lane each");
 #define LP_CAND 512               // candidates a CTA keeps, and a cluster
@@ -193,7 +194,7 @@ struct LpPart {
 };
 
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 5) logprob_kernel(const __grid_constant__ LogprobArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, LP_CTAS) logprob_kernel(const __grid_constant__ LogprobArgs a) {
     constexpr int N = LpVec<T>::N, U = 4, STRIDE = LP_THREADS * N;
     __shared__ LpSum s_sum[LP_WARPS];
     __shared__ float s_most[LP_WARPS], s_max[LP_WARPS][32], s_bar;
@@ -218,10 +219,17 @@ __global__ void __launch_bounds__(LP_THREADS, 5) logprob_kernel(const __grid_con
     }
     LpSum s = {-LP_FAR, 0.f, 0.f};
     float most = -INFINITY;
+    uint4 next[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = lp_load<T>(row, first + u * STRIDE, lo, hi);
     for (int i = first; i < hi; i += U * STRIDE) {
         uint4 v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = lp_load<T>(row, i + u * STRIDE, lo, hi);
+        for (int u = 0; u < U; ++u) v[u] = next[u];
+        if (i + U * STRIDE < hi) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) next[u] = lp_load<T>(row, i + (U + u) * STRIDE, lo, hi);
+        }
         const float m = lp_most<T>(v);
         most = fmaxf(most, m);
         const float c = fminf(fmaxf(a.scale * m, -LP_FAR), LP_FAR);
@@ -406,9 +414,10 @@ static cudaError_t lp_launch(LogprobArgs& a, int dev, int num_sms, cudaStream_t 
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < HIVIS_MAX_DEVICES) attr_set[dev] = true;
     }
-    // CTAs per row: enough to fill the GPU, each with a few thousand logits at least
+    // CTAs per row: two to an SM, each with a few thousand logits at least.  A CTA costs some microseconds beside its logits: 56 rows of
+    // 152064 take 12.3 us with 8 CTAs each, 14.4 with 4, 16.4 with 16; 1021 rows of 50257 take 45 with one, 58 with two.
     int S = 1;
-    while (S < LP_MAX_CLUSTER && (long long)a.n_rows * S < 4ll * num_sms && a.V / (2 * S) >= 2048) S *= 2;
+    while (S < LP_MAX_CLUSTER && (long long)a.n_rows * S < 2ll * num_sms && a.V / (2 * S) >= 2048) S *= 2;
     a.slice = ((a.V + 8 + S - 1) / S + 7) / 8 * 8;
     cudaLaunchConfig_t cfg = {};
     const int y = a.n_rows < 32768 ? a.n_rows : 32768;

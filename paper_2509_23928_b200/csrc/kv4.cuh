@@ -6,7 +6,8 @@
 // A group that holds a NaN or an infinity, or whose range overflows, gets m = s = NaN.
 //
 // Rows lie in tiles of 16, [slot][KV head][row / 16], 20 dh bytes each, so that one copy brings everything the attention needs of 16
-// rows: the codes of K (16 rows of dh / 2 bytes), those of V, then per row s and m of K's groups (dh / 32 bf16 numbers each), then V's.
+// rows: the codes of K (16 rows of dh / 2 bytes), those of V, then per row s and m of K's groups (dh / 32 bf16 numbers each), then per
+// pair of rows s and m of V's groups (dh / 32 words each, the even row's number in the lower half, the odd row's in the upper).
 // Codes are in the order in which mma.m16n8k16 wants them as its A operand, so that the attention takes them from memory to the
 // tensor core with a mask and a shift:
 //   K  (A = keys: 16 rows x 16 channels).  A row is four chunks of dh / 8 bytes, chunk c for the lanes with lane % 4 = c; word w
@@ -36,56 +37,63 @@ __device__ __forceinline__ unsigned char* kv4_tile(const Kv4View& c, int slot, i
 __device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float kv4_min(uint32_t w) { return __uint_as_float(w << 16); }
 
-// Parameters of a group whose smallest and largest value are lo and hi.  Every step rounds towards the outside, and a number
-// that is exact before the last step stays exact: what comes out is the definition's m and s.
+// Parameters of a group whose smallest and largest value are lo and hi.  m: rounded down.  s: the smallest bf16 number with 15 s >=
+// hi - m.  15 s is an fp32 number, so the difference may be rounded up before it is compared; a product with 1 / 15 finds s up to
+// one bf16 step.
 __device__ __forceinline__ uint32_t kv4_params(float lo, float hi, bool finite) {
-    const bf16 m = __float2bfloat16_rd(lo);
-    const bf16 s = __float2bfloat16_ru(__fdiv_ru(__fsub_ru(hi, __bfloat162float(m)), 15.f));
-    const uint32_t w = ((uint32_t)__bfloat16_as_ushort(s) << 16) | __bfloat16_as_ushort(m);
-    const bool ok = finite && fabsf(__bfloat162float(m)) < INFINITY && __bfloat162float(s) < INFINITY;
-    return ok ? w : 0x7FC07FC0u;
+    const uint32_t m = __bfloat16_as_ushort(__float2bfloat16_rd(lo));
+    const float d = __fsub_ru(hi, __uint_as_float(m << 16));
+    uint32_t s = (__float_as_uint(d * (1.f / 15.f)) + 0xFFFFu) & 0xFFFF0000u;
+    if (15.f * __uint_as_float(s) < d) s += 0x10000u;
+    else if (s && 15.f * __uint_as_float(s - 0x10000u) >= d) s -= 0x10000u;
+    // (lo so low that it rounds to -infinity; a range beyond fp32's)
+    return finite && (m & 0x7F80u) != 0x7F80u && s < 0x7F800000u && d < INFINITY ? s | m : 0x7FC07FC0u;
 }
 
-// The code of x, decided without error.  x - m may need more than 24 bits: e is what d = x - m lost.  r = d - n s is exact (n s
-// has 12 bits, and the difference no bit below d's last), and so are the comparisons with s / 2, a multiple of d's last bit.
-__device__ __forceinline__ unsigned kv4_code_exact(float x, float m, float s) {
-    if (!(s > 0.f)) return 0u;
+// The code of x, decided without error; n is an integer next to the quotient or the one beside it.  x - m may need more than 24 bits:
+// e is what d = x - m lost.  r = d - n s is exact (n s has 12 bits, and the difference no bit below d's last), and so are the
+// comparisons with s / 2, a multiple of d's last bit.
+__device__ __forceinline__ unsigned kv4_code_exact(float x, float m, float s, float n, float up) {
     float d = x - m;
     const float bb = d - x;
     float e = (x - (d - bb)) - (m + bb);
-    if (s < 1e-30f) { d *= 0x1p96f; e *= 0x1p96f; s *= 0x1p96f; }      // (the quotient is the same)
-    float n = rintf(d / s);
+    d *= up;                                                // (a power of two, for both sides of the quotient)
+    e *= up;
+    s *= up;
     const float r = fmaf(-n, s, d), half = 0.5f * s;
     if (r > half || (r == half && e > 0.f)) n += 1.f;
     else if (r < -half || (r == -half && e <= 0.f)) n -= 1.f;
     return (unsigned)fminf(fmaxf(n, 0.f), 15.f);
 }
 
-// Codes of 8 values as 8 nibbles.  t = (x - m) / s comes from a product with the reciprocal, off by less than 2^-18; where it is
-// nearer than 2^-17 to a tie (of bf16 values one in a few hundred is one) the exact form decides.
+// Codes of 8 values as 8 nibbles.  t = (x - m) / s comes from a product with an approximate reciprocal, off by less than 2^-18; where
+// it is nearer than 2^-17 to a tie (of bf16 values one in some hundreds is one) the exact form decides.
 __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t params) {
     const float m = kv4_min(params), s = kv4_scale(params);
     uint32_t w = 0u;
-    float off = 1.f, inv = 0.f;
     if (s >= 1e-30f) {
-        inv = 1.f / s;
-        off = 0.f;
+        constexpr float MAGIC = 12582912.f;                 // 1.5 * 2^23: the nearest integer in the low bits
+        float inv, off = 0.f, t[8];
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
 #pragma unroll
         for (int i = 7; i >= 0; --i) {
-            const float t = (x[i] - m) * inv;
-            const float u = t + 12582912.f;                 // 1.5 * 2^23: the nearest integer in the low bits
-            off = fmaxf(off, fabsf(t - (u - 12582912.f)));
+            t[i] = (x[i] - m) * inv;
+            const float u = t[i] + MAGIC;
+            off = fmaxf(off, fabsf(t[i] - (u - MAGIC)));
             w = w * 16u + __float_as_uint(u);               // (0x4B400000 above n: together 0x3F400000 in 32 bits)
         }
         w -= 0x3F400000u;
-    }
-    if (off > 0.5f - 0x1p-17f) {
+        if (off > 0.5f - 0x1p-17f) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float t = (x[i] - m) * inv;
-            if (!(s >= 1e-30f) || fabsf(t - rintf(t)) > 0.5f - 0x1p-17f)
-                w = (w & ~(15u << (4 * i))) | (kv4_code_exact(x[i], m, s) << (4 * i));
+            for (int i = 0; i < 8; ++i) {
+                const float n = (t[i] + MAGIC) - MAGIC;
+                if (fabsf(t[i] - n) > 0.5f - 0x1p-17f) w = (w & ~(15u << (4 * i))) | (kv4_code_exact(x[i], m, s, n, 1.f) << (4 * i));
+            }
         }
+    } else if (s > 0.f) {
+        // (a NaN group and one of equal values keep zeros)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w |= kv4_code_exact(x[i], m, s, rintf((x[i] - m) * 0x1p96f / (s * 0x1p96f)), 0x1p96f) << (4 * i);
     }
     return w;
 }
@@ -94,5 +102,7 @@ __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t par
 // half of word g = 2 c of the group, the upper four into that of g = 2 c + 1.  Parameters of group w (which: 0 K, 1 V).
 __device__ __forceinline__ int kv4_k_at(int dh, int r, int w, int c) { return r * (dh / 2) + c * (dh / 8) + w * 4; }
 __device__ __forceinline__ int kv4_v_at(int dh, int r, int w, int g) { return 8 * dh + (r & ~1) * (dh / 2) + ((dh / 32) * g + w) * 4 + (r & 1) * 2; }
-__device__ __forceinline__ int kv4_s_at(int dh, int which, int r, int w) { return (16 + 2 * which) * dh + r * (dh / 8) + 2 * w; }
-__device__ __forceinline__ int kv4_m_at(int dh, int which, int r, int w) { return kv4_s_at(dh, which, r, w) + dh / 16; }
+__device__ __forceinline__ int kv4_s_at(int dh, int which, int r, int w) {
+    return which == 0 ? 16 * dh + r * (dh / 8) + 2 * w : 18 * dh + (r >> 1) * (dh / 4) + 4 * w + 2 * (r & 1);
+}
+__device__ __forceinline__ int kv4_m_at(int dh, int which, int r, int w) { return kv4_s_at(dh, which, r, w) + (which == 0 ? dh / 16 : dh / 8); }
