@@ -53,7 +53,7 @@ enum {
     HIVIS_ERR_NOMEM = -8     /* device or host allocation failed                          */
 };
 
-enum { HIVIS_F32 = 0, HIVIS_BF16 = 1 };
+enum { HIVIS_F32 = 0, HIVIS_BF16 = 1, HIVIS_BF16_KV4 = 2 /* hivis_config.dtype only */ };
 
 #define HIVIS_MAX_BATCH 64   /* upper limit for hivis_config.max_batch */
 #define HIVIS_MAX_K 16       /* upper limit for hivis_config.max_k     */
@@ -62,6 +62,11 @@ typedef struct {
     uint32_t struct_size;    /* sizeof(hivis_config), checked                              */
     int dtype;               /* HIVIS_F32 | HIVIS_BF16: weights, hidden states, residual   */
                              /* rows and the KV cache are all stored in this type          */
+                             /* HIVIS_BF16_KV4: as HIVIS_BF16, with the KV cache held in 4 */
+                             /* bits (the format under hivis_kv4_cache, below): 0.3125 of  */
+                             /* the memory.  Rows are rounded to bf16 and then quantised,  */
+                             /* the step's own row before it is attended to.  Draft steps  */
+                             /* run as a few launches each; no draft trees (SHAPE)         */
     int d;                   /* model width; multiple of 8                                 */
     int n_q_heads, n_kv_heads;   /* n_q_heads % n_kv_heads == 0                            */
     int head_dim;            /* 64 or 128                                                  */
@@ -207,7 +212,7 @@ int hivis_verify_sampled(hivis_ctx* ctx, int B, const int* seq_slots_host, int k
  * The slot's row count does not change until hivis_verify_tree; rows [P, P + 1 + (depth-1)*topk) of the
  * slot are used for the tree's K/V rows, so that many rows must be free (CAPACITY otherwise).
  * Limits: 1 <= topk <= HIVIS_TREE_MAX_TOPK, 1 <= depth <= max_k, 1 <= keep <= HIVIS_TREE_MAX_KEEP.
- * Errors: ARG, STATE (no pending pair), CAPACITY, CUDA.                                              */
+ * Errors: ARG, STATE (no pending pair), SHAPE (a context of dtype HIVIS_BF16_KV4), CAPACITY, CUDA.   */
 #define HIVIS_TREE_MAX_TOPK 16
 #define HIVIS_TREE_MAX_KEEP 256
 int hivis_draft_tree(hivis_ctx* ctx, int slot, int topk, int depth, int keep, const void* resid, int n_resid,

@@ -8,7 +8,7 @@ from typing import Dict, NamedTuple, Optional, Sequence
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libhivis.so")
 
-HIVIS_F32, HIVIS_BF16 = 0, 1
+HIVIS_F32, HIVIS_BF16, HIVIS_BF16_KV4 = 0, 1, 2
 HIVIS_MAX_BATCH, HIVIS_MAX_K = 64, 16
 TAPS = {"u": 0, "attn": 1, "y": 2, "act": 3, "g": 4, "q": 5}
 ERRORS = {0: "OK", -1: "ARG", -2: "SHAPE", -3: "DTYPE", -4: "STATE", -5: "CAPACITY", -6: "CUDA",
@@ -306,12 +306,17 @@ class Drafter:
     """Owns one hivis context.  `weights`: name -> CUDA tensor in the context dtype, [out, in]."""
 
     def __init__(self, dims, weights: Dict[str, "object"], max_batch: int, max_len: int, max_k: int = 8,
-                 stream=None):
+                 stream=None, kv_bits: Optional[int] = None):
+        """kv_bits: None keeps the cache in the weights' type; 4 (bf16 weights) holds it in 4 bits (HIVIS_BF16_KV4)."""
         import torch
         self.torch = torch
         self.dims = dims
         self.dtype = HIVIS_BF16 if dims.dtype == "bf16" else HIVIS_F32
         self.tdtype = torch.bfloat16 if self.dtype == HIVIS_BF16 else torch.float32
+        if kv_bits is not None:
+            if kv_bits != 4 or self.dtype != HIVIS_BF16:
+                raise ValueError("kv_bits takes 4, for drafters with bf16 weights")
+            self.dtype = HIVIS_BF16_KV4
         cfg = hivis_config(C.sizeof(hivis_config), self.dtype, dims.d, dims.n_q_heads, dims.n_kv_heads,
                            dims.head_dim, dims.ffn, dims.vocab, float(dims.rms_eps), float(dims.rope_base),
                            int(max_batch), int(max_len), int(max_k))

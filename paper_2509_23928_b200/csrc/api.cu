@@ -20,6 +20,8 @@ struct hivis_ctx {
     // weights (library-owned copies)
     void *embed, *lm_head, *fc, *norm1, *wqkv, *bqkv, *wo, *norm2, *wgu, *wdown, *resid_proj;
     void *Kc, *Vc;
+    Kv4View kv4;                  // dtype HIVIS_BF16_KV4: the cache, held in 4 bits (Kc and Vc are null)
+    float* kv4_q;                 // [rows_cap][qw] the step's queries after the rotary embedding
     double* inv_freq;
     // per-slot state
     int* kv_len;
@@ -215,7 +217,7 @@ int64_t hivis_step_bytes(const hivis_ctx* c, int B, const int* kv_rows_host) {
     int64_t bytes = params * (int64_t)c->esize;
     for (int b = 0; b < B; ++b) {
         const int64_t rows = kv_rows_host ? kv_rows_host[b] : 0;
-        bytes += 2 * (rows + 1) * c->kvw * (int64_t)c->esize;
+        bytes += c->kv4.data ? (rows + 1) * c->kvw * 5 / 4 : 2 * (rows + 1) * c->kvw * (int64_t)c->esize;
     }
     return bytes;
 }
@@ -238,7 +240,7 @@ int hivis_init(hivis_ctx** out, const hivis_config* cfg, const hivis_weights* w,
     if (!out || !cfg || !w) return bad(HIVIS_ERR_ARG, "null argument");
     *out = nullptr;
     if (cfg->struct_size != sizeof(hivis_config)) return bad(HIVIS_ERR_ARG, "struct_size mismatch");
-    if (cfg->dtype != HIVIS_F32 && cfg->dtype != HIVIS_BF16) return bad(HIVIS_ERR_DTYPE, "unknown dtype");
+    if (cfg->dtype != HIVIS_F32 && cfg->dtype != HIVIS_BF16 && cfg->dtype != HIVIS_BF16_KV4) return bad(HIVIS_ERR_DTYPE, "unknown dtype");
     if (cfg->d < 8 || cfg->d % 8) return bad(HIVIS_ERR_SHAPE, "d must be a positive multiple of 8");
     if (cfg->head_dim != 64 && cfg->head_dim != 128) return bad(HIVIS_ERR_SHAPE, "head_dim must be 64 or 128");
     if (cfg->n_kv_heads < 1 || cfg->n_q_heads < 1 || cfg->n_q_heads % cfg->n_kv_heads)
@@ -262,8 +264,10 @@ int hivis_init(hivis_ctx** out, const hivis_config* cfg, const hivis_weights* w,
     hivis_ctx* c = new (std::nothrow) hivis_ctx();
     if (!c) return bad(HIVIS_ERR_NOMEM, "host allocation failed");
     c->cfg = *cfg;
-    c->dtype = cfg->dtype;
-    c->esize = cfg->dtype == HIVIS_BF16 ? 2 : 4;
+    const bool kv4 = cfg->dtype == HIVIS_BF16_KV4;
+    c->dtype = kv4 ? HIVIS_BF16 : cfg->dtype;
+    c->esize = c->dtype == HIVIS_BF16 ? 2 : 4;
+    c->kv4 = Kv4View{nullptr, cfg->max_batch, cfg->n_kv_heads, (cfg->max_len + 31) / 32 * 32, cfg->head_dim};
     c->qw = cfg->n_q_heads * cfg->head_dim;
     c->kvw = cfg->n_kv_heads * cfg->head_dim;
     c->qkvw = c->qw + 2 * c->kvw;
@@ -318,13 +322,13 @@ int hivis_init(hivis_ctx** out, const hivis_config* cfg, const hivis_weights* w,
     const long long tiles1 = (d + 127) / 128 * 4;       // partial sums of squares: one per 32 rows, whole 128-row tiles
     static_assert(HIVIS_MMA_TILE_ROWS == 32, "partial sums of squares");
 
-    char *embed, *lm, *fc, *n1, *wqkv, *bqkv = nullptr, *wo, *n2, *wgu, *wdown, *rp = nullptr, *Kc, *Vc;
+    char *embed, *lm, *fc, *n1, *wqkv, *bqkv = nullptr, *wo, *n2, *wgu, *wdown, *rp = nullptr, *Kc = nullptr, *Vc = nullptr;
     bool ok = dalloc(c, &embed, V * d * es) && dalloc(c, &lm, V * d * es) && dalloc(c, &fc, 2 * d * d * es) &&
               dalloc(c, &n1, d * es) && dalloc(c, &wqkv, (long long)c->qkvw * d * es) &&
               dalloc(c, &wo, d * c->qw * es) && dalloc(c, &n2, d * es) && dalloc(c, &wgu, 2 * F * d * es) &&
               dalloc(c, &wdown, d * F * es) &&
-              dalloc(c, &Kc, MB * c->kvw * (long long)cfg->max_len * es) &&
-              dalloc(c, &Vc, MB * c->kvw * (long long)cfg->max_len * es);
+              (kv4 ? dalloc(c, &c->kv4.data, (size_t)kv4_bytes(c->kv4)) && dalloc(c, &c->kv4_q, R * c->qw)
+                   : dalloc(c, &Kc, MB * c->kvw * (long long)cfg->max_len * es) && dalloc(c, &Vc, MB * c->kvw * (long long)cfg->max_len * es));
     if (ok && nb) ok = dalloc(c, &bqkv, (long long)c->qkvw * es);
     if (ok && w->resid_proj) ok = dalloc(c, &rp, d * d * es);
     ok = ok && dalloc(c, &c->inv_freq, cfg->head_dim / 2) && dalloc(c, &c->kv_len, MB) &&
@@ -410,8 +414,12 @@ int hivis_init(hivis_ctx** out, const hivis_config* cfg, const hivis_weights* w,
         CK(c, cudaMemsetAsync(c->attn_h, 0, R * c->qw * sizeof(bf16), st));
         CK(c, cudaMemsetAsync(c->xm, 0, R * d * sizeof(bf16), st));
         CK(c, cudaMemsetAsync(c->act_h, 0, R * F * sizeof(bf16), st));
-        CK(c, cudaMemsetAsync(c->Kc, 0, MB * c->kvw * (long long)cfg->max_len * es, st));
-        CK(c, cudaMemsetAsync(c->Vc, 0, MB * c->kvw * (long long)cfg->max_len * es, st));
+        if (kv4) {
+            CK(c, cudaMemsetAsync(c->kv4.data, 0, (size_t)kv4_bytes(c->kv4), st));
+        } else {
+            CK(c, cudaMemsetAsync(c->Kc, 0, MB * c->kvw * (long long)cfg->max_len * es, st));
+            CK(c, cudaMemsetAsync(c->Vc, 0, MB * c->kvw * (long long)cfg->max_len * es, st));
+        }
         return HIVIS_OK;
     };
     rc = run();
@@ -421,6 +429,7 @@ int hivis_init(hivis_ctx** out, const hivis_config* cfg, const hivis_weights* w,
         delete c;
         return rc;
     }
+    if (kv4) c->chain_ok = false;                       // (the one-sequence chain kernel reads 16- or 32-bit rows)
     if (c->chain_ok) {
         ChainArgs ca;
         fill_chain_args(c, &ca);
@@ -435,14 +444,15 @@ int hivis_init(hivis_ctx** out, const hivis_config* cfg, const hivis_weights* w,
                    dalloc(c, &c->tile_ctr, c->tc_tiles) &&
                    dalloc(c, &c->phase_t, (size_t)HIVIS_MAX_K * HIVIS_PHASE_EVENTS * c->num_sms);
         if (ok2) ok2 = cudaMemsetAsync(c->tile_ctr, 0, c->tc_tiles * sizeof(int), st) == cudaSuccess;
+        // (a cache held in 4 bits has its own attention: the launches leave that phase out, and the maps of the caches are of any buffer)
+        const void *mapK = kv4 ? (const void*)c->attn_h : c->Kc, *mapV = kv4 ? (const void*)c->attn_h : c->Vc;
+        const long long map_rows = kv4 ? 32 : MB * (long long)cfg->n_kv_heads * cfg->max_len;
         if (ok2)
             ok2 = tc_build_maps(&c->tc_maps, ca.ph, cfg->d, c->qw, cfg->ffn, c->feat_h, c->xq, c->attn_h, c->xm, c->act_h,
-                                c->xe_h, c->Kc, c->Vc, MB * (long long)cfg->n_kv_heads * cfg->max_len,
-                                cfg->head_dim, TC_OP_ROWS) == cudaSuccess;
+                                c->xe_h, mapK, mapV, map_rows, cfg->head_dim, TC_OP_ROWS) == cudaSuccess;
         if (ok2 && R > TC_OP_ROWS)
             ok2 = tc_build_maps(&c->tc_maps_wide, ca.ph, cfg->d, c->qw, cfg->ffn, c->feat_h, c->xq, c->attn_h, c->xm, c->act_h,
-                                c->xe_h, c->Kc, c->Vc, MB * (long long)cfg->n_kv_heads * cfg->max_len,
-                                cfg->head_dim, HIVIS_MAX_BATCH) == cudaSuccess;
+                                c->xe_h, mapK, mapV, map_rows, cfg->head_dim, HIVIS_MAX_BATCH) == cudaSuccess;
         if (!ok2) cudaGetLastError();
         c->tc_ok = ok2;
     }
@@ -623,7 +633,7 @@ static void fill_tc_args(hivis_ctx* c, TcArgs* out, int B, int k, int lo, const 
     TcArgs& a = *out;
     memset(&a, 0, sizeof(a));
     for (int p = 0; p < PH_COUNT; ++p) a.ph[p] = ca.ph[p];
-    a.k = k; a.B = B; a.lo = lo;
+    a.k = a.k_rows = k; a.B = B; a.lo = lo;
     a.d = g.d; a.qw = c->qw; a.kvw = c->kvw; a.F = g.ffn; a.V = g.vocab; a.Hq = g.n_q_heads; a.Hkv = g.n_kv_heads;
     a.dh = g.head_dim; a.max_len = g.max_len; a.eps = g.rms_eps; a.scale = 1.0f / sqrtf((float)g.head_dim);
     a.norm1 = (const bf16*)c->norm1; a.norm2 = (const bf16*)c->norm2; a.bqkv = (const bf16*)c->bqkv;
@@ -720,7 +730,7 @@ int hivis_prefill(hivis_ctx* c, int B, const int* seq_slots_host, const int32_t*
         a.norm1 = (const bf16*)c->norm1; a.rho0 = rho0; a.rho0_h = raw_rho ? (const bf16*)resid0 : nullptr;
         a.xe = c->pf_xe; a.xq = c->pf_xq; a.ssq = c->pf_ssq; a.rope = c->pf_rope;
         a.slot_of = c->slot_of; a.row_of = c->row_of; a.inv_freq = c->inv_freq;
-        a.Kc = (bf16*)c->Kc; a.Vc = (bf16*)c->Vc;
+        a.Kc = (bf16*)c->Kc; a.Vc = (bf16*)c->Vc; a.kv4 = c->kv4;
         a.wait_cycles = c->wait_cycles; a.error_flag = c->error_flag;
         CK(c, launch_prefill_tc(a, st));
         c->launches += 3;
@@ -736,11 +746,37 @@ int hivis_prefill(hivis_ctx* c, int B, const int* seq_slots_host, const int32_t*
             if (rc) return rc;
             rc = run_qkv(c, mma, 0, P, c->qw, 2 * c->kvw, c->qkv, st);   // K and V rows only
             if (rc) return rc;
-            CKL(c, launch_kv_append(c->dtype, c->qkv, P, c->slot_of + j0, c->row_of + j0, c->inv_freq,
-                                    c->cfg.n_kv_heads, c->cfg.head_dim, c->cfg.max_len, c->Kc, c->Vc, st));
+            if (c->kv4.data)
+                CKL(c, launch_kv4_put(c->kv4, P, c->qkv, 2 * c->kvw, 0, c->slot_of + j0, c->row_of + j0, 0, c->inv_freq, 0, nullptr, st));
+            else
+                CKL(c, launch_kv_append(c->dtype, c->qkv, P, c->slot_of + j0, c->row_of + j0, c->inv_freq,
+                                        c->cfg.n_kv_heads, c->cfg.head_dim, c->cfg.max_len, c->Kc, c->Vc, st));
         }
     }
     prefill_done(c, sl, new_upper, start_pos_host != nullptr);
+    return HIVIS_OK;
+}
+
+// what every draft leaves in the host's mirrors
+static void draft_done(hivis_ctx* c, const SlotList& sl, int k, bool mma) {
+    for (int b = 0; b < sl.n; ++b) {
+        const int s = sl.slot[b];
+        c->kv_upper[s] += k;
+        c->pending[s] = false;
+        c->last_k[s] = k;
+    }
+    c->tap_B = sl.n;
+    c->tap_mma = mma;
+}
+
+// The attention of draft step s over a cache held in 4 bits: the step's keys and values are quantised into it, then the rotated
+// queries attend.
+static int kv4_attention(hivis_ctx* c, const SlotList& sl, int s, int lo, cudaStream_t st) {
+    const hivis_config& g = c->cfg;
+    const int G = g.n_q_heads / g.n_kv_heads;
+    CKP(c, CLS_ATTN, st, launch_kv4_put(c->kv4, sl.n, c->qkv, c->qkvw, c->qw, c->d_slots, c->d_pos0, s, c->inv_freq, G, c->kv4_q, st));
+    CKP(c, CLS_ATTN, st, launch_kv4_draft_attention(c->kv4, sl, c->d_pos0, s, G, c->kv4_q, 1.0f / sqrtf((float)g.head_dim), c->attn, c->attn_h,
+                                                    lo, c->num_sms, st));
     return HIVIS_OK;
 }
 
@@ -822,6 +858,40 @@ static int draft_impl(hivis_ctx* c, int B, const int* seq_slots_host, int k, con
         a.out_ids = out_ids;
         a.gumbel_u = uniforms;
         a.inv_t = inv_t;
+        if (c->kv4.data) {
+            // one step after the other, each in two parts around the attention over the 4-bit cache
+            const TcMaps& maps = B <= TC_OP_ROWS ? c->tc_maps : c->tc_maps_wide;
+            const u64 G = (u64)c->num_sms;
+            u64 skew = a.bar_off;                                    // (of the first launch)
+            c->debug_skew = false;
+            a.k = 1;
+            a.out_ids = nullptr;
+            a.forced = nullptr;
+            a.n_resid = 1;
+            for (int s = 0; s < k; ++s) {
+                if (s > 0)
+                    CKP(c, CLS_OTHER, st, launch_step_operands_tc(B, k, s, d, c->keys, c->key_stride, forced_ids, (const bf16*)c->embed, V,
+                                                                  c->xe_h, c->id_flag, st));
+                const long long row = resid ? (s < n_resid - 1 ? s : n_resid - 1) : 0;
+                a.rho = resid && !raw_rho ? c->rho + row * d : nullptr;
+                a.rho_h = raw_rho ? (const bf16*)resid + row * d : nullptr;
+                a.keys = c->keys + s;
+                a.logits_out = out_logits ? out_logits + (long long)s * V : nullptr;
+                a.gumbel_u = uniforms ? uniforms + (long long)s * V : nullptr;
+                a.seq_first = 1; a.seq_last = 2;                     // fusion FC, QKV (the operands are gathered already)
+                a.bar_off = skew - G;                                // as if the gather had been arrived on
+                skew = 0;
+                CKP(c, CLS_CHAIN, st, launch_tc_chain(maps, a, c->num_sms, st));
+                rc = kv4_attention(c, sl, s, lo, st);
+                if (rc) return rc;
+                a.seq_first = 4; a.seq_last = 7;                     // O, gate/up, down, LM head
+                a.bar_off = 0 - G * 4;                               // as if gather .. attention had been arrived on
+                CKP(c, CLS_CHAIN, st, launch_tc_chain(maps, a, c->num_sms, st));
+            }
+            CKP(c, CLS_OTHER, st, launch_draft_finish(B, k, c->keys, c->key_stride, out_ids, st));
+            draft_done(c, sl, k, true);
+            return HIVIS_OK;
+        }
         if (c->opt_phase_times) {
             CK(c, cudaMemsetAsync(c->phase_t, 0, (size_t)k * HIVIS_PHASE_EVENTS * c->num_sms * sizeof(u64), st));
             a.phase_t = c->phase_t;
@@ -829,14 +899,7 @@ static int draft_impl(hivis_ctx* c, int B, const int* seq_slots_host, int k, con
         }
         c->debug_skew = false;
         CKP(c, CLS_CHAIN, st, launch_tc_chain(B <= TC_OP_ROWS ? c->tc_maps : c->tc_maps_wide, a, c->num_sms, st));
-        for (int b = 0; b < B; ++b) {
-            const int s = sl.slot[b];
-            c->kv_upper[s] += k;
-            c->pending[s] = false;
-            c->last_k[s] = k;
-        }
-        c->tap_B = B;
-        c->tap_mma = true;
+        draft_done(c, sl, k, true);
         return HIVIS_OK;
     }
     CKP(c, CLS_OTHER, st, launch_draft_setup(sl, k, d, c->d_slots, c->d_pos0, c->kv_len, c->pend_feat, c->pend_id, c->feat,
@@ -865,7 +928,10 @@ static int draft_impl(hivis_ctx* c, int B, const int* seq_slots_host, int k, con
             if (rc) return rc;
         }
         // ---- RoPE, KV append, attention over the text-only cache
-        {
+        if (c->kv4.data) {
+            rc = kv4_attention(c, sl, s, 0, st);
+            if (rc) return rc;
+        } else {
             AttnArgs a;
             memset(&a, 0, sizeof(a));
             a.qkv = c->qkv; a.ld = c->qkvw; a.Kc = c->Kc; a.Vc = c->Vc; a.slots = c->d_slots; a.pos0 = c->d_pos0;
@@ -883,14 +949,7 @@ static int draft_impl(hivis_ctx* c, int B, const int* seq_slots_host, int k, con
         }
     }
     CKP(c, CLS_OTHER, st, launch_draft_finish(B, k, c->keys, c->key_stride, out_ids, st));
-    for (int b = 0; b < B; ++b) {
-        const int s = sl.slot[b];
-        c->kv_upper[s] += k;
-        c->pending[s] = false;
-        c->last_k[s] = k;
-    }
-    c->tap_B = B;
-    c->tap_mma = mma;
+    draft_done(c, sl, k, mma);
     return HIVIS_OK;
 }
 
@@ -981,6 +1040,7 @@ int hivis_draft_tree(hivis_ctx* c, int slot, int topk, int depth, int keep, cons
     if (depth < 1 || depth > c->cfg.max_k) return fail(c, HIVIS_ERR_CAPACITY, "depth=%d outside [1,%d]", depth, c->cfg.max_k);
     if (keep < 1 || keep > HIVIS_TREE_MAX_KEEP) return fail(c, HIVIS_ERR_CAPACITY, "keep=%d outside [1,%d]", keep, HIVIS_TREE_MAX_KEEP);
     if (resid && (n_resid < 1 || n_resid > HIVIS_MAX_K)) return fail(c, HIVIS_ERR_ARG, "n_resid=%d outside [1,%d]", n_resid, HIVIS_MAX_K);
+    if (c->kv4.data) return fail(c, HIVIS_ERR_SHAPE, "draft trees need a 16- or 32-bit cache: this context holds it in 4 bits");
     if (!c->pending[slot]) return fail(c, HIVIS_ERR_STATE, "slot %d has no pending pair", slot);
     const int tree_rows = 1 + (depth - 1) * topk;
     if (c->kv_upper[slot] + tree_rows > c->cfg.max_len)
@@ -1146,6 +1206,10 @@ int hivis_read_kv(hivis_ctx* c, int slot, int row0, int n, float* out_k, float* 
     if (slot < 0 || slot >= c->cfg.max_batch) return fail(c, HIVIS_ERR_ARG, "slot %d out of range", slot);
     if (!out_k || !out_v || misaligned(out_k) || misaligned(out_v)) return fail(c, HIVIS_ERR_ARG, "bad output pointer");
     if (row0 < 0 || n < 0 || row0 + n > c->cfg.max_len) return fail(c, HIVIS_ERR_CAPACITY, "rows [%d,%d) outside the cache", row0, row0 + n);
+    if (c->kv4.data) {
+        CKL(c, launch_kv4_read_slot(c->kv4, slot, row0, n, out_k, out_v, (cudaStream_t)stream));
+        return HIVIS_OK;
+    }
     CKL(c, launch_read_kv(c->dtype, c->Kc, c->Vc, slot, row0, n, c->cfg.n_kv_heads, c->cfg.head_dim,
                           c->cfg.max_len, out_k, out_v, (cudaStream_t)stream));
     return HIVIS_OK;

@@ -161,6 +161,28 @@ struct CuSeqlens {
 };
 
 // ---------------------------------------------------------------------------------------------
+// A cache held in 4 bits (kv4.cuh, kernels_kv4.cu), as the contexts of dtype HIVIS_BF16_KV4 use it.
+// ---------------------------------------------------------------------------------------------
+struct Kv4View {
+    unsigned char* data;       // nullptr: the cache is not held in 4 bits
+    int n_slots, Hkv, max_len, dh;
+};
+long long kv4_bytes(const Kv4View& c);
+// One new row for each of n rows of `kv` ([n][ld], fp32, the keys before the rotary embedding at column k_col, the values behind
+// them): rotated at its cache row, rounded to bf16 and quantised into slot slots[j], row rows[j] + row_add (a negative row: left
+// out).  q_out (nullable, [n][G * Hkv * dh]): the queries at column 0, rotated too.
+cudaError_t launch_kv4_put(const Kv4View& c, int n, const float* kv, int ld, int k_col, const int* slots, const int* rows, int row_add,
+                           const double* inv_freq, int G, float* q_out, cudaStream_t st);
+// Decode attention of a draft step: query b (fp32, rotated, [n][G * Hkv * dh]) over the first pos0[b] + step + 1 rows of its slot;
+// results in fp32 and in bf16 as in AttnArgs.
+cudaError_t launch_kv4_draft_attention(const Kv4View& c, const SlotList& sl, const int* pos0, int step, int G, const float* q, float scale,
+                                       float* attn, bf16* attn_h, int lo_rows, int num_sms, cudaStream_t st);
+cudaError_t launch_kv4_read_slot(const Kv4View& c, int slot, int row0, int n, float* out_k, float* out_v, cudaStream_t st);
+// embedding rows of the tokens of draft step s > 0 (the argmax keys of the step before, or forced [B][k])
+cudaError_t launch_step_operands_tc(int B, int k, int s, int d, const u64* keys, int key_stride, const int32_t* forced, const bf16* embed,
+                                    int vocab, bf16* xe_h, int* id_flag, cudaStream_t st);
+
+// ---------------------------------------------------------------------------------------------
 // Tensor-core chain kernel (bf16 weights, 1..64 sequences): all k steps in one cooperative launch,
 // weights streamed by TMA into a shared-memory ring, tcgen05.mma with the weights as the M operand
 // (128 rows) and the batch as N (32 or 64 columns), accumulators in tensor memory.
@@ -177,6 +199,7 @@ struct TcMaps {
 struct TcArgs {
     ChainPhase ph[PH_COUNT];
     int k, B;
+    int k_rows;                // rows per sequence of logits_out and gumbel_u: the draft's k (a launch may run one of its steps)
     int lo;                    // > 0: operand rows [lo, lo + B) carry the bf16 rounding remainders of rows [0, B)
     int d, qw, kvw, F, V, Hq, Hkv, dh, max_len;
     float eps, scale;
@@ -250,6 +273,7 @@ struct PrefillTcArgs {
     const int *slot_of, *row_of;
     const double* inv_freq;
     bf16 *Kc, *Vc;
+    Kv4View kv4;               // where the rows go if the cache is held in 4 bits
     long long wait_cycles;
     int* error_flag;
 };

@@ -1,10 +1,11 @@
-// The 4-bit key/value cache: rows go in (quantised), come out (as fp32 values), and are attended over.  No call needs a context
-// or a workspace.  kv4.cuh has the format.
+// The 4-bit key/value cache: rows go in (quantised), come out (as fp32 values), and are attended over, for callers with a cache of
+// their own (no context or workspace) and for the drafter contexts that keep theirs so.  kv4.cuh has the format.
 #include <cstdio>
 #include <cstring>
 
 #include <cooperative_groups.h>
 
+#include "attn_body.cuh"
 #include "kv4.cuh"
 
 namespace cg = cooperative_groups;
@@ -15,7 +16,8 @@ struct Kv4RowsArgs {
     SlotList sl;
     CuSeqlens cu;              // packed rows: sequence b owns [cu.v[b], cu.v[b + 1])
     CuSeqlens pairs;           // append: first pair of rows of each sequence: half its rows and one, whichever way its start is aligned
-    const int* start;          // [B] cache row of each sequence's first packed row
+    const int* start;          // [B] cache row of each sequence's first packed row; nullptr: start_host for all
+    int start_host;
     const void *k, *v;         // packed rows [.][ld]
     long long ld;
     float *out_k, *out_v;      // read: [.][Hkv * dh]
@@ -156,7 +158,7 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ K
         live[u] = j < total;
         if (!live[u]) break;
         while (j >= a.cu.v[b + 1]) ++b;
-        const int start = a.start[b];
+        const int start = a.start ? a.start[b] : a.start_host;
         live[u] = start >= 0 && start < a.c.max_len && j - a.cu.v[b] < a.c.max_len - start;
         if (!live[u]) continue;
         const int row = start + (j - a.cu.v[b]), r = row % KV4_TILE;
@@ -184,6 +186,63 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ K
         *(float4*)(a.out_v + o) = make_float4(value(vw[u], 0, p[u][2], p[u][3]), value(vw[u], 1, p[u][2], p[u][3]),
                                               value(vw[u], 2, p[u][2], p[u][3]), value(vw[u], 3, p[u][2], p[u][3]));
     }
+}
+
+// ------------------------------------------------------------------------------------------------ rows of a drafter context
+// A CTA has one KV head of one row: its first warp rotates and quantises the row (half its lanes: a row alone has no partner), the
+// others rotate the head group's queries.  The angles are made once per CTA (fp64, see rope_cs).
+template <int DH>
+__global__ void __launch_bounds__(128) kv4_put_kernel(Kv4View c, const float* kv, int ld, int k_col, const int* slots, const int* rows,
+                                                      int row_add, const double* inv_freq, int G, float* q_out) {
+    constexpr int LR = DH / 8, HALF = DH / 2;
+    __shared__ float2 s_cs[HALF];
+    pdl_wait();
+    pdl_trigger();
+    const int h = blockIdx.x, j = blockIdx.y, row = rows[j];
+    if (row < 0 || row + row_add >= c.max_len) return;
+    if (threadIdx.x < HALF) {
+        float cs, sn;
+        rope_cs(row + row_add, inv_freq[threadIdx.x], cs, sn);
+        s_cs[threadIdx.x] = make_float2(cs, sn);
+    }
+    __syncthreads();
+    const float* in = kv + (long long)j * ld;
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x, l = lane % LR;
+        const bool live = lane < LR;
+        const float* k = in + k_col + h * DH;
+        const float* v = k + (long long)c.Hkv * DH;
+        float x[8], y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = 8 * l + i;
+            const float own = k[e], other = k[e ^ HALF];
+            const float2 t = s_cs[e % HALF];
+            x[i] = __bfloat162float(__float2bfloat16_rn(e < HALF ? own * t.x - other * t.y : own * t.x + other * t.y));
+            y[i] = __bfloat162float(__float2bfloat16_rn(v[e]));
+        }
+        Kv4Place p;
+        p.h = h; p.slot = slots[j]; p.w = l >> 2; p.c = l & 3; p.row = row + row_add; p.packed = 0;
+        kv4_store_row<DH>(c, p, live, x, y);
+    } else if (q_out) {
+        for (int i = threadIdx.x - 32; i < G * HALF; i += 96) {
+            const int g = i / HALF, e = i % HALF, at = (h * G + g) * DH + e;
+            const float2 t = s_cs[e];
+            const float lo = in[at], hi = in[at + HALF];
+            float* out = q_out + (long long)j * G * c.Hkv * DH + at;
+            out[0] = lo * t.x - hi * t.y;
+            out[HALF] = hi * t.x + lo * t.y;
+        }
+    }
+}
+
+long long kv4_bytes(const Kv4View& c) { return (long long)c.n_slots * c.Hkv * (c.max_len / KV4_TILE) * kv4_tile_bytes(c.dh); }
+
+cudaError_t launch_kv4_put(const Kv4View& c, int n, const float* kv, int ld, int k_col, const int* slots, const int* rows, int row_add,
+                           const double* inv_freq, int G, float* q_out, cudaStream_t st) {
+    const dim3 grid((unsigned)c.Hkv, (unsigned)n);
+    if (c.dh == 128) return launch_pdl(kv4_put_kernel<128>, grid, dim3(128), 0, st, c, kv, ld, k_col, slots, rows, row_add, inv_freq, G, q_out);
+    return launch_pdl(kv4_put_kernel<64>, grid, dim3(128), 0, st, c, kv, ld, k_col, slots, rows, row_add, inv_freq, G, q_out);
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -219,7 +278,15 @@ struct Kv4AttnArgs {
     void* out;                 // [B * n_q][out_ld]
     long long out_ld;
     int n_blocks;              // blocks of 8 NT columns
+    int rows_add;              // added to rows[b]
+    bf16* out_h;               // drafts: bf16 copy of out, its rounding remainders lo_rows rows further on if that is not 0
+    int lo_rows;
 };
+
+// Element types of a draft step: queries in fp32, rounded to fp16 like the probabilities; results in fp32 and in bf16.
+struct Kv4DraftIo {};
+template <typename T> struct Kv4Io { typedef T Query; static constexpr bool SPLIT = sizeof(T) == 4; };
+template <> struct Kv4Io<Kv4DraftIo> { typedef float Query; static constexpr bool SPLIT = false; };
 
 __device__ __forceinline__ uint32_t kv4_saddr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ bool kv4_wait(uint32_t bar, uint32_t parity) {
@@ -308,6 +375,15 @@ __device__ __forceinline__ void kv4_put(const Kv4AttnArgs& a, int b, int h, int 
     if constexpr (sizeof(T) == 2) {
         const __nv_bfloat162 u = __floats2bfloat162_rn(o.x * inv, o.y * inv), v = __floats2bfloat162_rn(o.z * inv, o.w * inv);
         *(uint2*)((bf16*)a.out + at) = make_uint2(*(const unsigned*)&u, *(const unsigned*)&v);
+    } else if constexpr (sizeof(T) == 1) {
+        const float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+        *(float4*)((float*)a.out + at) = make_float4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bf16 hi = __float2bfloat16_rn(x[i]);
+            a.out_h[at + i] = hi;
+            if (a.lo_rows > 0) a.out_h[at + a.lo_rows * a.out_ld + i] = __float2bfloat16_rn(x[i] - __bfloat162float(hi));
+        }
     } else {
         *(float4*)((float*)a.out + at) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     }
@@ -606,8 +682,8 @@ __device__ __forceinline__ void kv4_sum_parts(const float (&sum)[Q], int c, uint
 
 // The queries as B fragments: column lane / 4 of every block of eight, channels 32 w + 8 (lane % 4) + 0..7 of every group.
 template <int DH, int NT, typename T>
-__device__ __forceinline__ void kv4_load_queries(Kv4Warp<DH, NT, sizeof(T) == 4>& st, const Kv4AttnArgs& a, int b, int h, int j0, int lane) {
-    constexpr bool SPLIT = sizeof(T) == 4;
+__device__ __forceinline__ void kv4_load_queries(Kv4Warp<DH, NT, Kv4Io<T>::SPLIT>& st, const Kv4AttnArgs& a, int b, int h, int j0, int lane) {
+    constexpr bool SPLIT = Kv4Io<T>::SPLIT;
     constexpr int Q = DH / 32;
     constexpr float UNIT = SPLIT ? 1.f : 0x1p-24f;                // what a code of 1 is to the tensor core
     const int g = lane >> 2, c = lane & 3;
@@ -619,7 +695,7 @@ __device__ __forceinline__ void kv4_load_queries(Kv4Warp<DH, NT, sizeof(T) == 4>
         for (int w = 0; w < Q; ++w) {
             if (j < a.ncol) {
                 const long long at = (long long)(b * a.n_q + j / a.G) * a.q_ld + (h * a.G + j % a.G) * DH + 32 * w + 8 * c;
-                kv4_load8<T>(a.q, at, x[w]);
+                kv4_load8<typename Kv4Io<T>::Query>(a.q, at, x[w]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[w][i] = 0.f;
@@ -685,7 +761,7 @@ __host__ __device__ constexpr size_t kv4_smem(int warps) {
 
 template <int DH, int NT, typename T, int U, int WARPS, int CTAS>
 __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid_constant__ Kv4AttnArgs a) {
-    constexpr bool SPLIT = sizeof(T) == 4;
+    constexpr bool SPLIT = Kv4Io<T>::SPLIT;
     constexpr int Q = DH / 32, NB = 8 * NT, LDO = DH + 4, TB = kv4_tile_bytes(DH), ROWS = KV4_TILE * U, STAGES = KV4_RING / U;
     constexpr float UNIT = SPLIT ? 1.f : 0x1p-24f;
     extern __shared__ __align__(128) unsigned char kv4_sm[];
@@ -704,7 +780,7 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
     pdl_wait();
     pdl_trigger();
     Kv4Sight sight;
-    sight.nrows = min(max(a.rows[b], 0), a.c.max_len);
+    sight.nrows = min(max(a.rows[b] + a.rows_add, 0), a.c.max_len);
     sight.n_q = a.n_q; sight.mask_rows = a.mask_rows; sight.mask_words = a.mask_words;
     sight.mask = a.mask ? a.mask + (long long)b * a.n_q * a.mask_words : nullptr;
     const int i_first = j0 / a.G, i_last = (min(j0 + NB, a.ncol) - 1) / a.G;
@@ -889,6 +965,20 @@ static cudaError_t kv4_launch_attn_n(Kv4AttnArgs& a, int dev, int num_sms, cudaS
     }
 }
 
+cudaError_t launch_kv4_draft_attention(const Kv4View& c, const SlotList& sl, const int* pos0, int step, int G, const float* q, float scale,
+                                       float* attn, bf16* attn_h, int lo_rows, int num_sms, cudaStream_t st) {
+    Kv4AttnArgs a;
+    memset(&a, 0, sizeof(a));
+    a.c = c; a.sl = sl; a.rows = pos0; a.rows_add = step + 1;
+    a.q = q; a.n_q = 1; a.G = a.ncol = G; a.Hq = G * c.Hkv; a.q_ld = a.out_ld = (long long)a.Hq * c.dh;
+    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.out = attn; a.out_h = attn_h; a.lo_rows = lo_rows;
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    return c.dh == 128 ? kv4_launch_attn_n<128, Kv4DraftIo>(a, dev, num_sms, st) : kv4_launch_attn_n<64, Kv4DraftIo>(a, dev, num_sms, st);
+}
+
 // ------------------------------------------------------------------------------------------------ C entries
 #define KV4_FAIL(code, ...)                                   \
     do {                                                      \
@@ -950,6 +1040,17 @@ static bool kv4_rows_grid(Kv4RowsArgs* a, int units, int rounds, int items, dim3
     const long long y = (a->c.Hkv + (1 << a->heads_log2) - 1) >> a->heads_log2;
     *grid = dim3((unsigned)(((long long)items + per - 1) / per), (unsigned)y);
     return y <= 65535;
+}
+
+cudaError_t launch_kv4_read_slot(const Kv4View& c, int slot, int row0, int n, float* out_k, float* out_v, cudaStream_t st) {
+    if (n <= 0) return cudaSuccess;
+    Kv4RowsArgs a;
+    memset(&a, 0, sizeof(a));
+    a.c = c; a.sl.n = 1; a.sl.slot[0] = slot; a.cu.v[1] = n; a.start_host = row0;
+    a.out_k = out_k; a.out_v = out_v;
+    dim3 grid;
+    if (!kv4_rows_grid(&a, 256 / (c.dh / 4), KV4_READ_ROWS, n, &grid)) return cudaErrorInvalidValue;
+    return c.dh == 128 ? launch_pdl(kv4_read_kernel<128>, grid, dim3(256), 0, st, a) : launch_pdl(kv4_read_kernel<64>, grid, dim3(256), 0, st, a);
 }
 
 static int kv4_cuda(const char* who, cudaError_t e) {

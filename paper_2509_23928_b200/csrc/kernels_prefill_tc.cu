@@ -30,6 +30,7 @@
 #include <cuda.h>
 
 #include "attn_body.cuh"
+#include "kv4.cuh"
 
 #define PF_THREADS 192
 #define PF_MAX_STAGES 9
@@ -175,6 +176,7 @@ struct PfParams {
     const int *slot_of, *row_of;
     const float2* rope;        // [pairs][dh / 2] (cos, sin) at the pair's position
     bf16 *Kc, *Vc;
+    Kv4View kv4;
 };
 
 __device__ __forceinline__ unsigned pf_pack(float x0, float x1) {
@@ -251,6 +253,7 @@ __device__ __forceinline__ PfPair pf_pair(const PfParams& P, int pair, bool live
     }
     return p;
 }
+template <bool KV4>
 __device__ __forceinline__ void pf_out_kv(const PfParams& P, uint32_t tacc, const PfPair& pp, int c, int n0, int pair) {
     const int half = P.dh >> 1, g = n0 + c;                 // row of the stacked [K ; V] projection
     const bool isK = g < P.kvw;
@@ -259,7 +262,6 @@ __device__ __forceinline__ void pf_out_kv(const PfParams& P, uint32_t tacc, cons
     pf_ld32(tacc + c, lo);
     pf_ld32(tacc + c + half, hi);
     if (pp.crow < 0) return;
-    bf16* dst = (isK ? P.Kc : P.Vc) + ((pp.slot_base + head) * P.max_len + pp.crow) * P.dh + e0;
     // (one rounding for scale and bias, as in the builds of 16 pairs per pass)
     if (P.bias) {
         pf_load32(P.bias + g, x);
@@ -285,10 +287,23 @@ __device__ __forceinline__ void pf_out_kv(const PfParams& P, uint32_t tacc, cons
             hi[2 * q + 1] = fmaf(u1, t.z, __fmul_rn(l1, t.w));
         }
     }
-    pf_store32(dst, lo);
-    pf_store32(dst + half, hi);
+    if constexpr (KV4) {
+        // the two runs of 32 channels are groups of the 4-bit format; it takes them as a 16-bit cache would hold them
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            lo[i] = __bfloat162float(__float2bfloat16_rn(lo[i]));
+            hi[i] = __bfloat162float(__float2bfloat16_rn(hi[i]));
+        }
+        unsigned char* tile = kv4_tile(P.kv4, (int)(pp.slot_base / P.Hkv), head, pp.crow);
+        kv4_store32(tile, P.dh, isK ? 0 : 1, pp.crow % KV4_TILE, e0 / KV4_GROUP, lo);
+        kv4_store32(tile, P.dh, isK ? 0 : 1, pp.crow % KV4_TILE, (e0 + half) / KV4_GROUP, hi);
+    } else {
+        bf16* dst = (isK ? P.Kc : P.Vc) + ((pp.slot_base + head) * P.max_len + pp.crow) * P.dh + e0;
+        pf_store32(dst, lo);
+        pf_store32(dst + half, hi);
+    }
 }
-template <int EPI, int BN>   // EPI 0: fusion FC, 1: K and V
+template <int EPI, int BN>   // EPI 0: fusion FC, 1: K and V, 2: K and V into a cache held in 4 bits
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PF_THREADS, 1) prefill_tc_kernel(const __grid_constant__ PfParams P) {
     constexpr int B_BYTES = (BN / 2) * PF_BK * 2;
     constexpr unsigned PF_STAGES = PfRing<BN>::STAGES;
@@ -382,7 +397,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PF_THREADS, 1) prefi
             const int pair = (w / P.n_tiles) * PF_TM + (int)rank * 128 + quarter * 32 + lane, n0 = (w % P.n_tiles) * BN;
             const bool live = pair < P.n_pairs;
             PfPair pp;
-            if (EPI == 1) pp = pf_pair(P, pair, live);
+            if (EPI != 0) pp = pf_pair(P, pair, live);
             bool ok = true;
             if (lane == 0) ok = pf_wait(pf_saddr(&ctl->tfull[acc]), use & 1u, ctl, P.wait_cycles, P.error_flag);
             ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
@@ -398,7 +413,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PF_THREADS, 1) prefi
                 for (int q = 0; q < BN / 64; ++q) {
                     const int c = P.dh == 64 ? 64 * q : 128 * (q >> 1) + 32 * (q & 1);
                     if (n0 + c >= P.rows) break;                    // (uniform)
-                    pf_out_kv(P, tacc, pp, c, n0, pair);
+                    pf_out_kv<EPI == 2>(P, tacc, pp, c, n0, pair);
                 }
             }
             pf_fence_before();
@@ -523,5 +538,6 @@ cudaError_t launch_prefill_tc(const PrefillTcArgs& a, cudaStream_t st) {
     Q.ssq_in = a.ssq; Q.ssq_tiles = (d + 127) / 128; Q.pair_cap = a.pair_cap; Q.d = d; Q.eps = a.eps;
     Q.bias = a.bkv; Q.kvw = a.kvw; Q.Hkv = a.Hkv; Q.dh = a.dh; Q.max_len = a.max_len;
     Q.slot_of = a.slot_of; Q.row_of = a.row_of; Q.rope = a.rope; Q.Kc = a.Kc; Q.Vc = a.Vc;
-    return pf_launch<1>(Q, a.wkv, a.num_sms, st);
+    Q.kv4 = a.kv4;
+    return a.kv4.data ? pf_launch<2>(Q, a.wkv, a.num_sms, st) : pf_launch<1>(Q, a.wkv, a.num_sms, st);
 }

@@ -60,6 +60,23 @@ __global__ void __launch_bounds__(512) tc_setup_kernel(SlotList sl, int k, int d
         if (lo) ((uint4*)(feat_h + (long long)(b + lo) * d))[i] = make_uint4(rem[0], rem[1], rem[2], rem[3]);
     }
 }
+// Operands of draft step s > 0 where the steps are launched one by one: the embedding rows of the tokens chosen (or forced) in the
+// step before.  (The layer's output is there already, as the hidden operand.)
+__global__ void __launch_bounds__(512) step_operands_kernel(int k, int s, int d, const u64* keys, int key_stride, const int32_t* forced,
+                                                            const bf16* embed, int vocab, bf16* xe_h, int* id_flag) {
+    pdl_wait();
+    pdl_trigger();
+    const int b = blockIdx.x;
+    const int id = checked_token(forced ? forced[(long long)b * k + s - 1] : key_index(keys[(long long)b * key_stride + s - 1]), vocab, id_flag);
+    const uint4* er = (const uint4*)(embed + (long long)id * d);
+    uint4* xe = (uint4*)(xe_h + (long long)b * d);
+    for (int i = threadIdx.x; i < d / 8; i += blockDim.x) xe[i] = ld_stream(er + i);
+}
+cudaError_t launch_step_operands_tc(int B, int k, int s, int d, const u64* keys, int key_stride, const int32_t* forced, const bf16* embed,
+                                    int vocab, bf16* xe_h, int* id_flag, cudaStream_t st) {
+    return launch_pdl(step_operands_kernel, dim3(B), dim3(512), 0, st, k, s, d, keys, key_stride, forced, embed, vocab, xe_h, id_flag);
+}
+
 cudaError_t launch_tc_setup(const SlotList& sl, int k, int d, int lo, int* d_slots, int* d_pos0, int* kv_len,
                             const float* pend_feat, const int* pend_id, float* feat, bf16* feat_h, int* cur_id,
                             u64* keys, int key_stride, const bf16* embed, int vocab, bf16* xe_h, int* id_flag,

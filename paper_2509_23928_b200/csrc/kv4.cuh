@@ -20,10 +20,6 @@
 
 #include <cuda_fp16.h>
 
-struct Kv4View {
-    unsigned char* data;
-    int n_slots, Hkv, max_len, dh;
-};
 #define KV4_GROUP 32
 #define KV4_TILE 16
 __host__ __device__ __forceinline__ constexpr int kv4_tile_bytes(int dh) { return 20 * dh; }
@@ -106,3 +102,30 @@ __device__ __forceinline__ int kv4_s_at(int dh, int which, int r, int w) {
     return which == 0 ? 16 * dh + r * (dh / 8) + 2 * w : 18 * dh + (r >> 1) * (dh / 4) + 4 * w + 2 * (r & 1);
 }
 __device__ __forceinline__ int kv4_m_at(int dh, int which, int r, int w) { return kv4_s_at(dh, which, r, w) + (which == 0 ? dh / 16 : dh / 8); }
+
+// One lane's 32 values - channels 32 w .. 32 w + 31 of row r, bf16 numbers - into a tile; which: 0 K, 1 V.
+__device__ __forceinline__ void kv4_store32(unsigned char* tile, int dh, int which, int r, int w, const float (&x)[32]) {
+    float lo = x[0], hi = x[0], zero = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        lo = fminf(lo, x[i]);
+        hi = fmaxf(hi, x[i]);
+        zero = fmaf(x[i], 0.f, zero);
+    }
+    const uint32_t params = kv4_params(lo, hi, zero == 0.f);
+    *(uint16_t*)(tile + kv4_s_at(dh, which, r, w)) = (uint16_t)(params >> 16);
+    *(uint16_t*)(tile + kv4_m_at(dh, which, r, w)) = (uint16_t)params;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[8 * c + i];
+        const uint32_t codes = kv4_codes8(y, params);
+        if (which == 0) {
+            *(uint32_t*)(tile + kv4_k_at(dh, r, w, c)) = codes;
+        } else {
+            *(uint16_t*)(tile + kv4_v_at(dh, r, w, 2 * c)) = (uint16_t)codes;
+            *(uint16_t*)(tile + kv4_v_at(dh, r, w, 2 * c + 1)) = (uint16_t)(codes >> 16);
+        }
+    }
+}

@@ -943,7 +943,7 @@ __device__ __forceinline__ void epi_preload(const TcArgs& a, int p, int s, int t
         // the uniform numbers of the row's token, one per sequence (the noise is added in the output stage)
 #pragma unroll
         for (int b = 0; b < 16; ++b)
-            if (b < B) pre.add[b] = __ldg(a.gumbel_u + ((long long)(b0 + b) * a.k + s) * N + row);
+            if (b < B) pre.add[b] = __ldg(a.gumbel_u + ((long long)(b0 + b) * a.k_rows + s) * N + row);
     }
 }
 
@@ -1017,7 +1017,7 @@ __device__ __forceinline__ void epi_output(const TcArgs& a, TcCtl* ctl, int p, i
         for (int b = 0; b < 16; ++b) {
             keys[b] = 0ull;
             if (rok && b < B) {
-                if (a.logits_out) a.logits_out[((long long)(b0 + b) * a.k + s) * a.V + row] = val[b];
+                if (a.logits_out) a.logits_out[((long long)(b0 + b) * a.k_rows + s) * a.V + row] = val[b];
                 keys[b] = pack_key(SMP ? gumbel_perturbed(val[b], a.inv_t, pre.add[b]) : val[b], row);
             }
         }
