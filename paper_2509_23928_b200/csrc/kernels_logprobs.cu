@@ -2,7 +2,7 @@
 //
 // In powers of two, with y_i = log2(e) / T x_i - c: log2 p_i = y_i - log2 Z, Z = sum 2^y, and H = log2 Z - W / Z, W = sum 2^y y, for any
 // c near the largest logit's.  A thread takes c from its first 32 (bf16) or 16 logits and raises it only when later ones are above
-// it by 2^60 - raising by d turns (Z, W) into (Z f, (W - d Z) f), f = 2^-d - so that a logit costs one multiply-add for y, the
+// it by 2^3 (with 2^60 the rounding of y in the largest terms cost a digit: 9.7e-7 of the results) - raising by d turns (Z, W) into (Z f, (W - d Z) f), f = 2^-d - so that a logit costs one multiply-add for y, the
 // exponential, and one operation for each sum.  Threads are joined in a CTA and CTAs, up to 16 to a row, in a cluster, always in
 // the same order, in fp32; the row's results are made of the joined sums in fp64.
 // A CTA whose largest logit is so far from zero that y would lose it (|log2(e) / T x| > 2^28: a row of the type's lowest number, say)
@@ -41,7 +41,7 @@ struct LogprobArgs {
 };
 
 #define LP_FAR 0x1p28f            // |c| is at most this
-#define LP_RISE 60.f              // y beyond which c is raised
+#define LP_RISE 3.f               // y beyond which c is raised: y is rounded to 2^-24 of itself
 
 struct LpSum {
     float c, z, w;
