@@ -77,20 +77,14 @@ __device__ __forceinline__ void kv4_load8(const void* p, long long i, float (&x)
 
 // parameters of the group whose 32 values the four lanes of a quad hold (every lane of the warp takes part)
 __device__ __forceinline__ uint32_t kv4_group_params(const float (&x)[8]) {
-    float lo = x[0], hi = x[0], zero = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        zero = fmaf(x[i], 0.f, zero);                       // NaN once a value is not finite
-    }
+    float lo = kv4_min_nan(kv4_min_nan(kv4_min_nan(x[0], x[1]), kv4_min_nan(x[2], x[3])), kv4_min_nan(kv4_min_nan(x[4], x[5]), kv4_min_nan(x[6], x[7])));
+    float hi = kv4_max_nan(kv4_max_nan(kv4_max_nan(x[0], x[1]), kv4_max_nan(x[2], x[3])), kv4_max_nan(kv4_max_nan(x[4], x[5]), kv4_max_nan(x[6], x[7])));
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        lo = kv4_min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = kv4_max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
-    const unsigned bad = __ballot_sync(0xffffffffu, zero != 0.f);
-    return kv4_params(lo, hi, ((bad >> (threadIdx.x & 28)) & 15u) == 0u);
+    return kv4_params(lo, hi);
 }
 
 // One row's 8 channels of K and of V into the cache.  `live`: the lane has a row; every lane of the warp takes part.

@@ -34,16 +34,16 @@ __device__ __forceinline__ float kv4_scale(uint32_t w) { return __uint_as_float(
 __device__ __forceinline__ float kv4_min(uint32_t w) { return __uint_as_float(w << 16); }
 
 // Parameters of a group whose smallest and largest value are lo and hi.  m: rounded down.  s: the smallest bf16 number with 15 s >=
-// hi - m.  15 s is an fp32 number, so the difference may be rounded up before it is compared; a product with 1 / 15 finds s up to
+// hi - m (NaN where lo or hi is not finite: taken with min and max that keep a NaN).  15 s is an fp32 number, so the difference may be rounded up before it is compared; a product with 1 / 15 finds s up to
 // one bf16 step.
-__device__ __forceinline__ uint32_t kv4_params(float lo, float hi, bool finite) {
+__device__ __forceinline__ uint32_t kv4_params(float lo, float hi) {
     const uint32_t m = __bfloat16_as_ushort(__float2bfloat16_rd(lo));
     const float d = __fsub_ru(hi, __uint_as_float(m << 16));
     uint32_t s = (__float_as_uint(d * (1.f / 15.f)) + 0xFFFFu) & 0xFFFF0000u;
     if (15.f * __uint_as_float(s) < d) s += 0x10000u;
     else if (s && 15.f * __uint_as_float(s - 0x10000u) >= d) s -= 0x10000u;
     // (lo so low that it rounds to -infinity; a range beyond fp32's)
-    return finite && (m & 0x7F80u) != 0x7F80u && s < 0x7F800000u && d < INFINITY ? s | m : 0x7FC07FC0u;
+    return fabsf(lo) < INFINITY && (m & 0x7F80u) != 0x7F80u && s < 0x7F800000u && d < INFINITY ? s | m : 0x7FC07FC0u;
 }
 
 // The code of x, decided without error; n is an integer next to the quotient or the one beside it.  x - m may need more than 24 bits:
@@ -62,6 +62,35 @@ __device__ __forceinline__ unsigned kv4_code_exact(float x, float m, float s, fl
     return (unsigned)fminf(fmaxf(n, 0.f), 15.f);
 }
 
+// min and max that keep a NaN
+__device__ __forceinline__ float kv4_min_nan(float x, float y) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float kv4_max_nan(float x, float y) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+// two fp32 operations at once
+__device__ __forceinline__ u64 kv4_pack2(float x, float y) {
+    u64 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void kv4_unpack2(u64 v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ u64 kv4_add2(u64 a, u64 b) {
+    u64 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ u64 kv4_mul2(u64 a, u64 b) {
+    u64 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // Codes of 8 values as 8 nibbles.  t = (x - m) / s comes from a product with an approximate reciprocal, off by less than 2^-18; where
 // it is nearer than 2^-17 to a tie (of bf16 values one in some hundreds is one) the exact form decides.
 __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t params) {
@@ -69,20 +98,26 @@ __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t par
     uint32_t w = 0u;
     if (s >= 1e-30f) {
         constexpr float MAGIC = 12582912.f;                 // 1.5 * 2^23: the nearest integer in the low bits
-        float inv, off = 0.f, t[8];
+        float inv, off = 0.f, t[8], u[8];
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+        const u64 mm = kv4_pack2(-m, -m), ii = kv4_pack2(inv, inv), up = kv4_pack2(MAGIC, MAGIC), down = kv4_pack2(-MAGIC, -MAGIC),
+                  minus = kv4_pack2(-1.f, -1.f);
 #pragma unroll
-        for (int i = 7; i >= 0; --i) {
-            t[i] = (x[i] - m) * inv;
-            const float u = t[i] + MAGIC;
-            off = fmaxf(off, fabsf(t[i] - (u - MAGIC)));
-            w = w * 16u + __float_as_uint(u);               // (0x4B400000 above n: together 0x3F400000 in 32 bits)
+        for (int i = 0; i < 8; i += 2) {
+            const u64 tt = kv4_mul2(kv4_add2(kv4_pack2(x[i], x[i + 1]), mm), ii), uu = kv4_add2(tt, up);
+            float d0, d1;
+            kv4_unpack2(kv4_add2(tt, kv4_mul2(kv4_add2(uu, down), minus)), d0, d1);
+            off = fmaxf(off, fmaxf(fabsf(d0), fabsf(d1)));
+            kv4_unpack2(tt, t[i], t[i + 1]);
+            kv4_unpack2(uu, u[i], u[i + 1]);
         }
+#pragma unroll
+        for (int i = 7; i >= 0; --i) w = w * 16u + __float_as_uint(u[i]);      // (0x4B400000 above n: together 0x3F400000 in 32 bits)
         w -= 0x3F400000u;
         if (off > 0.5f - 0x1p-17f) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float n = (t[i] + MAGIC) - MAGIC;
+                const float n = u[i] - MAGIC;
                 if (fabsf(t[i] - n) > 0.5f - 0x1p-17f) w = (w & ~(15u << (4 * i))) | (kv4_code_exact(x[i], m, s, n, 1.f) << (4 * i));
             }
         }
@@ -105,14 +140,13 @@ __device__ __forceinline__ int kv4_m_at(int dh, int which, int r, int w) { retur
 
 // One lane's 32 values - channels 32 w .. 32 w + 31 of row r, bf16 numbers - into a tile; which: 0 K, 1 V.
 __device__ __forceinline__ void kv4_store32(unsigned char* tile, int dh, int which, int r, int w, const float (&x)[32]) {
-    float lo = x[0], hi = x[0], zero = 0.f;
+    float lo = x[0], hi = x[0];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        zero = fmaf(x[i], 0.f, zero);
+    for (int i = 1; i < 32; ++i) {
+        lo = kv4_min_nan(lo, x[i]);
+        hi = kv4_max_nan(hi, x[i]);
     }
-    const uint32_t params = kv4_params(lo, hi, zero == 0.f);
+    const uint32_t params = kv4_params(lo, hi);
     *(uint16_t*)(tile + kv4_s_at(dh, which, r, w)) = (uint16_t)(params >> 16);
     *(uint16_t*)(tile + kv4_m_at(dh, which, r, w)) = (uint16_t)params;
 #pragma unroll
