@@ -35,38 +35,14 @@ __device__ __forceinline__ int kv4_owner(const CuSeqlens& first, int n, int i) {
     return lo;
 }
 
-// Append: DH / 8 lanes a row, a lane has 8 neighbouring channels, four lanes a group.  Two halves of 2 * DH / 8 lanes take the two
-// rows of a pair, which share the words of their V codes.
 struct Kv4Place {
-    int h, slot, w, c;         // KV head, slot, group, lane of the group
-    int row, packed;           // cache row; row of the packed input, -1: none
+    int h, slot, row, w, c;    // KV head, slot, cache row, group, lane of the group
 };
-template <int DH>
-__device__ __forceinline__ Kv4Place kv4_place(const Kv4RowsArgs& a) {
-    constexpr int LR = DH / 8, UNITS = 256 / (2 * LR);
-    Kv4Place p;
-    const int l = threadIdx.x % LR, odd = (threadIdx.x / LR) & 1, unit = threadIdx.x / (2 * LR);
-    p.h = (blockIdx.y << a.heads_log2) + (unit & ((1 << a.heads_log2) - 1));
-    const int pair = blockIdx.x * (UNITS >> a.heads_log2) + (unit >> a.heads_log2);
-    p.w = l >> 2;
-    p.c = l & 3;
-    p.packed = -1;
-    p.row = 0;
-    const int b = kv4_owner(a.pairs, a.sl.n, pair);
-    p.slot = a.sl.slot[b];
-    if (pair >= a.pairs.v[a.sl.n] || p.h >= a.c.Hkv) return p;
-    const int start = a.start[b], n = a.cu.v[b + 1] - a.cu.v[b];
-    if (start < 0 || start >= a.c.max_len) return p;
-    p.row = ((start >> 1) + (pair - a.pairs.v[b])) * 2 + odd;
-    const int i = p.row - start;
-    if (i >= 0 && i < n && p.row < a.c.max_len) p.packed = a.cu.v[b] + i;
-    return p;
-}
 
 template <typename T>
 __device__ __forceinline__ void kv4_load8(const void* p, long long i, float (&x)[8]) {
     if constexpr (sizeof(T) == 2) {
-        const uint4 w = ld_stream((const uint4*)((const bf16*)p + i));
+        const uint4 w = __ldg((const uint4*)((const bf16*)p + i));
         x[0] = bf16_lo(w.x); x[1] = bf16_hi(w.x); x[2] = bf16_lo(w.y); x[3] = bf16_hi(w.y);
         x[4] = bf16_lo(w.z); x[5] = bf16_hi(w.z); x[6] = bf16_lo(w.w); x[7] = bf16_hi(w.w);
     } else {
@@ -87,14 +63,11 @@ __device__ __forceinline__ uint32_t kv4_group_params(const float (&x)[8]) {
     return kv4_params(lo, hi);
 }
 
-// One row's 8 channels of K and of V into the cache.  `live`: the lane has a row; every lane of the warp takes part.
+// One row's 8 channels of K and of V into the cache (four lanes a group).  `live`: the lane has some; every lane of the warp takes part.
 template <int DH>
 __device__ __forceinline__ void kv4_store_row(const Kv4View& c, const Kv4Place& p, bool live, const float (&k)[8], const float (&v)[8]) {
-    constexpr int LR = DH / 8;
     const uint32_t kp = kv4_group_params(k), vp = kv4_group_params(v);
     const uint32_t kw = kv4_codes8(k, kp), vw = kv4_codes8(v, vp);
-    const uint32_t other = __shfl_xor_sync(0xffffffffu, vw, LR);
-    const bool both = __shfl_xor_sync(0xffffffffu, live ? 1 : 0, LR) != 0 && live;
     if (!live) return;
     unsigned char* tile = kv4_tile(c, p.slot, p.h, p.row);
     const int r = p.row % KV4_TILE;
@@ -105,29 +78,94 @@ __device__ __forceinline__ void kv4_store_row(const Kv4View& c, const Kv4Place& 
         *(uint16_t*)(tile + kv4_s_at(DH, 1, r, p.w)) = (uint16_t)(vp >> 16);
         *(uint16_t*)(tile + kv4_m_at(DH, 1, r, p.w)) = (uint16_t)vp;
     }
-    const bool odd = (p.row & 1) != 0;
-    if (both) {
-        // the pair's words are whole: the even row's lane writes the first, the odd row's the second
-        const uint32_t word = odd ? ((other >> 16) | (vw & 0xFFFF0000u)) : ((vw & 0xFFFFu) | (other << 16));
-        *(uint32_t*)(tile + kv4_v_at(DH, r & ~1, p.w, 2 * p.c + (odd ? 1 : 0))) = word;
-    } else {
-        *(uint16_t*)(tile + kv4_v_at(DH, r, p.w, 2 * p.c)) = (uint16_t)vw;
-        *(uint16_t*)(tile + kv4_v_at(DH, r, p.w, 2 * p.c + 1)) = (uint16_t)(vw >> 16);
-    }
+    *(uint16_t*)(tile + kv4_v_at(DH, r, p.w, 2 * p.c)) = (uint16_t)vw;
+    *(uint16_t*)(tile + kv4_v_at(DH, r, p.w, 2 * p.c + 1)) = (uint16_t)(vw >> 16);
 }
 
+// Append: a lane has one group of 32 channels of a row, first K's, then V's, so that nothing is shared but the words of the V codes,
+// which the two rows of a pair exchange (DH / 32 lanes further on).  The values are read twice, the second time from L1: for their
+// range, then eight at a time for their codes.  6144 rows of 32 heads, bf16: 62 us with 8 channels a lane and shuffles for the
+// groups (most of it went into finding the place and the parameters for too few values), 57 us with everything unrolled (a third
+// of that waiting for code).
 template <int DH, typename T>
-__global__ void __launch_bounds__(256) kv4_append_kernel(const __grid_constant__ Kv4RowsArgs a) {
+__global__ void __launch_bounds__(128) kv4_append_kernel(const __grid_constant__ Kv4RowsArgs a) {
+    constexpr int Q = DH / 32, UNITS = 128 / (2 * Q);
     pdl_wait();
     pdl_trigger();
-    const Kv4Place p = kv4_place<DH>(a);
-    float k[8] = {0.f}, v[8] = {0.f};
-    if (p.packed >= 0) {
-        const long long i = (long long)p.packed * a.ld + p.h * DH + 32 * p.w + 8 * p.c;
-        kv4_load8<T>(a.k, i, k);
-        kv4_load8<T>(a.v, i, v);
+    const int w = threadIdx.x % Q, odd = (threadIdx.x / Q) & 1, unit = threadIdx.x / (2 * Q);
+    const int h = (blockIdx.y << a.heads_log2) + (unit & ((1 << a.heads_log2) - 1));
+    const int pair = blockIdx.x * (UNITS >> a.heads_log2) + (unit >> a.heads_log2);
+    const int b = kv4_owner(a.pairs, a.sl.n, pair);
+    int row = 0, packed = -1;
+    if (pair < a.pairs.v[a.sl.n] && h < a.c.Hkv) {
+        const int start = a.start[b], n = a.cu.v[b + 1] - a.cu.v[b];
+        row = ((start >> 1) + (pair - a.pairs.v[b])) * 2 + odd;
+        const int i = row - start;
+        if (start >= 0 && start < a.c.max_len && i >= 0 && i < n && row < a.c.max_len) packed = a.cu.v[b] + i;
     }
-    kv4_store_row<DH>(a.c, p, p.packed >= 0, k, v);
+    const bool live = packed >= 0, both = __shfl_xor_sync(0xffffffffu, live ? 1 : 0, Q) != 0 && live;
+    const long long at = (long long)packed * a.ld + h * DH + 32 * w;
+    unsigned char* tile = kv4_tile(a.c, a.sl.slot[b], h, row);
+    const int r = row % KV4_TILE;
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        const void* src = which == 0 ? a.k : a.v;
+        uint32_t params = 0u;
+        if (live) {
+            float lo, hi;
+            if constexpr (sizeof(T) == 2) {
+                uint4 u[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = __ldg((const uint4*)((const bf16*)src + at) + i);
+                const uint32_t* x = (const uint32_t*)u;
+                auto two = [&](int i) { return *(const __nv_bfloat162*)&x[i]; };
+                __nv_bfloat162 m = two(0), n = two(0);
+#pragma unroll
+                for (int i = 1; i < 16; ++i) {
+                    m = __hmin2_nan(m, two(i));
+                    n = __hmax2_nan(n, two(i));
+                }
+                lo = kv4_min_nan(__low2float(m), __high2float(m));
+                hi = kv4_max_nan(__low2float(n), __high2float(n));
+            } else {
+                float4 u[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = __ldg((const float4*)((const float*)src + at) + i);
+                const float* x = (const float*)u;
+                lo = hi = x[0];
+#pragma unroll
+                for (int i = 1; i < 32; ++i) {
+                    lo = kv4_min_nan(lo, x[i]);
+                    hi = kv4_max_nan(hi, x[i]);
+                }
+            }
+            params = kv4_params(lo, hi);
+            *(uint16_t*)(tile + kv4_s_at(DH, which, r, w)) = (uint16_t)(params >> 16);
+            *(uint16_t*)(tile + kv4_m_at(DH, which, r, w)) = (uint16_t)params;
+        }
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+            float x[8];
+            uint32_t codes = 0u;
+            if (live) {
+                kv4_load8<T>(src, at + 8 * c, x);
+                codes = kv4_codes8(x, params);
+            }
+            if (which == 0) {
+                if (live) *(uint32_t*)(tile + kv4_k_at(DH, r, w, c)) = codes;
+                continue;
+            }
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, codes, Q);
+            if (both) {
+                // the pair's words are whole: the even row's lane writes the first, the odd row's the second
+                const uint32_t word = odd ? ((other >> 16) | (codes & 0xFFFF0000u)) : ((codes & 0xFFFFu) | (other << 16));
+                *(uint32_t*)(tile + kv4_v_at(DH, r & ~1, w, 2 * c + odd)) = word;
+            } else if (live) {
+                *(uint16_t*)(tile + kv4_v_at(DH, r, w, 2 * c)) = (uint16_t)codes;
+                *(uint16_t*)(tile + kv4_v_at(DH, r, w, 2 * c + 1)) = (uint16_t)(codes >> 16);
+            }
+        }
+    }
 }
 
 // Read: a lane has four neighbouring channels of a row, so that a warp writes whole lines, and four rows.
@@ -216,7 +254,7 @@ __global__ void __launch_bounds__(128) kv4_put_kernel(Kv4View c, const float* kv
             y[i] = __bfloat162float(__float2bfloat16_rn(v[e]));
         }
         Kv4Place p;
-        p.h = h; p.slot = slots[j]; p.w = l >> 2; p.c = l & 3; p.row = row + row_add; p.packed = 0;
+        p.h = h; p.slot = slots[j]; p.w = l >> 2; p.c = l & 3; p.row = row + row_add;
         kv4_store_row<DH>(c, p, live, x, y);
     } else if (q_out) {
         for (int i = threadIdx.x - 32; i < G * HALF; i += 96) {
@@ -1066,8 +1104,8 @@ extern "C" int hivis_kv4_append(const hivis_kv4_cache* cache, int B, const int* 
     if (ld % 8 || ld < (int64_t)a.c.Hkv * a.c.dh) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: ld must be a multiple of 8 of at least n_kv_heads * head_dim", who);
     a.k = k; a.v = v; a.ld = ld;
     dim3 grid;
-    const dim3 block(256);
-    if (!kv4_rows_grid(&a, 256 / (a.c.dh / 4), 1, a.pairs.v[B], &grid)) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads", who);
+    const dim3 block(128);
+    if (!kv4_rows_grid(&a, 128 / (a.c.dh / 16), 1, a.pairs.v[B], &grid)) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads", who);
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e;
     if (dtype == HIVIS_BF16) e = a.c.dh == 128 ? launch_pdl(kv4_append_kernel<128, bf16>, grid, block, 0, st, a) : launch_pdl(kv4_append_kernel<64, bf16>, grid, block, 0, st, a);
