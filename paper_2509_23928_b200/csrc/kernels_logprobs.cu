@@ -21,9 +21,6 @@
 
 namespace cg = cooperative_groups;
 
-#define LP_THREADS 256
-#define LP_WARPS (LP_THREADS / 32)
-#define LP_CTAS 4                 // to an SM
 #define LP_MAX_CLUSTER 16
 static_assert(HIVIS_LOGPROBS_MAX_IDS <= 32 && HIVIS_LOGPROBS_MAX_TOP <= 32, "a lane each");
 #define LP_CAND 512               // candidates a CTA keeps, and a cluster
@@ -62,6 +59,9 @@ __device__ __forceinline__ void lp_lower(float& z, float& w, float d) {
 template <typename T>
 struct LpVec {
     static constexpr int N = 16 / (int)sizeof(T);
+    // Threads to a CTA; 1024 to an SM.  Smaller CTAs even out the last wave of many rows (1021 fp32 rows of 50257: 41 us with 128
+    // threads, 45 with 256); with eight bf16 logits to a load a row needs the 256 (512 rows of 152064: 49 us, 55).
+    static constexpr int THREADS = sizeof(T) == 2 ? 256 : 128;
 };
 template <typename T>
 __device__ __forceinline__ uint4 lp_load(const T* row, int i, int lo, int hi) {
@@ -194,7 +194,8 @@ struct LpPart {
 };
 
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, LP_CTAS) logprob_kernel(const __grid_constant__ LogprobArgs a) {
+__global__ void __launch_bounds__(LpVec<T>::THREADS, 1024 / LpVec<T>::THREADS) logprob_kernel(const __grid_constant__ LogprobArgs a) {
+    constexpr int LP_THREADS = LpVec<T>::THREADS, LP_WARPS = LP_THREADS / 32;
     constexpr int N = LpVec<T>::N, U = 4, STRIDE = LP_THREADS * N;
     __shared__ LpSum s_sum[LP_WARPS];
     __shared__ float s_most[LP_WARPS], s_max[LP_WARPS][32], s_bar;
@@ -414,15 +415,15 @@ static cudaError_t lp_launch(LogprobArgs& a, int dev, int num_sms, cudaStream_t 
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < HIVIS_MAX_DEVICES) attr_set[dev] = true;
     }
-    // CTAs per row: two to an SM, each with a few thousand logits at least.  A CTA costs some microseconds beside its logits: 56 rows of
+    // CTAs per row: half of what the GPU holds, each with a few thousand logits at least.  A CTA costs some microseconds beside its logits: 56 rows of
     // 152064 take 12.3 us with 8 CTAs each, 14.4 with 4, 16.4 with 16; 1021 rows of 50257 take 45 with one, 58 with two.
     int S = 1;
-    while (S < LP_MAX_CLUSTER && (long long)a.n_rows * S < 2ll * num_sms && a.V / (2 * S) >= 2048) S *= 2;
+    while (S < LP_MAX_CLUSTER && (long long)a.n_rows * S < (long long)num_sms * 512 / LpVec<T>::THREADS && a.V / (2 * S) >= 8 * LpVec<T>::THREADS) S *= 2;
     a.slice = ((a.V + 8 + S - 1) / S + 7) / 8 * 8;
     cudaLaunchConfig_t cfg = {};
     const int y = a.n_rows < 32768 ? a.n_rows : 32768;
     cfg.gridDim = dim3((unsigned)S, (unsigned)y, (unsigned)((a.n_rows + y - 1) / y));
-    cfg.blockDim = dim3(LP_THREADS);
+    cfg.blockDim = dim3(LpVec<T>::THREADS);
     cfg.stream = st;
     cudaLaunchAttribute at[2] = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
