@@ -558,7 +558,7 @@ class Kv4Cache:
         t, B = self.torch, len(cu_seqlens) - 1
         shape = (int(cu_seqlens[-1]), self.n_kv_heads, self.head_dim)
         k = t.empty(shape, dtype=t.float32, device=self.dev)
-        v = t.empty(shape, dtype=t.float32, device=self.dev)
+        v = k.new_empty(shape)
         _check(lib.hivis_kv4_read(self._ref, B, _slots(slots, B), _ints(cu_seqlens), self._counts(start_rows, B, "start_rows"), k.data_ptr(),
                                   v.data_ptr(), _raw_stream(self.dev.index)))
         return k, v
@@ -578,7 +578,7 @@ class Kv4Cache:
                 raise ValueError("mask must be a contiguous int32 tensor [B, n_q, ceil(mask_rows / 32)]")
             mask_ptr = mask.data_ptr()
         if out is None:
-            out = t.empty(q.shape, dtype=q.dtype, device=self.dev)
+            out = q.new_empty(q.shape)
             out_ld = heads * self.head_dim
         else:
             if out.dtype is not q.dtype:
@@ -618,16 +618,16 @@ def logprobs(logits, ids=None, temperature: float = 1.0, top_n: int = 0, entropy
         n_ids = ids.shape[1]
     lp = h = top = top_lp = None
     p_lp = p_h = p_top = p_top_lp = None
-    dev = logits.device
+    f32 = torch.float32
     if n_ids:
-        lp = torch.empty((n, n_ids), dtype=torch.float32, device=dev)
+        lp = logits.new_empty((n, n_ids), dtype=f32)
         p_lp = lp.data_ptr()
     if entropy:
-        h = torch.empty((n,), dtype=torch.float32, device=dev)
+        h = logits.new_empty((n,), dtype=f32)
         p_h = h.data_ptr()
     if top_n > 0:
-        top = torch.empty((n, top_n), dtype=torch.int32, device=dev)
-        top_lp = torch.empty((n, top_n), dtype=torch.float32, device=dev)
+        top = logits.new_empty((n, top_n), dtype=torch.int32)
+        top_lp = logits.new_empty((n, top_n), dtype=f32)
         p_top, p_top_lp = top.data_ptr(), top_lp.data_ptr()
     _check(lib.hivis_logprobs(n, vocab, logits.data_ptr(), _dtype(logits), stride[0] if n > 1 else vocab, temperature,
                               ids.data_ptr() if n_ids else None, n_ids, top_n, p_lp, p_h, p_top, p_top_lp, _raw_stream(index)))

@@ -12,6 +12,18 @@
 typedef __nv_bfloat16 bf16;
 typedef unsigned long long u64;
 
+// SMs of a device, asked for once
+inline cudaError_t device_sms(int dev, int* sms) {
+    static int known[64] = {0};
+    if (dev >= 0 && dev < 64 && known[dev] > 0) {
+        *sms = known[dev];
+        return cudaSuccess;
+    }
+    const cudaError_t e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) known[dev] = *sms;
+    return e;
+}
+
 void hivis_set_global_error(const char* msg);   // text of a failed call that has no context
 
 #define HIVIS_MAX_DEVICES 64   // per-device caches of function attributes are indexed by device ordinal
@@ -454,6 +466,25 @@ inline cudaError_t launch_pdl(void (*kernel)(P...), dim3 grid, dim3 block, size_
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
+
+// The same for clusters of `cluster` CTAs along x (1: none).
+template <typename... P, typename... A>
+inline cudaError_t launch_cluster_pdl(void (*kernel)(P...), int cluster, dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
 }
 

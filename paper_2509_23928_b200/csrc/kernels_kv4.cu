@@ -961,20 +961,8 @@ static cudaError_t kv4_launch(void (*kernel)(Kv4AttnArgs), bool* attr_set, Kv4At
     }
     a.n_blocks = (a.ncol + columns - 1) / columns;
     const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, step_rows, resident);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)S, (unsigned)(a.c.Hkv * a.n_blocks), (unsigned)a.sl.n);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute at[2] = {};
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = (unsigned)S;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    const dim3 grid((unsigned)S, (unsigned)(a.c.Hkv * a.n_blocks), (unsigned)a.sl.n);
+    return launch_cluster_pdl(kernel, S, grid, dim3((unsigned)threads), smem, st, a);
 }
 template <int DH, int NT, typename T, int U, int WARPS, int CTAS>
 static cudaError_t kv4_launch_attn(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
@@ -1156,7 +1144,7 @@ extern "C" int hivis_kv4_attention(const hivis_kv4_cache* cache, int B, const in
     if ((long long)a.c.Hkv * ((a.ncol + 7) / 8) > 65535) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: too many heads and queries for one call", who);
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = device_sms(dev, &sms);
     if (e != cudaSuccess) return kv4_cuda(who, e);
     cudaStream_t st = (cudaStream_t)stream;
     if (dtype == HIVIS_BF16) e = a.c.dh == 128 ? kv4_launch_attn_n<128, bf16>(a, dev, sms, st) : kv4_launch_attn_n<64, bf16>(a, dev, sms, st);

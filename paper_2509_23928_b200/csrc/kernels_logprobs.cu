@@ -420,20 +420,9 @@ static cudaError_t lp_launch(LogprobArgs& a, int dev, int num_sms, cudaStream_t 
     int S = 1;
     while (S < LP_MAX_CLUSTER && (long long)a.n_rows * S < (long long)num_sms * 512 / LpVec<T>::THREADS && a.V / (2 * S) >= 8 * LpVec<T>::THREADS) S *= 2;
     a.slice = ((a.V + 8 + S - 1) / S + 7) / 8 * 8;
-    cudaLaunchConfig_t cfg = {};
     const int y = a.n_rows < 32768 ? a.n_rows : 32768;
-    cfg.gridDim = dim3((unsigned)S, (unsigned)y, (unsigned)((a.n_rows + y - 1) / y));
-    cfg.blockDim = dim3(LpVec<T>::THREADS);
-    cfg.stream = st;
-    cudaLaunchAttribute at[2] = {};
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = (unsigned)S;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    const dim3 grid((unsigned)S, (unsigned)y, (unsigned)((a.n_rows + y - 1) / y));
+    return launch_cluster_pdl(kernel, S, grid, dim3(LpVec<T>::THREADS), 0, st, a);
 }
 
 #define LP_FAIL(code, ...)                                    \
@@ -470,7 +459,7 @@ extern "C" int hivis_logprobs(int n_rows, int vocab, const void* logits, int log
     a.out_lp = n_ids > 0 ? out_logprobs : nullptr; a.out_h = out_entropy; a.out_top = out_top_ids; a.out_top_lp = out_top_logprobs;
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = device_sms(dev, &sms);
     cudaStream_t st = (cudaStream_t)stream;
     if (e == cudaSuccess) {
         if (logits_dtype == HIVIS_BF16) e = top_n ? lp_launch<bf16, true>(a, dev, sms, st) : lp_launch<bf16, false>(a, dev, sms, st);
