@@ -646,22 +646,25 @@ def tree_and_sampling(weights: WeightCache, reps: int = 30):
     return out
 
 
-def draft_verify_refresh_loop(weights: WeightCache, rounds: int = 40, tc_prefill_min: int = 0):
+def draft_verify_refresh_loop(weights: WeightCache, rounds: int = 40, tc_prefill_min: int = 0, kv_bits: int = 16,
+                              alternatives: int = -1):
     """Algorithm 1 as a loop on the drafter's side, batch 16 of the headline shape: draft k tokens, verify them against a
     toy target whose accept lengths are planted (a truncated geometric law with ratio 0.75, drawn per sequence and
     round), then rebuild the rows of the accepted tokens from the target's "true" features (seeded noise standing in for
     them) with hivis_prefill(start_pos) and go on with the next round.  The accept counts travel to the host every round,
-    as they do to whoever runs the target.  Reported: tokens committed per round and sequence, the time of the three calls
+    as they do to whoever runs the target.  kv_bits 4: the drafter's cache is held in 4 bits; alternatives n >= 0: every
+    round also returns the log-probabilities, entropies and n alternatives of the committed tokens' rows.  Reported: tokens committed per round and sequence, the time of the three calls
     (CUDA events), and committed tokens per second of drafter-side time."""
     import torch
     from hivis_inputs.device import to_dev
-    from paper_2509_23928_b200 import Drafter
+    from paper_2509_23928_b200 import Drafter, logprobs
     wl = hi.workload(BATCH16)
     B, k, V, d = wl.batch, wl.k, wl.dims.vocab, wl.dims.d
     ids, hidden, cu = hi.make_prompt(wl)
     lens = np.diff(cu).astype(np.int64)
     resid = hi.make_residuals(wl)
-    dr = Drafter(wl.dims, weights.get(wl), max_batch=B, max_len=int(lens.max()) + rounds * (k + 1) + 8, max_k=8)
+    dr = Drafter(wl.dims, weights.get(wl), max_batch=B, max_len=int(lens.max()) + rounds * (k + 1) + 8, max_k=8,
+                 kv_bits=4 if kv_bits == 4 else None)
     if tc_prefill_min:
         dr.set_tc_prefill(tc_prefill_min)
     d_resid = to_dev(resid, wl.dims.dtype)
@@ -674,7 +677,7 @@ def draft_verify_refresh_loop(weights: WeightCache, rounds: int = 40, tc_prefill
     rows_b = torch.arange(B, device="cuda")[:, None]
     cols_k = torch.arange(k + 1, device="cuda")[None, :]
     ev = lambda: torch.cuda.Event(enable_timing=True)
-    t_draft, t_verify, t_refresh, committed = [], [], [], 0
+    t_draft, t_verify, t_refresh, t_logprobs, committed = [], [], [], [], 0
     T = lens.copy()
     torch.cuda.synchronize()
     t0 = time.perf_counter()
@@ -695,6 +698,14 @@ def draft_verify_refresh_loop(weights: WeightCache, rounds: int = 40, tc_prefill
         e1b = ev(); e1b.record()
         acc, nxt, kv = dr.verify(out_ids, logits)
         e2.record()
+        if alternatives >= 0:
+            e2b = ev()
+            logprobs(logits.view(B * (k + 1), V), torch.cat([out_ids, nxt[:, None]], 1).view(-1, 1), top_n=alternatives)
+            e2b.record()
+            torch.cuda.synchronize()
+            if r >= 3:
+                t_logprobs.append(e2.elapsed_time(e2b))
+            e2.record()
         n = acc.cpu().numpy().astype(np.int64)                                             # the host learns the outcome
         nx = nxt.cpu().numpy()
         oi = out_ids.cpu().numpy()
@@ -721,7 +732,8 @@ def draft_verify_refresh_loop(weights: WeightCache, rounds: int = 40, tc_prefill
             "drafter_side_us_per_round": round(side, 1),
             "committed_tokens_per_s_of_drafter_time": round(B * tau / (side * 1e-6), 1),
             "wall_ms_per_round_with_toy_target": round(wall / rounds * 1e3, 3),
-            "tc_prefill_min_pairs": tc_prefill_min or "default"}
+            "tc_prefill_min_pairs": tc_prefill_min or "default", "kv_bits": kv_bits,
+            **({"logprobs_us": us(t_logprobs), "alternatives": alternatives} if t_logprobs else {})}
 
 
 def stub_replica(rank: int) -> dict:
@@ -747,6 +759,8 @@ def main():
                     help="time tree drafting + tree verification (one sequence) and speculative-sampling verification (batch 16)")
     ap.add_argument("--loop", action="store_true",
                     help="draft -> verify -> refresh rounds at batch 16 against a toy target with planted accept lengths")
+    ap.add_argument("--kv-bits", type=int, default=16, choices=[4, 16], help="with --loop: bits of a cached value")
+    ap.add_argument("--alternatives", type=int, default=-1, help="with --loop: log-probabilities with this many alternatives every round")
     ap.add_argument("--tc-prefill-min", type=int, default=0, help="with --loop: smallest prefill call (pairs) on the tensor-core path")
     ap.add_argument("--phase-times", action="store_true",
                     help="print where a draft step of the tensor-core chain kernel goes (its own time stamps) and exit")
@@ -808,7 +822,8 @@ def main():
         print(json.dumps(tree_and_sampling(weights)))
         return
     if args.loop:
-        print(json.dumps(draft_verify_refresh_loop(weights, tc_prefill_min=args.tc_prefill_min)))
+        print(json.dumps(draft_verify_refresh_loop(weights, tc_prefill_min=args.tc_prefill_min, kv_bits=args.kv_bits,
+                                                   alternatives=args.alternatives)))
         return
     if args.phase_times:
         print(json.dumps(phase_breakdown(hi.workload(args.workload or BATCH16), weights)))

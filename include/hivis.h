@@ -406,7 +406,7 @@ int hivis_kv4_read(const hivis_kv4_cache* cache, int B, const int* seq_slots_hos
  *   mask NULL: causal.  The queries sit on the last n_q rows: query i sees rows [0, rows[b] - n_q + i].
  *   mask (uint32 [B, n_q, ceil(mask_rows / 32)]): a draft tree, or anything else over the last mask_rows rows: query i sees
  *   rows [0, rows[b] - mask_rows), and row rows[b] - mask_rows + j iff bit j % 32 of word j / 32 is set.
- * A query that sees no row gets zeros.  Rows that a query does not see do not touch its result, whatever they hold.
+ * scale: positive, below 1e38.  A query that sees no row gets zeros.  Rows that a query does not see do not touch its result, whatever they hold.
  * q [B * n_q, n_q_heads * head_dim] and out likewise in `dtype` (HIVIS_F32 | HIVIS_BF16), q_ld and out_ld elements from one
  * row to the next.  The result does not depend on anything but the arguments: sums are made in one order.
  * Errors: ARG, SHAPE (n_q_heads not a multiple of n_kv_heads, q_ld or out_ld not a multiple of 8), DTYPE, CAPACITY (B, n_q >
@@ -418,7 +418,7 @@ int hivis_kv4_attention(const hivis_kv4_cache* cache, int B, const int* seq_slot
 /* Log-probabilities of rows of logits: what a server returns for the tokens a verification committed, and what tells how
  * sure a draft is.  (The paper has no counterpart.)  Needs no context or workspace and keeps nothing; each logit is read once.
  * logits [n_rows, vocab] in logits_dtype (HIVIS_F32 | HIVIS_BF16), ld >= vocab elements from one row to the next (any number:
- * rows need not be aligned); p = softmax(row / temperature).
+ * rows need not be aligned); p = softmax(row / temperature), 1e-30 < temperature < 1e30.
  *   ids (int32 [n_rows, n_ids], with n_ids > 0): out_logprobs fp32 [n_rows, n_ids] = log p of each; -infinity for a token
  *   without mass and for an id outside [0, vocab).
  *   out_entropy (nullable, fp32 [n_rows]): -sum p log p, in nats.

@@ -509,6 +509,8 @@ class Kv4Cache:
             self.dev = torch.device("cuda", torch.cuda.current_device())
         self.n_slots, self.n_kv_heads, self.head_dim = int(n_slots), int(n_kv_heads), int(head_dim)
         self.max_len = (int(max_len) + 31) // 32 * 32
+        if self.n_slots < 1 or self.n_kv_heads < 1 or self.max_len < 32 or self.head_dim not in (64, 128):
+            raise ValueError("a cache has at least one slot, KV head and row, and a head_dim of 64 or 128")
         self.data = torch.zeros(self.n_slots * self.n_kv_heads * self.max_len * self.head_dim * 5 // 4, dtype=torch.uint8, device=self.dev)
         self.c = hivis_kv4_cache(C.sizeof(hivis_kv4_cache), self.n_slots, self.n_kv_heads, self.head_dim, self.max_len,
                                  self.data.data_ptr())

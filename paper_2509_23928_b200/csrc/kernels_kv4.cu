@@ -99,9 +99,11 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(const __grid_constant__
     int row = 0, packed = -1;
     if (pair < a.pairs.v[a.sl.n] && h < a.c.Hkv) {
         const int start = a.start[b], n = a.cu.v[b + 1] - a.cu.v[b];
-        row = ((start >> 1) + (pair - a.pairs.v[b])) * 2 + odd;
-        const int i = row - start;
-        if (start >= 0 && start < a.c.max_len && i >= 0 && i < n && row < a.c.max_len) packed = a.cu.v[b] + i;
+        if (start >= 0 && start < a.c.max_len) {
+            row = ((start >> 1) + (pair - a.pairs.v[b])) * 2 + odd;
+            const int i = row - start;
+            if (i >= 0 && i < n && row < a.c.max_len) packed = a.cu.v[b] + i;
+        }
     }
     const bool live = packed >= 0, both = __shfl_xor_sync(0xffffffffu, live ? 1 : 0, Q) != 0 && live;
     const long long at = (long long)packed * a.ld + h * DH + 32 * w;
@@ -1134,7 +1136,7 @@ extern "C" int hivis_kv4_attention(const hivis_kv4_cache* cache, int B, const in
     if (n_q_heads < 1 || n_q_heads % a.c.Hkv) KV4_FAIL(HIVIS_ERR_SHAPE, "%s: n_q_heads must be a multiple of n_kv_heads", who);
     if (q_ld % 8 || out_ld % 8 || q_ld < (int64_t)n_q_heads * a.c.dh || out_ld < (int64_t)n_q_heads * a.c.dh)
         KV4_FAIL(HIVIS_ERR_SHAPE, "%s: q_ld and out_ld must be multiples of 8 of at least n_q_heads * head_dim", who);
-    if (!(scale > 0.f) || !(scale < 3e38f)) KV4_FAIL(HIVIS_ERR_ARG, "%s: scale must be positive", who);
+    if (!(scale > 0.f) || !(scale < 1e38f)) KV4_FAIL(HIVIS_ERR_ARG, "%s: scale must be positive and less than 1e38", who);
     if (mask && (mask_rows < 1 || mask_rows > HIVIS_KV4_MAX_MASK))
         KV4_FAIL(HIVIS_ERR_CAPACITY, "%s: mask_rows=%d outside [1,%d]", who, mask_rows, HIVIS_KV4_MAX_MASK);
     a.rows = rows; a.q = q; a.q_ld = q_ld; a.n_q = n_q; a.Hq = n_q_heads; a.G = n_q_heads / a.c.Hkv; a.ncol = n_q * a.G;

@@ -440,7 +440,7 @@ extern "C" int hivis_logprobs(int n_rows, int vocab, const void* logits, int log
     if (vocab < 1 || vocab > HIVIS_LOGPROBS_MAX_VOCAB) LP_FAIL(HIVIS_ERR_SHAPE, "hivis_logprobs: vocab=%d outside [1,%d]", vocab, HIVIS_LOGPROBS_MAX_VOCAB);
     if (logits_dtype != HIVIS_F32 && logits_dtype != HIVIS_BF16) LP_FAIL(HIVIS_ERR_DTYPE, "hivis_logprobs: unknown logits dtype");
     if (ld < vocab) LP_FAIL(HIVIS_ERR_SHAPE, "hivis_logprobs: ld is less than vocab");
-    if (!(temperature > 0.f) || !(temperature < 3e38f)) LP_FAIL(HIVIS_ERR_ARG, "hivis_logprobs: temperature must be positive");
+    if (!(temperature > 1e-30f) || !(temperature < 1e30f)) LP_FAIL(HIVIS_ERR_ARG, "hivis_logprobs: temperature outside (1e-30, 1e30)");
     if (n_ids < 0 || n_ids > HIVIS_LOGPROBS_MAX_IDS) LP_FAIL(HIVIS_ERR_CAPACITY, "hivis_logprobs: n_ids=%d outside [0,%d]", n_ids, HIVIS_LOGPROBS_MAX_IDS);
     if (top_n < 0 || top_n > HIVIS_LOGPROBS_MAX_TOP) LP_FAIL(HIVIS_ERR_CAPACITY, "hivis_logprobs: top_n=%d outside [0,%d]", top_n, HIVIS_LOGPROBS_MAX_TOP);
     if (n_rows == 0) return HIVIS_OK;

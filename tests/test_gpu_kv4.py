@@ -425,3 +425,45 @@ def test_tensors_that_do_not_fit_are_refused():
             call()
     with pytest.raises(TypeError):
         cache.append(k.half(), k.half(), [0, 4], _ints([0]))
+    for bad in ((0, 2, 64, 32), (1, 0, 64, 32), (1, 2, 96, 32), (1, 2, 64, 0)):
+        with pytest.raises(ValueError):
+            _cache(*bad)
+
+
+@pytest.mark.parametrize("call", ["append", "attention", "logprobs"])
+def test_a_first_call_may_be_a_captured_one(call):
+    """In a process of its own: nothing has been loaded or set up when the capture begins."""
+    import subprocess
+    import sys
+    code = f"""
+import torch
+from paper_2509_23928_b200 import Kv4Cache, logprobs
+cache = Kv4Cache(2, 2, 64, 64)
+k = torch.randn(10, 2, 64, device="cuda").bfloat16()
+q = torch.randn(2, 4, 64, device="cuda").bfloat16()
+x = torch.randn(3, 500, device="cuda")
+zero, rows = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.tensor([5, 5], dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+f = dict(append=lambda: cache.append(k, k, [0, 5, 10], zero), attention=lambda: cache.attention(q, rows), logprobs=lambda: logprobs(x, top_n=3))["{call}"]
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    out = f()
+g.replay()
+torch.cuda.synchronize()
+got = cache.data.clone() if out is None else out.clone() if torch.is_tensor(out) else out.top_logprobs.clone()
+again = f()
+assert torch.equal(got, cache.data if again is None else again if torch.is_tensor(again) else again.top_logprobs)
+print("done")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "done" in r.stdout, r.stderr[-2000:]
+
+
+def test_the_output_may_be_the_queries():
+    t = _torch()
+    for n_q, G in ((1, 2), (5, 7)):
+        f = Filled("bf16", 128, 2, G, [1500, 33], n_q, seed=23)
+        f.put()
+        want = f.cache.attention(f.q, f.rows, n_q=n_q)
+        q = f.q.clone()
+        assert t.equal(f.cache.attention(q, f.rows, n_q=n_q, out=q), want) and t.equal(q, want)

@@ -11,7 +11,7 @@ def _call(n=3, vocab=100, logits=P, dtype=0, ld=100, temperature=1.0, ids=P, n_i
 
 @pytest.mark.parametrize("kw,code", [
     (dict(n=-1), -5), (dict(vocab=0), -2), (dict(vocab=2 ** 28 + 1, ld=2 ** 29), -2), (dict(dtype=2), -3), (dict(ld=99), -2),
-    (dict(temperature=0.0), -1), (dict(temperature=-1.0), -1), (dict(temperature=float("nan")), -1), (dict(temperature=float("inf")), -1),
+    (dict(temperature=0.0), -1), (dict(temperature=-1.0), -1), (dict(temperature=float("nan")), -1), (dict(temperature=float("inf")), -1), (dict(temperature=1e-38), -1),
     (dict(n_ids=33), -5), (dict(n_ids=-1), -5), (dict(top=33), -5), (dict(top=-1), -5), (dict(logits=None), -1), (dict(ids=None), -1),
     (dict(lp=None), -1), (dict(top_ids=None), -1), (dict(top_lp=None), -1), (dict(logits=P + 4), -1), (dict(ids=P + 4), -1),
     (dict(h=P + 8), -1), (dict(top_lp=P + 2), -1), (dict(n_ids=0, top=0, h=None), -1),
