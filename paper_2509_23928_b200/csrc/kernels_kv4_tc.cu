@@ -1,0 +1,579 @@
+// Attention of many columns (queries x query heads of a KV head) over a 4-bit cache, on the tcgen05 tensor cores.
+//
+// A CTA has 64 columns and takes 128 rows of the cache at a time:
+//   S^T [128 rows x 64 columns] = K Q^T      A = K's values, B = the queries, accumulators in tensor memory
+//   P^T = 2^(S^T f - m)                      a thread has one row and half the columns
+//   O^T [channels x 64] += V^T P^T           A = V's values, B = the probabilities; a column's sum of weights is one more product, of ones
+// Eight warps take the codes apart, eight others have the probabilities: rows' values t + 1 are made while the probabilities of rows t
+// are.  Values m + s n are written as fp16 numbers (11 bits, like the probabilities; a bf16 result has 8) to shared memory in the
+// layouts that tcgen05.mma reads (rows of 128 bytes, 128-byte swizzle).  A word of K codes has eight channels of a row: 16 bytes of
+// that row, the channels of a group in the order of the nibbles, and the queries' in the same.  Two words of V codes have four channels
+// each of two neighbouring rows: 16 bytes of either row, channels of two groups side by side; V^T and P^T are read transposed, a row
+// of the cache to 128 bytes, and the results' channels put in order when they leave.
+// Keys are scaled by a power of two of their row (which the row's scores undo), values by one of the CTA, R, so that fp16's range
+// holds them; probabilities are written for a running maximum that is raised once a score is above it by 2^8.
+#include <cstring>
+
+#include <cooperative_groups.h>
+
+#include "kv4_attn.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+constexpr int KT_COLS = 64, KT_ROWS = 128, KT_GROUP = 256, KT_THREADS = 2 * KT_GROUP, KT_STAGES = 3, KT_TILES = KT_ROWS / KV4_TILE;
+constexpr uint32_t KT_TMEM = 256;                                     // columns: S^T of two steps, O^T, the sums
+// Probabilities are held as 2^KT_LIFT p, below 2^15: fp16 has them to 2^-31 of a column's largest.
+#define KT_LIFT 7.f
+constexpr uint32_t KT_S = 0, KT_O = 128, KT_L = 192;
+
+// Shared memory, every block 1024-byte aligned.  K: [64 channels a block][128 rows][128 bytes], Q: [64 channels a block][64][128 bytes];
+// V: [64 channels a block][128 rows][128 bytes] (head_dim 64: a block of channels, a block of ones), P: [128 rows][128 bytes].
+template <int DH>
+struct KtSmem {
+    static constexpr int KB = DH / 64;                                 // blocks of 64 channels
+    static constexpr int RAW = KT_TILES * kv4_tile_bytes(DH);
+    static constexpr int K = KT_STAGES * RAW, V = K + KB * 16384, P = V + 2 * 16384, Q = P + 16384, ONES = Q + KB * 8192;
+    static constexpr int END = ONES + 4096;
+    static constexpr int LDO = DH + 4;
+    static constexpr int BYTES = END + 1024;                           // (the base is aligned by hand)
+    static_assert(RAW % 1024 == 0 && KT_COLS * LDO * 4 <= END && BYTES <= 227 * 1024, "layout");
+};
+
+// fp16 operands, fp32 accumulators, M = 128, N = 64; ROWS: both operands with the products' axis along 128-byte rows, else across them
+template <bool ROWS>
+__device__ __forceinline__ void kt_mma(uint32_t d, u64 a, u64 b, uint32_t accumulate) {
+    constexpr uint32_t IDESC = (1u << 4) | (ROWS ? 0u : 3u << 15) | ((KT_COLS >> 3) << 17) | ((128 >> 4) << 24);
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(IDESC), "r"(accumulate) : "memory");
+}
+// 128-byte rows, 128-byte swizzle, groups of 8 rows 1024 bytes apart; blocks of 64 elements across `apart` bytes apart
+__device__ __forceinline__ u64 kt_desc(uint32_t addr, uint32_t apart = 16) {
+    const uint32_t lo = ((addr >> 4) & 0x3FFFu) | ((apart >> 4) << 16), hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+    return ((u64)hi << 32) | lo;
+}
+__device__ __forceinline__ void kt_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void kt_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void kt_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void kt_fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ bool kt_elect() {
+    uint32_t p;
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+template <int ID>
+__device__ __forceinline__ void kt_sync() { asm volatile("barrier.cta.sync %0, %1;" ::"n"(ID), "n"(KT_GROUP) : "memory"); }
+template <int ID>
+__device__ __forceinline__ bool kt_sync_or(bool x) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)x), "n"(ID), "n"(KT_GROUP) : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ void kt_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+#define KT_R(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
+#define KT_W(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+// 32 columns of the 32 tensor-memory lanes that this warp may touch
+__device__ __forceinline__ void kt_ld32(uint32_t t, uint32_t (&r)[32]) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : KT_R(r, 0), KT_R(r, 8), KT_R(r, 16), KT_R(r, 24) : "r"(t) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+// 16 columns
+__device__ __forceinline__ void kt_ld16(uint32_t t, uint32_t (&r)[16]) {
+    __syncwarp();
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : KT_R(r, 0), KT_R(r, 8) : "r"(t) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void kt_st32(uint32_t t, const uint32_t (&r)[32]) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        ::KT_W(r, 0), KT_W(r, 8), KT_W(r, 16), KT_W(r, 24), "r"(t) : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ uint32_t kt_h2(const __half2& h) { return *(const uint32_t*)&h; }
+__device__ __forceinline__ __half2 kt_as_h2(uint32_t w) { return *(const __half2*)&w; }
+
+// The eight values of a word of codes, in the nibbles' order (0 and 4, 1 and 5, 2 and 6, 3 and 7), for s, s / 16 and m as pairs.
+__device__ __forceinline__ void kt_values(uint32_t x, const __half2& s, const __half2& s16, const __half2& m, uint32_t (&v)[4]) {
+    const uint32_t y = x >> 8;
+    v[0] = kt_h2(__hfma2(kt_as_h2(kv4_lo<true>(x)), s, m));
+    v[1] = kt_h2(__hfma2(kt_as_h2(kv4_hi<true>(x)), s16, m));
+    v[2] = kt_h2(__hfma2(kt_as_h2(kv4_lo<true>(y)), s, m));
+    v[3] = kt_h2(__hfma2(kt_as_h2(kv4_hi<true>(y)), s16, m));
+}
+// Which of the 32 rows from r0 on query i sees.
+__device__ __forceinline__ uint32_t kt_window(const Kv4Sight& s, int r0, int i) {
+    const int end = s.mask ? s.nrows : s.nrows - s.n_q + i + 1;        // (none from here on)
+    uint32_t w = 0xFFFFFFFFu;
+    if (s.mask) {
+        const int k = r0 - (s.nrows - s.mask_rows);
+        const uint32_t* m = s.mask + (long long)i * s.mask_words;
+        if (k >= 0) {
+            const int at = k >> 5;
+            const uint32_t lo = at < s.mask_words ? m[at] : 0u, hi = at + 1 < s.mask_words ? m[at + 1] : 0u;
+            w = __funnelshift_r(lo, hi, k);
+        } else if (k > -32) {
+            w = (m[0] << -k) | ((1u << -k) - 1u);
+        }
+    }
+    const int n = end - r0;
+    return n >= 32 ? w : n <= 0 ? 0u : w & ((1u << n) - 1u);
+}
+// The largest of |m| and 16 s over halves of words (bf16); NaNs are above everything.
+__device__ __forceinline__ uint32_t kt_reach(uint32_t s, uint32_t m) { return __vmaxu2(m & 0x7FFF7FFFu, s + 0x02000200u); }
+
+template <int DH>
+__global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_constant__ Kv4AttnArgs a) {
+    typedef KtSmem<DH> M;
+    constexpr int Q = DH / 32, KB = M::KB, H = Q / 2, TB = kv4_tile_bytes(DH), LDO = M::LDO;
+    extern __shared__ unsigned char kt_raw[];
+    // rows' codes; S^T of even and odd steps is there (and what goes with it); V is there; O^T is there, P and V may be overwritten
+    __shared__ u64 bars[KT_STAGES + 4];
+    __shared__ uint32_t s_tmem, s_poison[KT_COLS], s_nan[2][KT_ROWS];
+    __shared__ __align__(16) float2 s_fm[KT_COLS];                     // what a column's scores are to be multiplied with; its maximum less KT_LIFT
+    __shared__ float s_rk[2][KT_ROWS], s_fade[2], s_top[4][KT_COLS], s_fall[KT_COLS], s_L[KT_COLS], s_M[KT_COLS], s_R;
+    __shared__ uint32_t s_max[8];
+    __shared__ int s_has_nan[2];
+    unsigned char* sm = (unsigned char*)(((uintptr_t)kt_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t smem = kv4_saddr(sm), bar = kv4_saddr(bars), bar_s = bar + 8 * KT_STAGES, bar_v = bar_s + 16, bar_o = bar_v + 8;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int b = blockIdx.z, h = blockIdx.y / a.n_blocks, j0 = (blockIdx.y % a.n_blocks) * KT_COLS;
+    const int rank = blockIdx.x, S = gridDim.x;
+    if (tid < KT_STAGES + 4) {
+        const int n = tid < KT_STAGES || tid == KT_STAGES + 3 ? 1 : tid < KT_STAGES + 2 ? 2 : KT_GROUP / 32;
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar + tid * 8), "r"(n) : "memory");
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");
+    if (tid < KT_COLS) s_poison[tid] = 0u;
+    if (tid == 0) s_R = 1.f;
+    if (warp == 0) {
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kv4_saddr(&s_tmem)), "r"(KT_TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // ones, for the sums of weights (head_dim 64: below the channels, so that they come with O^T)
+    for (int i = tid; i < (DH == 128 ? 256 : 1024); i += KT_THREADS)
+        *(uint4*)(sm + (DH == 128 ? M::ONES : M::V + 16384) + 16 * i) = make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u);
+    kt_fence_before();
+    __syncthreads();
+    kt_fence_after();
+    const uint32_t tmem = s_tmem;
+    pdl_wait();
+    pdl_trigger();
+    Kv4Sight sight;
+    sight.nrows = min(max(a.rows[b] + a.rows_add, 0), a.c.max_len);
+    sight.n_q = a.n_q; sight.mask_rows = a.mask_rows; sight.mask_words = a.mask_words;
+    sight.mask = a.mask ? a.mask + (long long)b * a.n_q * a.mask_words : nullptr;
+    const int i_first = j0 / a.G, i_last = (min(j0 + KT_COLS, a.ncol) - 1) / a.G;
+    // rows [0, clear) are visible to every column of the block, rows from `end` on to none
+    const int clear = max(0, a.mask ? sight.nrows - a.mask_rows : sight.nrows - a.n_q + i_first + 1);
+    const int end = max(0, a.mask ? sight.nrows : sight.nrows - a.n_q + i_last + 1);
+    const int ntile = (end + KV4_TILE - 1) / KV4_TILE, nstep = (ntile + KT_TILES - 1) / KT_TILES, nfull = clear / KT_ROWS;
+    const unsigned char* base = kv4_tile(a.c, a.sl.slot[b], h, 0);
+    auto fetch = [&](int t, int stage) {                               // (one thread)
+        kv4_fetch(smem + stage * M::RAW, base + (long long)t * M::RAW, (uint32_t)(min(KT_TILES, ntile - t * KT_TILES) * TB), bar + stage * 8);
+    };
+    if (tid == 0) {
+#pragma unroll
+        for (int i = 0; i < KT_STAGES; ++i)
+            if (rank + i * S < nstep) fetch(rank + i * S, i);
+    }
+    // ---- queries: a thread has a quarter of a column's channels; its row scaled by a power of two, so that bf16 is exact in fp16
+    if (tid < KT_GROUP) {
+        const int col = tid >> 2, c = tid & 3, j = j0 + col;
+        float x[Q][8], mx = 0.f;
+#pragma unroll
+        for (int w = 0; w < Q; ++w) {
+            if (j < a.ncol) {
+                kv4_load8<bf16>(a.q, (long long)(b * a.n_q + j / a.G) * a.q_ld + (h * a.G + j % a.G) * DH + 32 * w + 8 * c, x[w]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[w][i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[w][i]));
+        }
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const int e = mx > 0.f ? min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 100) : 0;
+        const float up = kv4_pow2(14 - e);
+        if (c == 0) s_fm[col] = make_float2(kv4_pow2(e - 14) * a.scale_log2, KV4_NOTHING);
+#pragma unroll
+        for (int w = 0; w < Q; ++w) {
+            const float* y = x[w];
+            const int chunk = (w & 1) * 4 + c;
+            *(uint4*)(sm + M::Q + (w >> 1) * 8192 + col * 128 + ((chunk ^ (col & 7)) << 4)) =
+                make_uint4(kv4_half2(y[0] * up, y[4] * up), kv4_half2(y[1] * up, y[5] * up), kv4_half2(y[2] * up, y[6] * up), kv4_half2(y[3] * up, y[7] * up));
+        }
+    }
+    kt_fence_smem();
+    __syncthreads();
+
+    bool ok = true;                        // (once a wait has run out, the others do not wait: the CTA comes to its end)
+    int n = 0;                             // steps taken
+    if (warp < KT_GROUP / 32) {
+        // ================ codes into values
+        float R = 0x1p112f;                                            // (the same in all threads)
+        uint32_t r_limit = (uint32_t)(127 - 98) << 7;                  // |m| and 16 s of the values stay below 2^14 / R
+        int stage = 0;
+        uint32_t parity = 0;
+        const __half2 sixteenth = __floats2half2_rn(0.0625f, 0.0625f);
+        for (int t = rank; t < nstep; t += S, ++n) {
+            if (ok) ok = kv4_wait(bar + stage * 8, parity);
+            const unsigned char* step = sm + stage * M::RAW;
+            const bool edge = t >= nfull;
+            // ---- keys: a thread has half the chunks of a row, neighbouring rows' at different places (no bank twice)
+            if (ok && n > 0) ok = kv4_wait(bar_s + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
+            {
+                const int r = tid & 127, c0 = (tid >> 7) * 2 + (r >> 1);
+                const unsigned char* tile = step + (r / KV4_TILE) * TB;
+                uint32_t p[Q], big = 0u;
+                kv4_lds<Q>(tile + kv4_s_at(DH, 0, r % KV4_TILE, 0), p);    // s of the groups two by two, then m
+#pragma unroll
+                for (int w = 0; w < H; ++w) big = __vmaxu2(big, kt_reach(p[w], p[H + w]));
+                const uint32_t top = max(big >> 16, big & 0xFFFFu);
+                const int e = min(max((int)(top >> 7) - 127, -98), 130);   // all are below 2^(e + 1); a NaN stays one
+                const float up = kv4_pow2(13 - e);
+                if (tid < KT_ROWS) s_rk[n & 1][r] = kv4_pow2(e - 13);
+                __half2 s1[Q], m1[Q];
+#pragma unroll
+                for (int w = 0; w < Q; ++w) {
+                    const float x = (w & 1 ? bf16_hi(p[w >> 1]) : bf16_lo(p[w >> 1])) * up, y = (w & 1 ? bf16_hi(p[H + (w >> 1)]) : bf16_lo(p[H + (w >> 1)])) * up;
+                    s1[w] = __floats2half2_rn(x, x);
+                    m1[w] = __floats2half2_rn(y, y);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int c = (c0 + i) & 3;
+                    uint32_t x[Q];
+                    kv4_lds<Q>(tile + kv4_k_at(DH, r % KV4_TILE, 0, c), x);
+#pragma unroll
+                    for (int w = 0; w < Q; ++w) {
+                        uint32_t v[4];
+                        kt_values(x[w], s1[w], __hmul2(s1[w], sixteenth), m1[w], v);
+                        *(uint4*)(sm + M::K + (w >> 1) * 16384 + r * 128 + ((((w & 1) * 4 + c) ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                }
+            }
+            // ---- the values' parameters: a thread has a pair of rows
+            const int pr = tid & 63, part = tid >> 6;
+            const unsigned char* vtile = step + (pr / (KV4_TILE / 2)) * TB;
+            uint32_t sw[Q], mw[Q], big = 0u;
+            kv4_lds<Q>(vtile + kv4_s_at(DH, 1, 2 * pr % KV4_TILE, 0), sw);
+            kv4_lds<Q>(vtile + kv4_m_at(DH, 1, 2 * pr % KV4_TILE, 0), mw);
+            if (edge) {
+                // nothing was fetched behind `end`
+                const int r = t * KT_ROWS + 2 * pr;
+                const uint32_t keep = r + 1 < end ? 0xFFFFFFFFu : r < end ? 0xFFFFu : 0u;
+#pragma unroll
+                for (int w = 0; w < Q; ++w) { sw[w] &= keep; mw[w] &= keep; }
+            }
+#pragma unroll
+            for (int w = 0; w < Q; ++w) big = __vmaxu2(big, kt_reach(sw[w], mw[w]));
+            kt_fence_smem();
+            float fade = 1.f;
+            const bool smaller = kt_sync_or<1>(max(big >> 16, big & 0xFFFFu) >= r_limit);
+            if (smaller) {
+                uint32_t fin = 0u, nan = 0u;                           // groups of the pair's rows that hold a NaN: bits w and 4 + w
+#pragma unroll
+                for (int w = 0; w < Q; ++w)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t x = (sw[w] >> (16 * i)) & 0xFFFFu, y = (mw[w] >> (16 * i)) & 0x7FFFu;
+                        if (x < 0x7F80u) fin = max(fin, max(x + 0x0200u, y));
+                        else nan |= 1u << (4 * i + w);
+                    }
+                fin = __reduce_max_sync(0xffffffffu, fin);
+                if (lane == 0) s_max[warp] = fin;
+                if (part == 0) {
+                    s_nan[n & 1][2 * pr] = nan & 15u;
+                    s_nan[n & 1][2 * pr + 1] = nan >> 4;
+                }
+                kt_sync<1>();
+#pragma unroll
+                for (int w = 0; w < 8; ++w) fin = max(fin, s_max[w]);
+                const int e = min(max((int)(fin >> 7) - 127, -98), 130);
+                const float r = kv4_pow2(13 - e);
+                if (r < R) {
+                    fade = r / R;
+                    R = r;
+                    r_limit = (uint32_t)(e + 1 + 127) << 7;
+                }
+                if (edge && nan) {
+                    // columns that do not see the row take nothing of it: left out here, put in where the probabilities are
+#pragma unroll
+                    for (int w = 0; w < Q; ++w) {
+                        const uint32_t keep = (nan >> w & 1u ? 0u : 0xFFFFu) | (nan >> (4 + w) & 1u ? 0u : 0xFFFF0000u);
+                        sw[w] &= keep;
+                        mw[w] &= keep;
+                    }
+                }
+            }
+            if (warp == 0 && kt_elect()) {
+                s_fade[n & 1] = fade;
+                s_has_nan[n & 1] = smaller && edge;
+                kt_fence_after();
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        kt_mma<true>(tmem + KT_S + (n & 1) * KT_COLS, kt_desc(smem + M::K + kb * 16384) + 2 * k, kt_desc(smem + M::Q + kb * 8192) + 2 * k, kb | k ? 1u : 0u);
+                kt_commit(bar_s + 8 * (n & 1));
+                kt_arrive(bar_s + 8 * (n & 1));
+                // the step before this one's codes have been read
+                if (n > 0 && t + (KT_STAGES - 1) * S < nstep) fetch(t + (KT_STAGES - 1) * S, stage == 0 ? KT_STAGES - 1 : stage - 1);
+            }
+            __syncwarp();
+            // ---- values: four channels of a group and of its neighbour, of two rows
+            __half2 s1[2][H], m1[2][H];
+#pragma unroll
+            for (int w = 0; w < H; ++w) {
+                s1[0][w] = __floats2half2_rn(bf16_lo(sw[2 * w]) * R, bf16_lo(sw[2 * w + 1]) * R);
+                s1[1][w] = __floats2half2_rn(bf16_hi(sw[2 * w]) * R, bf16_hi(sw[2 * w + 1]) * R);
+                m1[0][w] = __floats2half2_rn(bf16_lo(mw[2 * w]) * R, bf16_lo(mw[2 * w + 1]) * R);
+                m1[1][w] = __floats2half2_rn(bf16_hi(mw[2 * w]) * R, bf16_hi(mw[2 * w + 1]) * R);
+            }
+            if (ok && n > 0) ok = kv4_wait(bar_o, (n - 1) & 1);
+            const int swap = (pr & 4) | ((pr ^ (pr << 1)) & 2) | ((pr >> 1) & 1);    // the banks of eight pairs' loads differ, and of four pairs' stores
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int g = (2 * part + i) ^ swap;
+                uint32_t x[Q];
+                kv4_lds<Q>(vtile + kv4_v_at(DH, 2 * pr % KV4_TILE, 0, g), x);
+#pragma unroll
+                for (int w = 0; w < H; ++w)
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {
+                        uint32_t v[4];
+                        kt_values(__byte_perm(x[2 * w], x[2 * w + 1], o ? 0x7632 : 0x5410), s1[o][w], __hmul2(s1[o][w], sixteenth), m1[o][w], v);
+                        const int chunk = H * g + w, row = 2 * pr + o;
+                        *(uint4*)(sm + M::V + (chunk >> 3) * 16384 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+            }
+            kt_fence_smem();
+            __syncwarp();
+            if (lane == 0) kt_arrive(bar_v);
+            if (++stage == KT_STAGES) { stage = 0; parity ^= 1u; }
+        }
+        if (tid == 0) s_R = R;
+    } else {
+        // ================ scores into probabilities
+        const int quarter = warp & 3, half = (warp - KT_GROUP / 32) >> 2;
+        const uint32_t my_tmem = tmem + ((uint32_t)(quarter * 32) << 16) + half * 32;     // this warp's lanes, its half of the columns
+        const int row = quarter * 32 + lane;
+        for (int t = rank; t < nstep; t += S, ++n) {
+            if (ok) ok = kv4_wait(bar_s + 8 * (n & 1), (n >> 1) & 1);
+            kt_fence_after();
+            const float rk = s_rk[n & 1][row], fade = s_fade[n & 1];
+            float y[32], top = -INFINITY;                              // by how much scores are above the columns' maxima
+            uint32_t see = 0xFFFFFFFFu;
+            {
+                uint32_t raw[32];
+                kt_ld32(my_tmem + KT_S + (n & 1) * KT_COLS, raw);
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                    const float4 f = *(const float4*)(s_fm + half * 32 + i);
+                    y[i] = fmaf(__uint_as_float(raw[i]) * rk, f.x, -f.y);
+                    y[i + 1] = fmaf(__uint_as_float(raw[i + 1]) * rk, f.z, -f.w);
+                }
+            }
+            if (t >= nfull) {
+                const uint32_t mine = kt_window(sight, t * KT_ROWS + quarter * 32, min((j0 + half * 32 + lane) / a.G, a.n_q - 1));
+                see = 0u;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    see |= (__shfl_sync(0xffffffffu, mine, i) >> lane & 1u) << i;
+                    if (!(see >> i & 1u)) y[i] = -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
+            if (ok && n > 0) ok = kv4_wait(bar_o, (n - 1) & 1);        // P may be overwritten
+            if (kt_sync_or<2>(top > KV4_LAZY + KT_LIFT || fade != 1.f)) {
+                // the columns' maxima: lane L of the warp gets that of its column L, by halving what each lane has to compare
+                uint32_t raw[32];
+                kt_ld32(my_tmem + KT_S + (n & 1) * KT_COLS, raw);
+                float x[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    y[i] = __uint_as_float(raw[i]) * rk * s_fm[half * 32 + i].x;
+                    if (!(see >> i & 1u)) y[i] = -INFINITY;
+                    x[i] = y[i];
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    const bool high = (lane & o) != 0;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i < o) {
+                            const float keep = high ? x[i + o] : x[i], give = high ? x[i] : x[i + o];
+                            x[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, o));
+                        }
+                }
+                s_top[quarter][half * 32 + lane] = x[0];
+                kt_sync<2>();
+                if (tid < KT_GROUP + KT_COLS) {
+                    const int c = tid - KT_GROUP;
+                    const float old = s_fm[c].y, m = fmaxf(old, fmaxf(fmaxf(s_top[0][c], s_top[1][c]), fmaxf(s_top[2][c], s_top[3][c])) - KT_LIFT);
+                    s_fm[c].y = m;
+                    s_fall[c] = kv4_exp2(old - m);
+                }
+                kt_sync<2>();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) y[i] -= s_fm[half * 32 + i].y;
+                if (n > 0) {
+                    kt_fence_after();
+                    uint32_t o[32];
+                    kt_ld32(my_tmem + KT_O, o);
+                    const float f = DH == 64 && quarter >= 2 ? 1.f : fade;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * (s_fall[half * 32 + i] * f));
+                    kt_st32(my_tmem + KT_O, o);
+                    if (DH == 128) {
+                        kt_ld32(my_tmem + KT_L, o);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * s_fall[half * 32 + i]);
+                        kt_st32(my_tmem + KT_L, o);
+                    }
+                }
+            }
+            // ---- probabilities
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+                uint32_t v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = kv4_half2(kv4_exp2(y[i + 2 * k]), kv4_exp2(y[i + 2 * k + 1]));
+                const int chunk = half * 4 + i / 8;
+                *(uint4*)(sm + M::P + row * 128 + ((chunk ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+            if (s_has_nan[n & 1]) {
+                // rows that hold a NaN: every column that sees them has it in that group's channels
+                const uint32_t mine = s_nan[n & 1][row];
+                if (mine) {
+#pragma unroll 1
+                    for (int i = 0; i < 32; ++i)
+                        if (see >> i & 1u) atomicOr(&s_poison[half * 32 + i], mine);
+                }
+            }
+            kt_fence_smem();
+            kt_fence_before();
+            kt_sync<2>();
+            if (warp == KT_GROUP / 32) {
+                if (ok) ok = kv4_wait(bar_v, n & 1);
+                if (kt_elect()) {
+                    kt_fence_after();
+#pragma unroll
+                    for (int k = 0; k < KT_ROWS / 16; ++k) {
+                        const uint32_t more = n || k ? 1u : 0u;
+                        const u64 pd = kt_desc(smem + M::P) + 128 * k;
+                        kt_mma<false>(tmem + KT_O, kt_desc(smem + M::V, 16384) + 128 * k, pd, more);
+                        if (DH == 128) kt_mma<false>(tmem + KT_L, kt_desc(smem + M::ONES, 2048), pd, more);
+                    }
+                    kt_commit(bar_o);
+                }
+                __syncwarp();
+            }
+        }
+    }
+    // ---- the CTA's columns: maximum, sum, output
+    if (ok && n > 0) ok = kv4_wait(bar_o, (n - 1) & 1);
+    if (!ok) {
+        // a copy or a product has not come: time for what is in flight, and the result is NaN
+        const long long t0 = clock64();
+        while (clock64() - t0 < 4000000ll) {}
+    }
+    ok = __syncthreads_and(ok) != 0;
+    kt_fence_after();
+    float* sO = (float*)sm;
+    if (n == 0) {
+        // (no row at all: zeros)
+        for (int i = tid; i < KT_COLS * LDO; i += KT_THREADS) sO[i] = 0.f;
+        if (tid < KT_COLS) s_L[tid] = 0.f;
+    } else {
+        // a warp has a quarter of the lanes, 16 columns
+        const int quarter = warp & 3, col = (warp >> 2) * 16;
+        const float down = 1.f / s_R;
+        uint32_t o[16];
+        if (DH == 128 || quarter < 3) {
+            kt_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + col + KT_O, o);
+            const int at = quarter * 32 + lane, w = at % (4 * Q) / 8 * 2 + (at & 1), ch = 32 * w + at / (4 * Q) * 4 + (at >> 1 & 3);
+            if (at < DH) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    sO[(col + i) * LDO + ch] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * down;
+            }
+        }
+        if (quarter == (DH == 128 ? 0 : 2)) {
+            if (DH == 128) kt_ld16(tmem + col + KT_L, o);
+            if (lane == 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s_L[col + i] = __uint_as_float(o[i]);
+            }
+        }
+    }
+    kt_fence_before();
+    __syncthreads();
+    if (tid < KT_COLS) {
+        s_M[tid] = s_fm[tid].y;
+        if (!ok) s_L[tid] = __uint_as_float(0x7FC00000u);
+    }
+    if (warp == 0) {
+        __syncwarp();
+        kt_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(KT_TMEM) : "memory");
+    }
+    cg::cluster_group cluster = cg::this_cluster();
+    if (S > 1) cluster.sync();
+    else __syncthreads();
+    const int cols = min(KT_COLS, a.ncol - j0);
+    for (int i = rank * KT_THREADS + tid; i < cols * (DH / 4); i += S * KT_THREADS) {
+        const int col = i / (DH / 4), ch = (i % (DH / 4)) * 4;
+        float m = KV4_NOTHING, l = 0.f;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int r = 0; r < S; ++r) m = fmaxf(m, *(S > 1 ? cluster.map_shared_rank(s_M + col, r) : s_M + col));
+#pragma unroll 1
+        for (int r = 0; r < S; ++r) {
+            const float f = kv4_exp2(*(S > 1 ? cluster.map_shared_rank(s_M + col, r) : s_M + col) - m);
+            const float4 y = *(const float4*)(S > 1 ? cluster.map_shared_rank(sO + col * LDO + ch, r) : sO + col * LDO + ch);
+            l = fmaf(*(S > 1 ? cluster.map_shared_rank(s_L + col, r) : s_L + col), f, l);
+            x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+        }
+        kv4_put<bf16>(a, b, h, j0 + col, ch, DH, x, l);
+    }
+    if (S > 1) cluster.sync();          // nobody leaves while its shared memory may still be read
+}
+
+template <int DH>
+cudaError_t kt_launch(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
+    static bool attr_set[HIVIS_MAX_DEVICES] = {false};
+    auto kernel = kv4_tc_kernel<DH>;
+    if (dev < 0 || dev >= HIVIS_MAX_DEVICES || !attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, KtSmem<DH>::BYTES);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < HIVIS_MAX_DEVICES) attr_set[dev] = true;
+    }
+    a.n_blocks = (a.ncol + KT_COLS - 1) / KT_COLS;
+    const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, KT_ROWS, num_sms);
+    const dim3 grid((unsigned)S, (unsigned)(a.c.Hkv * a.n_blocks), (unsigned)a.sl.n);
+    return launch_cluster_pdl(kernel, S, grid, dim3(KT_THREADS), KtSmem<DH>::BYTES, st, a);
+}
+
+}  // namespace
+
+cudaError_t launch_kv4_attn_tc(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
+    return a.c.dh == 128 ? kt_launch<128>(a, dev, num_sms, st) : kt_launch<64>(a, dev, num_sms, st);
+}
