@@ -3,7 +3,7 @@
 // A CTA has 64 columns and takes 128 rows of the cache at a time:
 //   S^T [128 rows x 64 columns] = K Q^T      A = K's values, B = the queries, accumulators in tensor memory
 //   P^T = 2^(S^T f - m)                      a thread has one row and half the columns
-//   O^T [channels x 64] += V^T P^T           A = V's values, B = the probabilities; a column's sum of weights is one more product, of ones
+//   O^T [channels x 64] += V^T P^T           A = V's values, B = the probabilities
 // Eight warps take the codes apart, eight others have the probabilities: rows' values t + 1 are made while the probabilities of rows t
 // are.  Values m + s n are written as fp16 numbers (11 bits, like the probabilities; a bf16 result has 8) to shared memory in the
 // layouts that tcgen05.mma reads (rows of 128 bytes, 128-byte swizzle).  A word of K codes has eight channels of a row: 16 bytes of
@@ -23,19 +23,20 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int KT_COLS = 64, KT_ROWS = 128, KT_GROUP = 256, KT_THREADS = 2 * KT_GROUP, KT_STAGES = 3, KT_TILES = KT_ROWS / KV4_TILE;
-constexpr uint32_t KT_TMEM = 256;                                     // columns: S^T of two steps, O^T, the sums
+constexpr uint32_t KT_TMEM = 256;                                     // columns: S^T of two steps, O^T
 // Probabilities are held as 2^KT_LIFT p, below 2^15: fp16 has them to 2^-31 of a column's largest.
 #define KT_LIFT 7.f
-constexpr uint32_t KT_S = 0, KT_O = 128, KT_L = 192;
+constexpr uint32_t KT_S = 0, KT_O = 128;
 
 // Shared memory, every block 1024-byte aligned.  K: [64 channels a block][128 rows][128 bytes], Q: [64 channels a block][64][128 bytes];
-// V: [64 channels a block][128 rows][128 bytes] (head_dim 64: a block of channels, a block of ones), P: [128 rows][128 bytes].
+// V, two steps': [64 channels a block][128 rows][128 bytes] (head_dim 64: and a block of zeros, the products' other 64 rows);
+// P, two steps': [128 rows][128 bytes].
 template <int DH>
 struct KtSmem {
     static constexpr int KB = DH / 64;                                 // blocks of 64 channels
     static constexpr int RAW = KT_TILES * kv4_tile_bytes(DH);
-    static constexpr int K = KT_STAGES * RAW, V = K + KB * 16384, P = V + 2 * 16384, Q = P + 16384, ONES = Q + KB * 8192;
-    static constexpr int END = ONES + 4096;
+    static constexpr int K = KT_STAGES * RAW, V = K + KB * 16384, P = V + (DH == 128 ? 4 : 3) * 16384, Q = P + 2 * 16384;
+    static constexpr int END = Q + KB * 8192;
     static constexpr int LDO = DH + 4;
     static constexpr int BYTES = END + 1024;                           // (the base is aligned by hand)
     static_assert(RAW % 1024 == 0 && KT_COLS * LDO * 4 <= END && BYTES <= 227 * 1024, "layout");
@@ -105,14 +106,17 @@ __device__ __forceinline__ void kt_st32(uint32_t t, const uint32_t (&r)[32]) {
 __device__ __forceinline__ uint32_t kt_h2(const __half2& h) { return *(const uint32_t*)&h; }
 __device__ __forceinline__ __half2 kt_as_h2(uint32_t w) { return *(const __half2*)&w; }
 
-// The eight values of a word of codes, in the nibbles' order (0 and 4, 1 and 5, 2 and 6, 3 and 7), for s, s / 16 and m as pairs.
+// The eight values of a word of codes, in the nibbles' order (0 and 4, 1 and 5, 2 and 6, 3 and 7), for s 2^24, s 2^20 and m as pairs:
+// a code in an fp16's lowest bits is the subnormal n 2^-24, four bits further up 16 n 2^-24.
 __device__ __forceinline__ void kt_values(uint32_t x, const __half2& s, const __half2& s16, const __half2& m, uint32_t (&v)[4]) {
     const uint32_t y = x >> 8;
-    v[0] = kt_h2(__hfma2(kt_as_h2(kv4_lo<true>(x)), s, m));
-    v[1] = kt_h2(__hfma2(kt_as_h2(kv4_hi<true>(x)), s16, m));
-    v[2] = kt_h2(__hfma2(kt_as_h2(kv4_lo<true>(y)), s, m));
-    v[3] = kt_h2(__hfma2(kt_as_h2(kv4_hi<true>(y)), s16, m));
+    v[0] = kt_h2(__hfma2(kt_as_h2(kv4_lo<false>(x)), s, m));
+    v[1] = kt_h2(__hfma2(kt_as_h2(kv4_hi<false>(x)), s16, m));
+    v[2] = kt_h2(__hfma2(kt_as_h2(kv4_lo<false>(y)), s, m));
+    v[3] = kt_h2(__hfma2(kt_as_h2(kv4_hi<false>(y)), s16, m));
 }
+// 2^e, -149 <= e <= 127
+__device__ __forceinline__ float kt_pow2(int e) { return __uint_as_float(e < -126 ? 1u << (e + 149) : (uint32_t)(e + 127) << 23); }
 // Which of the 32 rows from r0 on query i sees.
 __device__ __forceinline__ uint32_t kt_window(const Kv4Sight& s, int r0, int i) {
     const int end = s.mask ? s.nrows : s.nrows - s.n_q + i + 1;        // (none from here on)
@@ -132,6 +136,7 @@ __device__ __forceinline__ uint32_t kt_window(const Kv4Sight& s, int r0, int i) 
     return n >= 32 ? w : n <= 0 ? 0u : w & ((1u << n) - 1u);
 }
 // The largest of |m| and 16 s over halves of words (bf16); NaNs are above everything.
+// Below 2^(e + 1), rows are scaled by 2^-(e + 6): values stay below 2^-4, s 2^24 below 2^15, and a value's rounding below 2^-20 of the largest.
 __device__ __forceinline__ uint32_t kt_reach(uint32_t s, uint32_t m) { return __vmaxu2(m & 0x7FFF7FFFu, s + 0x02000200u); }
 
 template <int DH>
@@ -139,34 +144,32 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     typedef KtSmem<DH> M;
     constexpr int Q = DH / 32, KB = M::KB, H = Q / 2, TB = kv4_tile_bytes(DH), LDO = M::LDO;
     extern __shared__ unsigned char kt_raw[];
-    // rows' codes; S^T of even and odd steps is there (and what goes with it); V is there; O^T is there, P and V may be overwritten
-    __shared__ u64 bars[KT_STAGES + 4];
+    // rows' codes; of even and odd steps: S^T is there (and what goes with it); V is there; O^T is there, P and V may be overwritten
+    __shared__ u64 bars[KT_STAGES + 6];
     __shared__ uint32_t s_tmem, s_poison[KT_COLS], s_nan[2][KT_ROWS];
     __shared__ __align__(16) float2 s_fm[KT_COLS];                     // what a column's scores are to be multiplied with; its maximum less KT_LIFT
-    __shared__ float s_rk[2][KT_ROWS], s_fade[2], s_top[4][KT_COLS], s_fall[KT_COLS], s_L[KT_COLS], s_M[KT_COLS], s_R;
+    __shared__ float s_rk[2][KT_ROWS], s_fade[2], s_top[4][KT_COLS], s_fall[KT_COLS], s_L[KT_COLS], s_M[KT_COLS];
     __shared__ uint32_t s_max[8];
-    __shared__ int s_has_nan[2];
+    __shared__ int s_has_nan[2], s_eV;
     unsigned char* sm = (unsigned char*)(((uintptr_t)kt_raw + 1023) & ~(uintptr_t)1023);
-    const uint32_t smem = kv4_saddr(sm), bar = kv4_saddr(bars), bar_s = bar + 8 * KT_STAGES, bar_v = bar_s + 16, bar_o = bar_v + 8;
+    const uint32_t smem = kv4_saddr(sm), bar = kv4_saddr(bars), bar_s = bar + 8 * KT_STAGES, bar_v = bar_s + 16, bar_o = bar_v + 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = blockIdx.z, h = blockIdx.y / a.n_blocks, j0 = (blockIdx.y % a.n_blocks) * KT_COLS;
     const int rank = blockIdx.x, S = gridDim.x;
-    if (tid < KT_STAGES + 4) {
-        const int n = tid < KT_STAGES || tid == KT_STAGES + 3 ? 1 : tid < KT_STAGES + 2 ? 2 : KT_GROUP / 32;
+    if (tid < KT_STAGES + 6) {
+        const int n = tid < KT_STAGES || tid >= KT_STAGES + 4 ? 1 : tid < KT_STAGES + 2 ? 2 : KT_GROUP / 32;
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar + tid * 8), "r"(n) : "memory");
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async;" ::: "memory");
     if (tid < KT_COLS) s_poison[tid] = 0u;
-    if (tid == 0) s_R = 1.f;
     if (warp == 0) {
         __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kv4_saddr(&s_tmem)), "r"(KT_TMEM) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    // ones, for the sums of weights (head_dim 64: below the channels, so that they come with O^T)
-    for (int i = tid; i < (DH == 128 ? 256 : 1024); i += KT_THREADS)
-        *(uint4*)(sm + (DH == 128 ? M::ONES : M::V + 16384) + 16 * i) = make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u);
+    if (DH == 64)
+        for (int i = tid; i < 1024; i += KT_THREADS) *(uint4*)(sm + M::V + 2 * 16384 + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
     kt_fence_before();
     __syncthreads();
     kt_fence_after();
@@ -210,7 +213,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         const int e = mx > 0.f ? min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 100) : 0;
         const float up = kv4_pow2(14 - e);
-        if (c == 0) s_fm[col] = make_float2(kv4_pow2(e - 14) * a.scale_log2, KV4_NOTHING);
+        if (c == 0) s_fm[col] = make_float2(kv4_pow2(e + 2) * a.scale_log2, KV4_NOTHING);     // (2^-14 of the queries' scaling, 2^16 of the keys')
 #pragma unroll
         for (int w = 0; w < Q; ++w) {
             const float* y = x[w];
@@ -226,54 +229,58 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     int n = 0;                             // steps taken
     if (warp < KT_GROUP / 32) {
         // ================ codes into values
-        float R = 0x1p112f;                                            // (the same in all threads)
-        uint32_t r_limit = (uint32_t)(127 - 98) << 7;                  // |m| and 16 s of the values stay below 2^14 / R
+        int eV = -99;                                                  // |m| and 16 s of the values stay below 2^(eV + 1) (the same in all threads)
         int stage = 0;
         uint32_t parity = 0;
         const __half2 sixteenth = __floats2half2_rn(0.0625f, 0.0625f);
         for (int t = rank; t < nstep; t += S, ++n) {
             if (ok) ok = kv4_wait(bar + stage * 8, parity);
+            if (ok && n > 1) ok = kv4_wait(bar_o + 8 * (n & 1), ((n >> 1) - 1) & 1);
             const unsigned char* step = sm + stage * M::RAW;
             const bool edge = t >= nfull;
-            // ---- keys: a thread has half the chunks of a row, neighbouring rows' at different places (no bank twice)
-            if (ok && n > 0) ok = kv4_wait(bar_s + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
-            {
-                const int r = tid & 127, c0 = (tid >> 7) * 2 + (r >> 1);
-                const unsigned char* tile = step + (r / KV4_TILE) * TB;
-                uint32_t p[Q], big = 0u;
-                kv4_lds<Q>(tile + kv4_s_at(DH, 0, r % KV4_TILE, 0), p);    // s of the groups two by two, then m
+            // keys: a thread has half the chunks of a row, neighbouring rows' at different places (no bank twice); values: a quarter of the
+            // groups of four channels of a pair of rows, so that the banks of eight pairs' loads differ, and of four pairs' stores
+            const int r = tid & 127, c0 = (tid >> 7) * 2 + (r >> 1), pr = tid & 63, part = tid >> 6;
+            const int swap = (pr & 4) | ((pr ^ (pr << 1)) & 2) | ((pr >> 1) & 1);
+            const unsigned char *ktile = step + (r / KV4_TILE) * TB, *vtile = step + (pr / (KV4_TILE / 2)) * TB;
+            uint32_t kp[Q], kx[2][Q], sw[Q], mw[Q], vx[2][Q];
+            kv4_lds<Q>(ktile + kv4_s_at(DH, 0, r % KV4_TILE, 0), kp);      // s of the groups two by two, then m
+            kv4_lds<Q>(vtile + kv4_s_at(DH, 1, 2 * pr % KV4_TILE, 0), sw);
+            kv4_lds<Q>(vtile + kv4_m_at(DH, 1, 2 * pr % KV4_TILE, 0), mw);
 #pragma unroll
-                for (int w = 0; w < H; ++w) big = __vmaxu2(big, kt_reach(p[w], p[H + w]));
+            for (int i = 0; i < 2; ++i) {
+                kv4_lds<Q>(ktile + kv4_k_at(DH, r % KV4_TILE, 0, (c0 + i) & 3), kx[i]);
+                kv4_lds<Q>(vtile + kv4_v_at(DH, 2 * pr % KV4_TILE, 0, (2 * part + i) ^ swap), vx[i]);
+            }
+            // ---- keys
+            uint32_t big = 0u;
+            {
+#pragma unroll
+                for (int w = 0; w < H; ++w) big = __vmaxu2(big, kt_reach(kp[w], kp[H + w]));
                 const uint32_t top = max(big >> 16, big & 0xFFFFu);
                 const int e = min(max((int)(top >> 7) - 127, -98), 130);   // all are below 2^(e + 1); a NaN stays one
-                const float up = kv4_pow2(13 - e);
-                if (tid < KT_ROWS) s_rk[n & 1][r] = kv4_pow2(e - 13);
+                const float up = kt_pow2(-6 - e), up24 = kv4_pow2(18 - e);
+                if (tid < KT_ROWS) s_rk[n & 1][r] = kv4_pow2(e - 10);
                 __half2 s1[Q], m1[Q];
 #pragma unroll
                 for (int w = 0; w < Q; ++w) {
-                    const float x = (w & 1 ? bf16_hi(p[w >> 1]) : bf16_lo(p[w >> 1])) * up, y = (w & 1 ? bf16_hi(p[H + (w >> 1)]) : bf16_lo(p[H + (w >> 1)])) * up;
+                    const float x = (w & 1 ? bf16_hi(kp[w >> 1]) : bf16_lo(kp[w >> 1])) * up24, y = (w & 1 ? bf16_hi(kp[H + (w >> 1)]) : bf16_lo(kp[H + (w >> 1)])) * up;
                     s1[w] = __floats2half2_rn(x, x);
                     m1[w] = __floats2half2_rn(y, y);
                 }
+                if (ok && n > 0) ok = kv4_wait(bar_s + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int c = (c0 + i) & 3;
-                    uint32_t x[Q];
-                    kv4_lds<Q>(tile + kv4_k_at(DH, r % KV4_TILE, 0, c), x);
 #pragma unroll
                     for (int w = 0; w < Q; ++w) {
                         uint32_t v[4];
-                        kt_values(x[w], s1[w], __hmul2(s1[w], sixteenth), m1[w], v);
+                        kt_values(kx[i][w], s1[w], __hmul2(s1[w], sixteenth), m1[w], v);
                         *(uint4*)(sm + M::K + (w >> 1) * 16384 + r * 128 + ((((w & 1) * 4 + c) ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
             }
-            // ---- the values' parameters: a thread has a pair of rows
-            const int pr = tid & 63, part = tid >> 6;
-            const unsigned char* vtile = step + (pr / (KV4_TILE / 2)) * TB;
-            uint32_t sw[Q], mw[Q], big = 0u;
-            kv4_lds<Q>(vtile + kv4_s_at(DH, 1, 2 * pr % KV4_TILE, 0), sw);
-            kv4_lds<Q>(vtile + kv4_m_at(DH, 1, 2 * pr % KV4_TILE, 0), mw);
+            // ---- the values' parameters
             if (edge) {
                 // nothing was fetched behind `end`
                 const int r = t * KT_ROWS + 2 * pr;
@@ -282,10 +289,10 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 for (int w = 0; w < Q; ++w) { sw[w] &= keep; mw[w] &= keep; }
             }
 #pragma unroll
-            for (int w = 0; w < Q; ++w) big = __vmaxu2(big, kt_reach(sw[w], mw[w]));
+            for (int w = 0; w < Q; ++w) big = w ? __vmaxu2(big, kt_reach(sw[w], mw[w])) : kt_reach(sw[w], mw[w]);
             kt_fence_smem();
             float fade = 1.f;
-            const bool smaller = kt_sync_or<1>(max(big >> 16, big & 0xFFFFu) >= r_limit);
+            const bool smaller = kt_sync_or<1>(max(big >> 16, big & 0xFFFFu) >= (uint32_t)(eV + 1 + 127) << 7);
             if (smaller) {
                 uint32_t fin = 0u, nan = 0u;                           // groups of the pair's rows that hold a NaN: bits w and 4 + w
 #pragma unroll
@@ -306,11 +313,9 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
                 for (int w = 0; w < 8; ++w) fin = max(fin, s_max[w]);
                 const int e = min(max((int)(fin >> 7) - 127, -98), 130);
-                const float r = kv4_pow2(13 - e);
-                if (r < R) {
-                    fade = r / R;
-                    R = r;
-                    r_limit = (uint32_t)(e + 1 + 127) << 7;
+                if (e > eV) {
+                    fade = e - eV > 126 ? 0.f : kv4_pow2(eV - e);
+                    eV = e;
                 }
                 if (edge && nan) {
                     // columns that do not see the row take nothing of it: left out here, put in where the probabilities are
@@ -338,42 +343,43 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
             }
             __syncwarp();
             // ---- values: four channels of a group and of its neighbour, of two rows
+            const float R = kt_pow2(-6 - eV), R24 = kv4_pow2(18 - eV);
             __half2 s1[2][H], m1[2][H];
 #pragma unroll
             for (int w = 0; w < H; ++w) {
-                s1[0][w] = __floats2half2_rn(bf16_lo(sw[2 * w]) * R, bf16_lo(sw[2 * w + 1]) * R);
-                s1[1][w] = __floats2half2_rn(bf16_hi(sw[2 * w]) * R, bf16_hi(sw[2 * w + 1]) * R);
+                s1[0][w] = __floats2half2_rn(bf16_lo(sw[2 * w]) * R24, bf16_lo(sw[2 * w + 1]) * R24);
+                s1[1][w] = __floats2half2_rn(bf16_hi(sw[2 * w]) * R24, bf16_hi(sw[2 * w + 1]) * R24);
                 m1[0][w] = __floats2half2_rn(bf16_lo(mw[2 * w]) * R, bf16_lo(mw[2 * w + 1]) * R);
                 m1[1][w] = __floats2half2_rn(bf16_hi(mw[2 * w]) * R, bf16_hi(mw[2 * w + 1]) * R);
             }
-            if (ok && n > 0) ok = kv4_wait(bar_o, (n - 1) & 1);
-            const int swap = (pr & 4) | ((pr ^ (pr << 1)) & 2) | ((pr >> 1) & 1);    // the banks of eight pairs' loads differ, and of four pairs' stores
+            unsigned char* to = sm + M::V + (n & 1) * KB * 16384;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int g = (2 * part + i) ^ swap;
-                uint32_t x[Q];
-                kv4_lds<Q>(vtile + kv4_v_at(DH, 2 * pr % KV4_TILE, 0, g), x);
 #pragma unroll
                 for (int w = 0; w < H; ++w)
 #pragma unroll
                     for (int o = 0; o < 2; ++o) {
                         uint32_t v[4];
-                        kt_values(__byte_perm(x[2 * w], x[2 * w + 1], o ? 0x7632 : 0x5410), s1[o][w], __hmul2(s1[o][w], sixteenth), m1[o][w], v);
+                        kt_values(__byte_perm(vx[i][2 * w], vx[i][2 * w + 1], o ? 0x7632 : 0x5410), s1[o][w], __hmul2(s1[o][w], sixteenth), m1[o][w], v);
                         const int chunk = H * g + w, row = 2 * pr + o;
-                        *(uint4*)(sm + M::V + (chunk >> 3) * 16384 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *(uint4*)(to + (chunk >> 3) * 16384 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
             }
             kt_fence_smem();
             __syncwarp();
-            if (lane == 0) kt_arrive(bar_v);
+            if (lane == 0) kt_arrive(bar_v + 8 * (n & 1));
             if (++stage == KT_STAGES) { stage = 0; parity ^= 1u; }
         }
-        if (tid == 0) s_R = R;
+        if (tid == 0) s_eV = eV;
     } else {
         // ================ scores into probabilities
         const int quarter = warp & 3, half = (warp - KT_GROUP / 32) >> 2;
         const uint32_t my_tmem = tmem + ((uint32_t)(quarter * 32) << 16) + half * 32;     // this warp's lanes, its half of the columns
         const int row = quarter * 32 + lane;
+        float l[32];                                                   // sums of this row's weights, every 128th row's
+#pragma unroll
+        for (int i = 0; i < 32; ++i) l[i] = 0.f;
         for (int t = rank; t < nstep; t += S, ++n) {
             if (ok) ok = kv4_wait(bar_s + 8 * (n & 1), (n >> 1) & 1);
             kt_fence_after();
@@ -401,7 +407,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
             }
 #pragma unroll
             for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
-            if (ok && n > 0) ok = kv4_wait(bar_o, (n - 1) & 1);        // P may be overwritten
+            if (ok && n > 1) ok = kv4_wait(bar_o + 8 * (n & 1), ((n >> 1) - 1) & 1);       // P may be overwritten
             if (kt_sync_or<2>(top > KV4_LAZY + KT_LIFT || fade != 1.f)) {
                 // the columns' maxima: lane L of the warp gets that of its column L, by halving what each lane has to compare
                 uint32_t raw[32];
@@ -435,19 +441,17 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
                 for (int i = 0; i < 32; ++i) y[i] -= s_fm[half * 32 + i].y;
                 if (n > 0) {
+                    if (ok) ok = kv4_wait(bar_o + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
                     kt_fence_after();
                     uint32_t o[32];
                     kt_ld32(my_tmem + KT_O, o);
-                    const float f = DH == 64 && quarter >= 2 ? 1.f : fade;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * (s_fall[half * 32 + i] * f));
-                    kt_st32(my_tmem + KT_O, o);
-                    if (DH == 128) {
-                        kt_ld32(my_tmem + KT_L, o);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * s_fall[half * 32 + i]);
-                        kt_st32(my_tmem + KT_L, o);
+                    for (int i = 0; i < 32; ++i) {
+                        const float f = s_fall[half * 32 + i];
+                        l[i] *= f;
+                        o[i] = __float_as_uint(__uint_as_float(o[i]) * (f * fade));
                     }
+                    kt_st32(my_tmem + KT_O, o);
                 }
             }
             // ---- probabilities
@@ -455,9 +459,14 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
             for (int i = 0; i < 32; i += 8) {
                 uint32_t v[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = kv4_half2(kv4_exp2(y[i + 2 * k]), kv4_exp2(y[i + 2 * k + 1]));
+                for (int k = 0; k < 4; ++k) {
+                    const float p0 = kv4_exp2(y[i + 2 * k]), p1 = kv4_exp2(y[i + 2 * k + 1]);
+                    l[i + 2 * k] += p0;
+                    l[i + 2 * k + 1] += p1;
+                    v[k] = kv4_half2(p0, p1);
+                }
                 const int chunk = half * 4 + i / 8;
-                *(uint4*)(sm + M::P + row * 128 + ((chunk ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                *(uint4*)(sm + M::P + (n & 1) * 16384 + row * 128 + ((chunk ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
             }
             if (s_has_nan[n & 1]) {
                 // rows that hold a NaN: every column that sees them has it in that group's channels
@@ -472,24 +481,31 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
             kt_fence_before();
             kt_sync<2>();
             if (warp == KT_GROUP / 32) {
-                if (ok) ok = kv4_wait(bar_v, n & 1);
+                if (ok) ok = kv4_wait(bar_v + 8 * (n & 1), (n >> 1) & 1);
                 if (kt_elect()) {
                     kt_fence_after();
 #pragma unroll
-                    for (int k = 0; k < KT_ROWS / 16; ++k) {
-                        const uint32_t more = n || k ? 1u : 0u;
-                        const u64 pd = kt_desc(smem + M::P) + 128 * k;
-                        kt_mma<false>(tmem + KT_O, kt_desc(smem + M::V, 16384) + 128 * k, pd, more);
-                        if (DH == 128) kt_mma<false>(tmem + KT_L, kt_desc(smem + M::ONES, 2048), pd, more);
-                    }
-                    kt_commit(bar_o);
+                    for (int k = 0; k < KT_ROWS / 16; ++k)
+                        kt_mma<false>(tmem + KT_O, kt_desc(smem + M::V + (n & 1) * KB * 16384, DH == 64 ? (2 - (n & 1)) * 16384 : 16384) + 128 * k,
+                                      kt_desc(smem + M::P + (n & 1) * 16384) + 128 * k, n || k ? 1u : 0u);
+                    kt_commit(bar_o + 8 * (n & 1));
                 }
                 __syncwarp();
             }
         }
+        // the columns' sums, by halving
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const bool high = (lane & o) != 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < o) l[i] = (high ? l[i + o] : l[i]) + __shfl_xor_sync(0xffffffffu, high ? l[i] : l[i + o], o);
+        }
+        kt_sync<2>();
+        s_top[quarter][half * 32 + lane] = l[0];
     }
     // ---- the CTA's columns: maximum, sum, output
-    if (ok && n > 0) ok = kv4_wait(bar_o, (n - 1) & 1);
+    if (ok && n > 0) ok = kv4_wait(bar_o + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
     if (!ok) {
         // a copy or a product has not come: time for what is in flight, and the result is NaN
         const long long t0 = clock64();
@@ -501,34 +517,24 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     if (n == 0) {
         // (no row at all: zeros)
         for (int i = tid; i < KT_COLS * LDO; i += KT_THREADS) sO[i] = 0.f;
-        if (tid < KT_COLS) s_L[tid] = 0.f;
     } else {
         // a warp has a quarter of the lanes, 16 columns
         const int quarter = warp & 3, col = (warp >> 2) * 16;
-        const float down = 1.f / s_R;
+        const float down = kv4_pow2(s_eV - 10);                      // (and 2^16)
         uint32_t o[16];
-        if (DH == 128 || quarter < 3) {
+        if (quarter * 32 < DH) {
             kt_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + col + KT_O, o);
             const int at = quarter * 32 + lane, w = at % (4 * Q) / 8 * 2 + (at & 1), ch = 32 * w + at / (4 * Q) * 4 + (at >> 1 & 3);
-            if (at < DH) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    sO[(col + i) * LDO + ch] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * down;
-            }
-        }
-        if (quarter == (DH == 128 ? 0 : 2)) {
-            if (DH == 128) kt_ld16(tmem + col + KT_L, o);
-            if (lane == 0) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s_L[col + i] = __uint_as_float(o[i]);
-            }
+            for (int i = 0; i < 16; ++i)
+                sO[(col + i) * LDO + ch] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * 0x1p16f * down;
         }
     }
     kt_fence_before();
     __syncthreads();
     if (tid < KT_COLS) {
         s_M[tid] = s_fm[tid].y;
-        if (!ok) s_L[tid] = __uint_as_float(0x7FC00000u);
+        s_L[tid] = ok ? (s_top[0][tid] + s_top[1][tid]) + (s_top[2][tid] + s_top[3][tid]) : __uint_as_float(0x7FC00000u);
     }
     if (warp == 0) {
         __syncwarp();
