@@ -342,6 +342,13 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 if (n > 0 && t + (KT_STAGES - 1) * S < nstep) fetch(t + (KT_STAGES - 1) * S, stage == 0 ? KT_STAGES - 1 : stage - 1);
             }
             __syncwarp();
+            // (of eight pairs of rows, four start with the odd one: no bank twice)
+            const int flip = pr >> 2 & 1;
+#pragma unroll
+            for (int w = 0; w < Q; ++w) {
+                sw[w] = __byte_perm(sw[w], 0u, flip ? 0x1032 : 0x3210);
+                mw[w] = __byte_perm(mw[w], 0u, flip ? 0x1032 : 0x3210);
+            }
             // ---- values: four channels of a group and of its neighbour, of two rows
             const float R = kt_pow2(-6 - eV), R24 = kv4_pow2(18 - eV);
             __half2 s1[2][H], m1[2][H];
@@ -361,8 +368,8 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
                     for (int o = 0; o < 2; ++o) {
                         uint32_t v[4];
-                        kt_values(__byte_perm(vx[i][2 * w], vx[i][2 * w + 1], o ? 0x7632 : 0x5410), s1[o][w], __hmul2(s1[o][w], sixteenth), m1[o][w], v);
-                        const int chunk = H * g + w, row = 2 * pr + o;
+                        kt_values(__byte_perm(vx[i][2 * w], vx[i][2 * w + 1], o ^ flip ? 0x7632 : 0x5410), s1[o][w], __hmul2(s1[o][w], sixteenth), m1[o][w], v);
+                        const int chunk = H * g + w, row = 2 * pr + (o ^ flip);
                         *(uint4*)(to + (chunk >> 3) * 16384 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
             }
