@@ -12,6 +12,15 @@
 // of the cache to 128 bytes, and the results' channels put in order when they leave.
 // Keys are scaled by a power of two of their row (which the row's scores undo), values by one of the CTA, R, so that fp16's range
 // holds them; probabilities are written for a running maximum that is raised once a score is above it by 2^8.
+//
+// What bounds it: 64 sequences x 4 KV heads x 56 columns of 4096 rows take 139 us, 216 TFLOP/s, and 64 columns as long as 17: about 3500
+// cycles go by for 128 rows, of which the codes' warps (two to a scheduler) are busy all the time and the others two thirds.  Shared memory
+// is in use for half of them: values and probabilities are written once (640 cycles) and read by the products at 128 bytes a cycle (16 of
+// 6 KB: 790).  What was measured on the way: one group of eight warps that does everything in turn 238 us; two groups 161; keys' codes as
+// subnormal factors and all loads before all stores 152; sums of weights added up beside the probabilities instead of a product with ones,
+// and two steps' P and V in shared memory, 134; stores without bank conflicts 131; values' codes as whole numbers, for rows far below the
+// largest, 137.  Products started by other warps than now are no help: by the probabilities' 142, by warps of their own, which leave the
+// others fewer registers, 139 instead of 131.
 #include <cstring>
 
 #include <cooperative_groups.h>
@@ -22,7 +31,7 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int KT_COLS = 64, KT_ROWS = 128, KT_GROUP = 256, KT_THREADS = 2 * KT_GROUP, KT_STAGES = 3, KT_TILES = KT_ROWS / KV4_TILE;
+constexpr int KT_COLS = 64, KT_ROWS = 128, KT_GROUP = 256, KT_THREADS = 2 * KT_GROUP, KT_STAGES = 3, KT_CLUSTER = 8, KT_TILES = KT_ROWS / KV4_TILE;
 constexpr uint32_t KT_TMEM = 256;                                     // columns: S^T of two steps, O^T
 // Probabilities are held as 2^KT_LIFT p, below 2^15: fp16 has them to 2^-31 of a column's largest.
 #define KT_LIFT 7.f
@@ -106,14 +115,15 @@ __device__ __forceinline__ void kt_st32(uint32_t t, const uint32_t (&r)[32]) {
 __device__ __forceinline__ uint32_t kt_h2(const __half2& h) { return *(const uint32_t*)&h; }
 __device__ __forceinline__ __half2 kt_as_h2(uint32_t w) { return *(const __half2*)&w; }
 
-// The eight values of a word of codes, in the nibbles' order (0 and 4, 1 and 5, 2 and 6, 3 and 7), for s 2^24, s 2^20 and m as pairs:
-// a code in an fp16's lowest bits is the subnormal n 2^-24, four bits further up 16 n 2^-24.
+// The eight values of a word of codes, in the nibbles' order (0 and 4, 1 and 5, 2 and 6, 3 and 7), for s, s / 16 and m as pairs.
+// Not WHOLE: a code in an fp16's lowest bits is the subnormal n 2^-24, four bits further up 16 n 2^-24, and s has 2^24 in it.
+template <bool WHOLE>
 __device__ __forceinline__ void kt_values(uint32_t x, const __half2& s, const __half2& s16, const __half2& m, uint32_t (&v)[4]) {
     const uint32_t y = x >> 8;
-    v[0] = kt_h2(__hfma2(kt_as_h2(kv4_lo<false>(x)), s, m));
-    v[1] = kt_h2(__hfma2(kt_as_h2(kv4_hi<false>(x)), s16, m));
-    v[2] = kt_h2(__hfma2(kt_as_h2(kv4_lo<false>(y)), s, m));
-    v[3] = kt_h2(__hfma2(kt_as_h2(kv4_hi<false>(y)), s16, m));
+    v[0] = kt_h2(__hfma2(kt_as_h2(kv4_lo<WHOLE>(x)), s, m));
+    v[1] = kt_h2(__hfma2(kt_as_h2(kv4_hi<WHOLE>(x)), s16, m));
+    v[2] = kt_h2(__hfma2(kt_as_h2(kv4_lo<WHOLE>(y)), s, m));
+    v[3] = kt_h2(__hfma2(kt_as_h2(kv4_hi<WHOLE>(y)), s16, m));
 }
 // 2^e, -149 <= e <= 127
 __device__ __forceinline__ float kt_pow2(int e) { return __uint_as_float(e < -126 ? 1u << (e + 149) : (uint32_t)(e + 127) << 23); }
@@ -136,7 +146,8 @@ __device__ __forceinline__ uint32_t kt_window(const Kv4Sight& s, int r0, int i) 
     return n >= 32 ? w : n <= 0 ? 0u : w & ((1u << n) - 1u);
 }
 // The largest of |m| and 16 s over halves of words (bf16); NaNs are above everything.
-// Below 2^(e + 1), rows are scaled by 2^-(e + 6): values stay below 2^-4, s 2^24 below 2^15, and a value's rounding below 2^-20 of the largest.
+// Below 2^(e + 1), keys are scaled by 2^-(e + 6): they stay below 2^-4, s 2^24 below 2^15, and a rounding is 2^-20 of its row's largest at
+// most, or half a step of its own.  Values, whose scale R all rows of a CTA share, by 2^(13 - e): below 2^15, roundings 2^-38 of the largest.
 __device__ __forceinline__ uint32_t kt_reach(uint32_t s, uint32_t m) { return __vmaxu2(m & 0x7FFF7FFFu, s + 0x02000200u); }
 
 template <int DH>
@@ -148,6 +159,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     __shared__ u64 bars[KT_STAGES + 6];
     __shared__ uint32_t s_tmem, s_poison[KT_COLS], s_nan[2][KT_ROWS];
     __shared__ __align__(16) float2 s_fm[KT_COLS];                     // what a column's scores are to be multiplied with; its maximum less KT_LIFT
+    __shared__ float2 s_part[KT_CLUSTER][KT_COLS];
     __shared__ float s_rk[2][KT_ROWS], s_fade[2], s_top[4][KT_COLS], s_fall[KT_COLS], s_L[KT_COLS], s_M[KT_COLS];
     __shared__ uint32_t s_max[8];
     __shared__ int s_has_nan[2], s_eV;
@@ -275,7 +287,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
                     for (int w = 0; w < Q; ++w) {
                         uint32_t v[4];
-                        kt_values(kx[i][w], s1[w], __hmul2(s1[w], sixteenth), m1[w], v);
+                        kt_values<false>(kx[i][w], s1[w], __hmul2(s1[w], sixteenth), m1[w], v);
                         *(uint4*)(sm + M::K + (w >> 1) * 16384 + r * 128 + ((((w & 1) * 4 + c) ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
@@ -350,12 +362,12 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 mw[w] = __byte_perm(mw[w], 0u, flip ? 0x1032 : 0x3210);
             }
             // ---- values: four channels of a group and of its neighbour, of two rows
-            const float R = kt_pow2(-6 - eV), R24 = kv4_pow2(18 - eV);
+            const float R = kv4_pow2(13 - eV);
             __half2 s1[2][H], m1[2][H];
 #pragma unroll
             for (int w = 0; w < H; ++w) {
-                s1[0][w] = __floats2half2_rn(bf16_lo(sw[2 * w]) * R24, bf16_lo(sw[2 * w + 1]) * R24);
-                s1[1][w] = __floats2half2_rn(bf16_hi(sw[2 * w]) * R24, bf16_hi(sw[2 * w + 1]) * R24);
+                s1[0][w] = __floats2half2_rn(bf16_lo(sw[2 * w]) * R, bf16_lo(sw[2 * w + 1]) * R);
+                s1[1][w] = __floats2half2_rn(bf16_hi(sw[2 * w]) * R, bf16_hi(sw[2 * w + 1]) * R);
                 m1[0][w] = __floats2half2_rn(bf16_lo(mw[2 * w]) * R, bf16_lo(mw[2 * w + 1]) * R);
                 m1[1][w] = __floats2half2_rn(bf16_hi(mw[2 * w]) * R, bf16_hi(mw[2 * w + 1]) * R);
             }
@@ -368,7 +380,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
                     for (int o = 0; o < 2; ++o) {
                         uint32_t v[4];
-                        kt_values(__byte_perm(vx[i][2 * w], vx[i][2 * w + 1], o ^ flip ? 0x7632 : 0x5410), s1[o][w], __hmul2(s1[o][w], sixteenth), m1[o][w], v);
+                        kt_values<true>(__byte_perm(vx[i][2 * w], vx[i][2 * w + 1], o ^ flip ? 0x7632 : 0x5410), s1[o][w], __hmul2(s1[o][w], sixteenth), m1[o][w], v);
                         const int chunk = H * g + w, row = 2 * pr + (o ^ flip);
                         *(uint4*)(to + (chunk >> 3) * 16384 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
@@ -511,7 +523,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
         kt_sync<2>();
         s_top[quarter][half * 32 + lane] = l[0];
     }
-    // ---- the CTA's columns: maximum, sum, output
+    // ---- the CTA's columns: maximum, sum, output (over the sum before the scale is undone: a mean is no larger than its values)
     if (ok && n > 0) ok = kv4_wait(bar_o + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
     if (!ok) {
         // a copy or a product has not come: time for what is in flight, and the result is NaN
@@ -520,6 +532,11 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     }
     ok = __syncthreads_and(ok) != 0;
     kt_fence_after();
+    if (tid < KT_COLS) {
+        s_M[tid] = s_fm[tid].y;
+        s_L[tid] = ok ? (s_top[0][tid] + s_top[1][tid]) + (s_top[2][tid] + s_top[3][tid]) : __uint_as_float(0x7FC00000u);
+    }
+    __syncthreads();
     float* sO = (float*)sm;
     if (n == 0) {
         // (no row at all: zeros)
@@ -527,44 +544,47 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     } else {
         // a warp has a quarter of the lanes, 16 columns
         const int quarter = warp & 3, col = (warp >> 2) * 16;
-        const float down = kv4_pow2(s_eV - 10);                      // (and 2^16)
+        const float down = kv4_pow2(s_eV - 13);
         uint32_t o[16];
         if (quarter * 32 < DH) {
             kt_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + col + KT_O, o);
             const int at = quarter * 32 + lane, w = at % (4 * Q) / 8 * 2 + (at & 1), ch = 32 * w + at / (4 * Q) * 4 + (at >> 1 & 3);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                sO[(col + i) * LDO + ch] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * 0x1p16f * down;
+            for (int i = 0; i < 16; ++i) {
+                const float l = s_L[col + i], inv = l == 0.f ? 0.f : 1.f / l;      // nothing visible: zeros
+                sO[(col + i) * LDO + ch] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * inv * down;
+            }
         }
     }
     kt_fence_before();
     __syncthreads();
-    if (tid < KT_COLS) {
-        s_M[tid] = s_fm[tid].y;
-        s_L[tid] = ok ? (s_top[0][tid] + s_top[1][tid]) + (s_top[2][tid] + s_top[3][tid]) : __uint_as_float(0x7FC00000u);
-    }
     if (warp == 0) {
         __syncwarp();
         kt_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(KT_TMEM) : "memory");
     }
+    // ---- the CTAs of the cluster: every thread fetches one column's maximum and sum of one of them, then its share of the channels
     cg::cluster_group cluster = cg::this_cluster();
     if (S > 1) cluster.sync();
     else __syncthreads();
+    static_assert(KT_THREADS == KT_COLS * KT_CLUSTER, "a column of a CTA to a thread");
+    if (tid < S * KT_COLS) s_part[tid >> 6][tid & 63] = make_float2(*cluster.map_shared_rank(s_M + (tid & 63), tid >> 6), *cluster.map_shared_rank(s_L + (tid & 63), tid >> 6));
+    __syncthreads();
     const int cols = min(KT_COLS, a.ncol - j0);
     for (int i = rank * KT_THREADS + tid; i < cols * (DH / 4); i += S * KT_THREADS) {
         const int col = i / (DH / 4), ch = (i % (DH / 4)) * 4;
         float m = KV4_NOTHING, l = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int r = 0; r < S; ++r) m = fmaxf(m, *(S > 1 ? cluster.map_shared_rank(s_M + col, r) : s_M + col));
-#pragma unroll 1
+        for (int r = 0; r < S; ++r) m = fmaxf(m, s_part[r][col].x);
+        for (int r = 0; r < S; ++r) l = fmaf(s_part[r][col].y, kv4_exp2(s_part[r][col].x - m), l);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 4
         for (int r = 0; r < S; ++r) {
-            const float f = kv4_exp2(*(S > 1 ? cluster.map_shared_rank(s_M + col, r) : s_M + col) - m);
+            const float f = s_part[r][col].y * kv4_exp2(s_part[r][col].x - m) * inv;
             const float4 y = *(const float4*)(S > 1 ? cluster.map_shared_rank(sO + col * LDO + ch, r) : sO + col * LDO + ch);
-            l = fmaf(*(S > 1 ? cluster.map_shared_rank(s_L + col, r) : s_L + col), f, l);
             x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
         }
-        kv4_put<bf16>(a, b, h, j0 + col, ch, DH, x, l);
+        kv4_put<bf16>(a, b, h, j0 + col, ch, DH, x, 1.f);
     }
     if (S > 1) cluster.sync();          // nobody leaves while its shared memory may still be read
 }
@@ -580,7 +600,8 @@ cudaError_t kt_launch(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
         if (dev >= 0 && dev < HIVIS_MAX_DEVICES) attr_set[dev] = true;
     }
     a.n_blocks = (a.ncol + KT_COLS - 1) / KT_COLS;
-    const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, KT_ROWS, num_sms);
+    // a CTA has an SM to itself: sixteen would have to find a whole GPC free (8 x 64 columns of 2048 rows: 22 us, with eight 13)
+    const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, KT_ROWS, num_sms, KT_CLUSTER);
     const dim3 grid((unsigned)S, (unsigned)(a.c.Hkv * a.n_blocks), (unsigned)a.sl.n);
     return launch_cluster_pdl(kernel, S, grid, dim3(KT_THREADS), KtSmem<DH>::BYTES, st, a);
 }

@@ -3,8 +3,7 @@
 #include "kv4.cuh"
 
 #define KV4_MAX_CLUSTER 16
-#define KV4_TC_COLUMNS 16
-#define KV4_WAIT_LIMIT (1 << 22)     // polls of a copy's barrier before a warp gives up (each may suspend for a while)
+#define KV4_WAIT_LIMIT (1 << 20)     // polls of a barrier before a warp gives up (each may suspend for a while)
 
 struct Kv4AttnArgs {
     Kv4View c;
@@ -139,11 +138,11 @@ __device__ __forceinline__ void kv4_lds(const unsigned char* p, uint32_t (&w)[Q]
 
 // CTAs per (sequence, KV head, block of columns): as many as the GPU holds at once, but no more than the cache's full length has
 // steps for their warps.  Eight or sixteen, or less than eight: clusters of nine, say, leave a third of a GPC's places empty.
-inline int kv4_cluster(int units, int max_len, int step_rows, int resident) {
+inline int kv4_cluster(int units, int max_len, int step_rows, int resident, int largest = KV4_MAX_CLUSTER) {
     const int most = max_len / step_rows, want = resident / units;
     const int s = want < most ? want : most;
-    return s < 1 ? 1 : s < 8 ? s : s < KV4_MAX_CLUSTER ? 8 : KV4_MAX_CLUSTER;
+    return s < 1 ? 1 : s < 8 ? s : s < largest ? 8 : largest;
 }
 
-// bf16, more columns than KV4_TC_COLUMNS (kernels_kv4_tc.cu).
+// bf16, many columns (kernels_kv4_tc.cu).
 cudaError_t launch_kv4_attn_tc(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st);

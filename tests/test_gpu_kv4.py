@@ -467,3 +467,111 @@ def test_the_output_may_be_the_queries():
         want = f.cache.attention(f.q, f.rows, n_q=n_q)
         q = f.q.clone()
         assert t.equal(f.cache.attention(q, f.rows, n_q=n_q, out=q), want) and t.equal(q, want)
+
+
+# ---------------------------------------------------------------- many columns of bf16 queries (blocks of 64, 128 rows at a time)
+def _check_many(f, out, mask=None, mask_rows=0):
+    """Filled.check, and a score's error: its row's values are rounded to 11 bits, each by at most 2^-11 of itself.  As independent errors
+    of rms 2^-11 / sqrt(3) they add up to 6 * 2^-11 / sqrt(3) < 2^-9 of the root of the sum of the products' squares, six sigma; a weight,
+    and the sum that it is divided by, are off by as much."""
+    cu = _starts(f.lens)
+    got, q = _np(out).reshape(len(f.lens), f.n_q, f.Hkv * f.G, f.dh), _np(f.q).reshape(len(f.lens), f.n_q, -1, f.dh)
+    scale = f.dh ** -0.5
+    for b, L in enumerate(f.lens):
+        kq, vq = ref.quantise(_np(f.k[cu[b]:cu[b + 1]])), ref.quantise(_np(f.v[cu[b]:cu[b + 1]]))
+        see = ref.visible(L, f.n_q, None if mask is None else mask[b], mask_rows)
+        want, reach, _ = ref.attention(q[b], kq, vq, scale, see)
+        ds = np.zeros((f.n_q, f.Hkv * f.G, 1))
+        if L:
+            kk = np.repeat(ref.values(*kq), f.G, axis=1)
+            ds = 2.0 ** -9 * scale * np.sqrt(np.einsum("qhd,lhd->qhl", q[b] ** 2, kk ** 2)).max(-1, keepdims=True)
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -10 + 2.0 * np.expm1(ds)) * reach
+        d = np.abs(got[b] - want)
+        assert np.all(d <= tol + 1e-30), (b, L, float((d / (tol + 1e-30)).max()))
+
+
+@pytest.mark.parametrize("dh,Hkv,G,n_q", [(128, 2, 1, 17), (128, 1, 7, 8), (128, 1, 1, 64), (128, 1, 5, 64), (64, 1, 7, 7), (64, 2, 1, 64), (64, 1, 8, 33)])
+def test_many_columns_over_uneven_sequences(dh, Hkv, G, n_q):
+    f = Filled("bf16", dh, Hkv, G, [0, 1, 2, 15, 17, 63, 64, 65, 127, 128, 129, 200, 255, 257, 640, 1030], n_q, seed=dh + G + n_q)
+    f.put()
+    _check_many(f, f.cache.attention(f.q, f.rows, n_q=n_q))
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("max_len", [1024, 32768])
+@pytest.mark.parametrize("rising", [True, False])
+def test_many_columns_whose_scores_rise_and_fall(dh, max_len, rising):
+    """The running maximum and the values' scale change from step to step; max_len says how many CTAs share a sequence."""
+    t = _torch()
+    f = Filled("bf16", dh, 2, 1, [1024, 900, 385], 56, seed=31, max_len=max_len)
+    d = t.nn.functional.normalize(f.q[:56, 0].float().mean(0), dim=0)
+    cu = _starts(f.lens)
+    for b, n in enumerate(f.lens):
+        r = t.arange(n, device="cuda").float()
+        slope = r if rising else n - r
+        f.k[cu[b]:cu[b + 1]] = (f.k[cu[b]:cu[b + 1]].float() * 0.1 + (slope * 0.2)[:, None, None] * d).bfloat16()
+        f.v[cu[b]:cu[b + 1]] *= (10.0 ** ((r // 128) % 5 - 2))[:, None, None].bfloat16()
+    f.put()
+    _check_many(f, f.cache.attention(f.q, f.rows, n_q=56))
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("fill", [0xFF, 0x7F, 0x00])
+def test_many_columns_take_nothing_of_rows_they_do_not_see(dh, fill):
+    t = _torch()
+    f = Filled("bf16", dh, 1, 1, [0, 1, 60, 61, 127, 130, 300], 61, seed=37, fill=fill)
+    f.put()
+    _check_many(f, f.cache.attention(f.q, f.rows, n_q=61))
+    # a group of a row of values is NaN: those channels of the queries that see it, nothing else
+    for r in (0, 40, 255, 299):
+        f = Filled("bf16", dh, 1, 1, [300], 61, seed=41)
+        f.put()
+        clean = f.cache.attention(f.q, f.rows, n_q=61).reshape(61, dh)
+        f.v[r, 0, 32:] = math.nan
+        f.put()
+        out = f.cache.attention(f.q, f.rows, n_q=61).reshape(61, dh)
+        sees = t.arange(61, device="cuda") + 300 - 61 >= r
+        assert bool(out[sees][:, 32:].isnan().all()) and not bool(out[~sees].isnan().any()) and not bool(out[:, :32].isnan().any()), r
+        assert t.equal(out[~sees], clean[~sees])
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("mask_rows,lens", [(61, [61, 100, 10, 300]), (333, [333, 400, 20, 129]), (1024, [1000, 1024, 1, 0])])
+def test_many_columns_under_a_mask(dh, mask_rows, lens):
+    f = Filled("bf16", dh, 2, 1, lens, 61, seed=mask_rows)
+    f.put()
+    mask = f.rng.random((4, 61, mask_rows)) < 0.4
+    mask[:, 3] = False
+    mask[1, 5:9, : mask_rows // 2] = False
+    _check_many(f, f.cache.attention(f.q, f.rows, n_q=61, mask=_words(mask), mask_rows=mask_rows), mask, mask_rows)
+
+
+@pytest.mark.parametrize("scale_v", [1e-30, 1e-6, 1e6, 1e30, 1e37])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_many_columns_of_values_of_any_magnitude(dh, scale_v):
+    f = Filled("bf16", dh, 1, 1, [300], 61, seed=43)
+    f.v *= scale_v
+    f.put()
+    _check_many(f, f.cache.attention(f.q, f.rows, n_q=61))
+
+
+def test_many_columns_of_queries_of_any_size():
+    for q_std, spread in ((2.0 ** -60, 0.0), (30.0, 0.0), (1.0, 3.5), (8.0, 3.5)):
+        f = Filled("bf16", 128, 1, 4, [257, 40], 9, seed=44, q_std=q_std, spread=spread)
+        f.put()
+        _check_many(f, f.cache.attention(f.q, f.rows, n_q=9))
+
+
+def test_many_columns_of_strided_queries_and_outputs():
+    t = _torch()
+    f = Filled("bf16", 128, 2, 2, [500, 77], 20, seed=47)
+    f.put()
+    want = f.cache.attention(f.q, f.rows, n_q=20)
+    wide = t.full((40, 1024), 7.0, dtype=t.bfloat16, device="cuda")
+    wide[:, 256:768] = f.q.reshape(40, 512)
+    out = t.full((40, 1536), 3.0, dtype=t.bfloat16, device="cuda")
+    f.cache.attention(wide[:, 256:768].view(40, 4, 128), f.rows, n_q=20, out=out[:, 512:1024].view(40, 4, 128))
+    assert t.equal(out[:, 512:1024], want.reshape(40, 512))
+    assert bool((out[:, :512] == 3).all()) and bool((out[:, 1024:] == 3).all())
+    for _ in range(5):
+        assert t.equal(f.cache.attention(f.q, f.rows, n_q=20), want)
