@@ -46,7 +46,7 @@ struct KtSmem {
     static constexpr int RAW = KT_TILES * kv4_tile_bytes(DH);
     static constexpr int K = KT_STAGES * RAW, V = K + KB * 16384, P = V + (DH == 128 ? 4 : 3) * 16384, Q = P + 2 * 16384;
     static constexpr int END = Q + KB * 8192;
-    static constexpr int LDO = DH + 4;
+    static constexpr int LDO = DH + 32;                                // results: groups of channels 1024 / DH words apart, no bank twice
     static constexpr int BYTES = END + 1024;                           // (the base is aligned by hand)
     static_assert(RAW % 1024 == 0 && KT_COLS * LDO * 4 <= END && BYTES <= 227 * 1024, "layout");
 };
@@ -153,7 +153,7 @@ __device__ __forceinline__ uint32_t kt_reach(uint32_t s, uint32_t m) { return __
 template <int DH>
 __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_constant__ Kv4AttnArgs a) {
     typedef KtSmem<DH> M;
-    constexpr int Q = DH / 32, KB = M::KB, H = Q / 2, TB = kv4_tile_bytes(DH), LDO = M::LDO;
+    constexpr int APART = 1024 / DH, Q = DH / 32, KB = M::KB, H = Q / 2, TB = kv4_tile_bytes(DH), LDO = M::LDO;
     extern __shared__ unsigned char kt_raw[];
     // rows' codes; of even and odd steps: S^T is there (and what goes with it); V is there; O^T is there, P and V may be overwritten
     __shared__ u64 bars[KT_STAGES + 6];
@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float l = s_L[col + i], inv = l == 0.f ? 0.f : 1.f / l;      // nothing visible: zeros
-                sO[(col + i) * LDO + ch] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * inv * down;
+                sO[(col + i) * LDO + ch + APART * w] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * inv * down;
             }
         }
     }
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll 4
         for (int r = 0; r < S; ++r) {
             const float f = s_part[r][col].y * kv4_exp2(s_part[r][col].x - m) * inv;
-            const float4 y = *(const float4*)(S > 1 ? cluster.map_shared_rank(sO + col * LDO + ch, r) : sO + col * LDO + ch);
+            const float4 y = *(const float4*)(S > 1 ? cluster.map_shared_rank(sO + col * LDO + ch + ch / 32 * APART, r) : sO + col * LDO + ch + ch / 32 * APART);
             x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
         }
         kv4_put<bf16>(a, b, h, j0 + col, ch, DH, x, 1.f);
@@ -600,7 +600,7 @@ cudaError_t kt_launch(Kv4AttnArgs& a, int dev, int num_sms, cudaStream_t st) {
         if (dev >= 0 && dev < HIVIS_MAX_DEVICES) attr_set[dev] = true;
     }
     a.n_blocks = (a.ncol + KT_COLS - 1) / KT_COLS;
-    // a CTA has an SM to itself: sixteen would have to find a whole GPC free (8 x 64 columns of 2048 rows: 22 us, with eight 13)
+    // a CTA has an SM to itself: sixteen would have to find a whole GPC free (8 x 64 columns of 2048 rows: 24 us, with eight 12)
     const int S = kv4_cluster(a.sl.n * a.c.Hkv * a.n_blocks, a.c.max_len, KT_ROWS, num_sms, KT_CLUSTER);
     const dim3 grid((unsigned)S, (unsigned)(a.c.Hkv * a.n_blocks), (unsigned)a.sl.n);
     return launch_cluster_pdl(kernel, S, grid, dim3(KT_THREADS), KtSmem<DH>::BYTES, st, a);
