@@ -839,9 +839,10 @@ static cudaError_t kv4_launch_attn_n(Kv4AttnArgs& a, int dev, int num_sms, cudaS
         if (a.ncol <= 8) return kv4_launch_attn<DH, 1, T, 1, 4, 2>(a, dev, num_sms, st);
         return kv4_launch_attn<DH, 2, T, 1, 4, 2>(a, dev, num_sms, st);
     } else {
-        // Blocks of 64 columns, whose codes are taken apart once (kernels_kv4_tc.cu), or of 16 here.  64 sequences x 4 KV heads of 4096 rows, head_dim 128:
-        // 16 columns 124 against 95 us, 17 to 32 125 against 152, 64 127 against 242; 4 x 2048 rows: 17 columns 13.2 against 11.1, 64 14.4
-        // against 13.4.  head_dim 64, where taking apart is half the work, 32 x 8 of 2048 rows: 48 columns 65 against 56, 64 65 against 75.
+        // Blocks of 64 columns, whose codes are taken apart once (kernels_kv4_tc.cu), or of 16 here.  64 sequences x 4 KV heads of 4096 rows,
+        // head_dim 128: 16 columns 124 there, 95 us here, 17 to 32 131 and 152, 64 134 and 242; 32 heads of 2240 rows: 17 columns 19.7 and
+        // 18.3, 64 20.3 and 26.5; 4 heads of 2048 rows: 13.2 and 11.1, 13.8 and 13.4.  head_dim 64, where taking apart is half the work,
+        // 32 x 8 of 2048 rows: 48 columns 65 and 57, 64 67 and 75.
         if (std::is_same<T, bf16>::value && a.ncol > (DH == 128 ? 16 : 48)) return launch_kv4_attn_tc(a, dev, num_sms, st);
         if (a.ncol > 8) return kv4_launch_attn<DH, 2, T, 1, 4, 3>(a, dev, num_sms, st);
         // Few (sequence, KV head) pairs do not fill the GPU with clusters of 16: a warp then gets more registers (nothing spilled)

@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     __shared__ uint32_t s_tmem, s_poison[KT_COLS], s_nan[2][KT_ROWS];
     __shared__ __align__(16) float2 s_fm[KT_COLS];                     // what a column's scores are to be multiplied with; its maximum less KT_LIFT
     __shared__ float2 s_part[KT_CLUSTER][KT_COLS];
-    __shared__ float s_rk[2][KT_ROWS], s_fade[2], s_top[4][KT_COLS], s_fall[KT_COLS], s_L[KT_COLS], s_M[KT_COLS];
+    __shared__ float s_rk[2][KT_ROWS], s_fade[2], s_top[4][KT_COLS], s_fall[KT_COLS], s_inv[KT_COLS];
     __shared__ uint32_t s_max[8];
     __shared__ int s_has_nan[2], s_eV;
     unsigned char* sm = (unsigned char*)(((uintptr_t)kt_raw + 1023) & ~(uintptr_t)1023);
@@ -186,6 +186,8 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     __syncthreads();
     kt_fence_after();
     const uint32_t tmem = s_tmem;
+    // (waited for before the first access to another CTA's shared memory: all have started)
+    if (S > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     pdl_wait();
     pdl_trigger();
     Kv4Sight sight;
@@ -532,9 +534,15 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     }
     ok = __syncthreads_and(ok) != 0;
     kt_fence_after();
-    if (tid < KT_COLS) {
-        s_M[tid] = s_fm[tid].y;
-        s_L[tid] = ok ? (s_top[0][tid] + s_top[1][tid]) + (s_top[2][tid] + s_top[3][tid]) : __uint_as_float(0x7FC00000u);
+    // (every thread sends one column's maximum and sum to one of the cluster's CTAs)
+    cg::cluster_group cluster = cg::this_cluster();
+    static_assert(KT_THREADS == KT_COLS * KT_CLUSTER, "a column of a CTA to a thread");
+    if (S > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (tid < S * KT_COLS) {
+        const int col = tid % KT_COLS;
+        const float l = ok ? (s_top[0][col] + s_top[1][col]) + (s_top[2][col] + s_top[3][col]) : __uint_as_float(0x7FC00000u);
+        *(S > 1 ? cluster.map_shared_rank(&s_part[rank][col], tid / KT_COLS) : &s_part[0][col]) = make_float2(s_fm[col].y, l);
+        if (tid < KT_COLS) s_inv[col] = l == 0.f ? 0.f : 1.f / l;      // nothing visible: zeros
     }
     __syncthreads();
     float* sO = (float*)sm;
@@ -550,10 +558,8 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
             kt_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + col + KT_O, o);
             const int at = quarter * 32 + lane, w = at % (4 * Q) / 8 * 2 + (at & 1), ch = 32 * w + at / (4 * Q) * 4 + (at >> 1 & 3);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float l = s_L[col + i], inv = l == 0.f ? 0.f : 1.f / l;      // nothing visible: zeros
-                sO[(col + i) * LDO + ch + APART * w] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * inv * down;
-            }
+            for (int i = 0; i < 16; ++i)
+                sO[(col + i) * LDO + ch + APART * w] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * s_inv[col + i] * down;
         }
     }
     kt_fence_before();
@@ -563,13 +569,9 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
         kt_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(KT_TMEM) : "memory");
     }
-    // ---- the CTAs of the cluster: every thread fetches one column's maximum and sum of one of them, then its share of the channels
-    cg::cluster_group cluster = cg::this_cluster();
+    // ---- the CTAs of the cluster: each writes its share of the columns' channels
     if (S > 1) cluster.sync();
     else __syncthreads();
-    static_assert(KT_THREADS == KT_COLS * KT_CLUSTER, "a column of a CTA to a thread");
-    if (tid < S * KT_COLS) s_part[tid >> 6][tid & 63] = make_float2(*cluster.map_shared_rank(s_M + (tid & 63), tid >> 6), *cluster.map_shared_rank(s_L + (tid & 63), tid >> 6));
-    __syncthreads();
     const int cols = min(KT_COLS, a.ncol - j0);
     for (int i = rank * KT_THREADS + tid; i < cols * (DH / 4); i += S * KT_THREADS) {
         const int col = i / (DH / 4), ch = (i % (DH / 4)) * 4;
