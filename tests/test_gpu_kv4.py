@@ -575,3 +575,38 @@ def test_many_columns_of_strided_queries_and_outputs():
     assert bool((out[:, :512] == 3).all()) and bool((out[:, 1024:] == 3).all())
     for _ in range(5):
         assert t.equal(f.cache.attention(f.q, f.rows, n_q=20), want)
+
+
+def test_many_columns_on_two_streams_and_in_graphs():
+    """Calls that overlap on the GPU share nothing; a replayed call reads the lengths, queries and rows of its replay."""
+    t = _torch()
+    fs = [Filled("bf16", dh, 2, 1, [900, 31, 400], 61, seed=50 + dh) for dh in (64, 128)]
+    want = []
+    for f in fs:
+        f.put()
+        want.append(f.cache.attention(f.q, f.rows, n_q=61).clone())
+    graphs, outs, streams = [], [], [t.cuda.Stream(), t.cuda.Stream()]
+    for f, s in zip(fs, streams):
+        s.wait_stream(t.cuda.current_stream())
+        out = t.zeros_like(f.q)
+        g = t.cuda.CUDAGraph()
+        with t.cuda.graph(g, stream=s):
+            for _ in range(3):
+                f.cache.attention(f.q, f.rows, n_q=61, out=out)
+        graphs.append(g)
+        outs.append(out)
+    for _ in range(20):
+        for g, s in zip(graphs, streams):
+            with t.cuda.stream(s):
+                g.replay()
+    t.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert t.equal(o, w)
+    for f, g, o in zip(fs, graphs, outs):
+        f.lens = [123, 1, 0]
+        f.rows.copy_(_ints(f.lens))
+        f.q.mul_(0.5)
+        g.replay()
+        t.cuda.synchronize()
+        assert t.equal(o, f.cache.attention(f.q, f.rows, n_q=61))
+        assert bool((o.view(3, 61, -1)[2] == 0).all()) and bool((o.view(3, 61, -1)[1, :60] == 0).all())
