@@ -159,7 +159,8 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(const __grid_constant__
     }
 }
 
-// Read: a lane has four neighbouring channels of a row, so that a warp writes whole lines, and four rows.
+// Read: a lane has four neighbouring channels of a row, so that a warp writes whole lines, and four rows one after the other, whose
+// place is found once unless a tile or a sequence ends between them.
 #define KV4_READ_ROWS 4
 template <int DH>
 __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ Kv4RowsArgs a) {
@@ -168,24 +169,33 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ K
     pdl_trigger();
     const int l = threadIdx.x % LR, unit = threadIdx.x / LR, per = UNITS >> a.heads_log2;
     const int h = (blockIdx.y << a.heads_log2) + (unit & ((1 << a.heads_log2) - 1));
-    const int j0 = blockIdx.x * (per * KV4_READ_ROWS) + (unit >> a.heads_log2), total = a.cu.v[a.sl.n];
+    const int j0 = (blockIdx.x * per + (unit >> a.heads_log2)) * KV4_READ_ROWS, total = a.cu.v[a.sl.n];
     if (h >= a.c.Hkv || j0 >= total) return;
-    int b = kv4_owner(a.cu, a.sl.n, j0);
+    int b = kv4_owner(a.cu, a.sl.n, j0), last = 0, row = 0;
     const int w = l >> 3, at_k = kv4_k_at(DH, 0, w, (l >> 1) & 3) + 2 * (l & 1), at_v = kv4_v_at(DH, 0, w, l & 7);
     const long long head_stride = (long long)(a.c.max_len / KV4_TILE) * kv4_tile_bytes(DH);
+    const unsigned char* tile = nullptr;
     uint32_t kw[KV4_READ_ROWS], vw[KV4_READ_ROWS], p[KV4_READ_ROWS][4];
-    bool live[KV4_READ_ROWS];
+    bool live[KV4_READ_ROWS], inside = false;
 #pragma unroll
     for (int u = 0; u < KV4_READ_ROWS; ++u) {
-        const int j = j0 + u * per;
+        const int j = j0 + u;
         live[u] = j < total;
         if (!live[u]) break;
-        while (j >= a.cu.v[b + 1]) ++b;
-        const int start = a.start ? a.start[b] : a.start_host;
-        live[u] = start >= 0 && start < a.c.max_len && j - a.cu.v[b] < a.c.max_len - start;
+        if (u == 0 || j == last) {
+            while (j >= a.cu.v[b + 1]) ++b;
+            last = a.cu.v[b + 1];
+            const int start = a.start ? a.start[b] : a.start_host;
+            inside = start >= 0 && start < a.c.max_len;
+            row = start + (j - a.cu.v[b]);
+            tile = a.c.data + ((long long)a.sl.slot[b] * a.c.Hkv + h) * head_stride + (long long)(row / KV4_TILE) * kv4_tile_bytes(DH);
+        } else {
+            row += 1;
+            if (row % KV4_TILE == 0) tile += kv4_tile_bytes(DH);
+        }
+        live[u] = inside && row < a.c.max_len;
         if (!live[u]) continue;
-        const int row = start + (j - a.cu.v[b]), r = row % KV4_TILE;
-        const unsigned char* tile = a.c.data + ((long long)a.sl.slot[b] * a.c.Hkv + h) * head_stride + (long long)(row / KV4_TILE) * kv4_tile_bytes(DH);
+        const int r = row % KV4_TILE;
         auto half = [&](int at) { return (uint32_t)__ldg((const unsigned short*)(tile + at)); };
         kw[u] = half(at_k + r * (DH / 2));
         vw[u] = half(at_v + (r & ~1) * (DH / 2) + (r & 1) * 2);
@@ -200,7 +210,7 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ K
     };
 #pragma unroll
     for (int u = 0; u < KV4_READ_ROWS; ++u) {
-        const int j = j0 + u * per;
+        const int j = j0 + u;
         if (j >= total) break;
         if (!live[u]) continue;
         const long long o = ((long long)j * a.c.Hkv + h) * DH + 4 * l;
