@@ -73,9 +73,9 @@ __device__ __forceinline__ void kv4_store_row(const Kv4View& c, const Kv4Place& 
 
 // Append: a lane has one group of 32 channels of a row, first K's, then V's, so that nothing is shared but the words of the V codes,
 // which the two rows of a pair exchange (DH / 32 lanes further on).  The values are read twice, the second time from L1: for their
-// range, then eight at a time for their codes.  6144 rows of 32 heads, bf16: 62 us with 8 channels a lane and shuffles for the
-// groups (most of it went into finding the place and the parameters for too few values), 57 us with everything unrolled (a third
-// of that waiting for code).
+// range, then eight at a time for their codes.  6144 rows of 32 heads, bf16: 37 us (their bytes: 20), bound by issue slots; 62 us with
+// 8 channels a lane and shuffles for the groups (most of it went into finding the place and the parameters for too few values), 57 us
+// with everything unrolled (a third of that waiting for code), 47 us with values next to a tie decided in eight unrolled branches.
 template <int DH, typename T>
 __global__ void __launch_bounds__(128) kv4_append_kernel(const __grid_constant__ Kv4RowsArgs a) {
     constexpr int Q = DH / 32, UNITS = 128 / (2 * Q);
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(const __grid_constant__
 }
 
 // Read: a lane has four neighbouring channels of a row, so that a warp writes whole lines, and four rows one after the other, whose
-// place is found once unless a tile or a sequence ends between them.
+// place is found once unless a tile or a sequence ends between them: 42 us for the same rows (their bytes: 36), 46 with every place on its own.
 #define KV4_READ_ROWS 4
 template <int DH>
 __global__ void __launch_bounds__(256) kv4_read_kernel(const __grid_constant__ Kv4RowsArgs a) {

@@ -91,34 +91,45 @@ __device__ __forceinline__ u64 kv4_mul2(u64 a, u64 b) {
     return r;
 }
 
-// Codes of 8 values as 8 nibbles.  t = (x - m) / s comes from a product with an approximate reciprocal, off by less than 2^-18; where
-// it is nearer than 2^-17 to a tie (of bf16 values one in some hundreds is one) the exact form decides.
+__device__ __forceinline__ u64 kv4_fma2(u64 a, u64 b, u64 c) {
+    u64 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// Codes of 8 values as 8 nibbles.  t = (x - m) / s comes from a product with an approximate reciprocal, off by less than 2^-18, and n
+// is the integer next to it.  r = (x - m) - n s is exact but for what x - m lost, at most 2^-20 s: unless r is that near to s / 2 (a
+// tie: of bf16 values one in some hundreds is one), or beyond it, n is the code; otherwise the exact form decides.
 __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t params) {
     const float m = kv4_min(params), s = kv4_scale(params);
     uint32_t w = 0u;
     if (s >= 1e-30f) {
         constexpr float MAGIC = 12582912.f;                 // 1.5 * 2^23: the nearest integer in the low bits
-        float inv, off = 0.f, t[8], u[8];
+        const float lim = s * (0.5f - 0x1p-18f);
+        float inv, off = 0.f, r[8], u[8];
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
-        const u64 mm = kv4_pack2(-m, -m), ii = kv4_pack2(inv, inv), up = kv4_pack2(MAGIC, MAGIC), down = kv4_pack2(-MAGIC, -MAGIC),
-                  minus = kv4_pack2(-1.f, -1.f);
+        const u64 mm = kv4_pack2(-m, -m), ii = kv4_pack2(inv, inv), ss = kv4_pack2(-s, -s), up = kv4_pack2(MAGIC, MAGIC), down = kv4_pack2(-MAGIC, -MAGIC);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            const u64 tt = kv4_mul2(kv4_add2(kv4_pack2(x[i], x[i + 1]), mm), ii), uu = kv4_add2(tt, up);
-            float d0, d1;
-            kv4_unpack2(kv4_add2(tt, kv4_mul2(kv4_add2(uu, down), minus)), d0, d1);
-            off = fmaxf(off, fmaxf(fabsf(d0), fabsf(d1)));
-            kv4_unpack2(tt, t[i], t[i + 1]);
+            const u64 d = kv4_add2(kv4_pack2(x[i], x[i + 1]), mm), uu = kv4_add2(kv4_mul2(d, ii), up);
+            kv4_unpack2(kv4_fma2(kv4_add2(uu, down), ss, d), r[i], r[i + 1]);
             kv4_unpack2(uu, u[i], u[i + 1]);
+            off = fmaxf(off, fmaxf(fabsf(r[i]), fabsf(r[i + 1])));
         }
 #pragma unroll
         for (int i = 7; i >= 0; --i) w = w * 16u + __float_as_uint(u[i]);      // (0x4B400000 above n: together 0x3F400000 in 32 bits)
         w -= 0x3F400000u;
-        if (off > 0.5f - 0x1p-17f) {
+        if (off > lim) {
+            uint32_t which = 0u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float n = u[i] - MAGIC;
-                if (fabsf(t[i] - n) > 0.5f - 0x1p-17f) w = (w & ~(15u << (4 * i))) | (kv4_code_exact(x[i], m, s, n, 1.f) << (4 * i));
+            for (int i = 0; i < 8; ++i) which |= fabsf(r[i]) > lim ? 1u << i : 0u;
+#pragma unroll 1
+            for (; which; which &= which - 1u) {
+                const int i = __ffs((int)which) - 1;
+                float y = x[0];
+#pragma unroll
+                for (int k = 1; k < 8; ++k) y = i == k ? x[k] : y;
+                w = (w & ~(15u << (4 * i))) | (kv4_code_exact(y, m, s, (float)(w >> (4 * i) & 15u), 1.f) << (4 * i));
             }
         }
     } else if (s > 0.f) {
