@@ -56,7 +56,7 @@ __device__ __forceinline__ uint32_t kv4_group_params(const float (&x)[8]) {
 template <int DH>
 __device__ __forceinline__ void kv4_store_row(const Kv4View& c, const Kv4Place& p, bool live, const float (&k)[8], const float (&v)[8]) {
     const uint32_t kp = kv4_group_params(k), vp = kv4_group_params(v);
-    const uint32_t kw = kv4_codes8(k, kp), vw = kv4_codes8(v, vp);
+    const uint32_t kw = kv4_codes8<true>(k, kp), vw = kv4_codes8<true>(v, vp);
     if (!live) return;
     unsigned char* tile = kv4_tile(c, p.slot, p.h, p.row);
     const int r = p.row % KV4_TILE;
@@ -73,9 +73,10 @@ __device__ __forceinline__ void kv4_store_row(const Kv4View& c, const Kv4Place& 
 
 // Append: a lane has one group of 32 channels of a row, first K's, then V's, so that nothing is shared but the words of the V codes,
 // which the two rows of a pair exchange (DH / 32 lanes further on).  The values are read twice, the second time from L1: for their
-// range, then eight at a time for their codes.  6144 rows of 32 heads, bf16: 37 us (their bytes: 20), bound by issue slots; 62 us with
+// range, then eight at a time for their codes.  6144 rows of 32 heads, bf16: 35 us (their bytes: 20), bound by issue slots; 62 us with
 // 8 channels a lane and shuffles for the groups (most of it went into finding the place and the parameters for too few values), 57 us
-// with everything unrolled (a third of that waiting for code), 47 us with values next to a tie decided in eight unrolled branches.
+// with everything unrolled (a third of that waiting for code), 47 us with values next to a tie decided in eight unrolled branches, 37 us in a loop
+// that ties take too.
 template <int DH, typename T>
 __global__ void __launch_bounds__(128) kv4_append_kernel(const __grid_constant__ Kv4RowsArgs a) {
     constexpr int Q = DH / 32, UNITS = 128 / (2 * Q);
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(const __grid_constant__
             uint32_t codes = 0u;
             if (live) {
                 kv4_load8<T>(src, at + 8 * c, x);
-                codes = kv4_codes8(x, params);
+                codes = kv4_codes8<sizeof(T) == 2>(x, params);
             }
             if (which == 0) {
                 if (live) *(uint32_t*)(tile + kv4_k_at(DH, r, w, c)) = codes;

@@ -85,11 +85,6 @@ __device__ __forceinline__ u64 kv4_add2(u64 a, u64 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ u64 kv4_mul2(u64 a, u64 b) {
-    u64 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 
 __device__ __forceinline__ u64 kv4_fma2(u64 a, u64 b, u64 c) {
     u64 r;
@@ -98,23 +93,27 @@ __device__ __forceinline__ u64 kv4_fma2(u64 a, u64 b, u64 c) {
 }
 
 // Codes of 8 values as 8 nibbles.  t = (x - m) / s comes from a product with an approximate reciprocal, off by less than 2^-18, and n
-// is the integer next to it.  r = (x - m) - n s is exact but for what x - m lost, at most 2^-20 s: unless r is that near to s / 2 (a
-// tie: of bf16 values one in some hundreds is one), or beyond it, n is the code; otherwise the exact form decides.
+// is the integer next to t - 2^-17: never above the code, and at a tie the lower one.  r = (x - m) - n s is exact but for what x - m
+// lost, at most 2^-20 s, so that n is the code where r is below s / 2 by more than that.  Of bf16 values one in some hundreds is a tie:
+// r = s / 2 says so where x - m is exact, which it is if neither x nor m is below 2^-12 s (both are then multiples of 2^-20 s, and their
+// difference is below 2^4 s).  The exact form decides about what is left.  BF16: whether the values are bf16 numbers.
+template <bool BF16>
 __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t params) {
     const float m = kv4_min(params), s = kv4_scale(params);
     uint32_t w = 0u;
     if (s >= 1e-30f) {
         constexpr float MAGIC = 12582912.f;                 // 1.5 * 2^23: the nearest integer in the low bits
-        const float lim = s * (0.5f - 0x1p-18f);
+        const float lim = s * (0.5f - 0x1p-18f), half = 0.5f * s;
         float inv, off = 0.f, r[8], u[8];
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
-        const u64 mm = kv4_pack2(-m, -m), ii = kv4_pack2(inv, inv), ss = kv4_pack2(-s, -s), up = kv4_pack2(MAGIC, MAGIC), down = kv4_pack2(-MAGIC, -MAGIC);
+        const u64 mm = kv4_pack2(-m, -m), ii = kv4_pack2(inv, inv), ss = kv4_pack2(-s, -s), up = kv4_pack2(MAGIC, MAGIC), down = kv4_pack2(-MAGIC, -MAGIC),
+                  less = kv4_pack2(-0x1p-17f, -0x1p-17f);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            const u64 d = kv4_add2(kv4_pack2(x[i], x[i + 1]), mm), uu = kv4_add2(kv4_mul2(d, ii), up);
+            const u64 d = kv4_add2(kv4_pack2(x[i], x[i + 1]), mm), uu = kv4_add2(kv4_fma2(d, ii, less), up);
             kv4_unpack2(kv4_fma2(kv4_add2(uu, down), ss, d), r[i], r[i + 1]);
             kv4_unpack2(uu, u[i], u[i + 1]);
-            off = fmaxf(off, fmaxf(fabsf(r[i]), fabsf(r[i + 1])));
+            off = fmaxf(off, fmaxf(r[i], r[i + 1]));
         }
 #pragma unroll
         for (int i = 7; i >= 0; --i) w = w * 16u + __float_as_uint(u[i]);      // (0x4B400000 above n: together 0x3F400000 in 32 bits)
@@ -122,7 +121,17 @@ __device__ __forceinline__ uint32_t kv4_codes8(const float (&x)[8], uint32_t par
         if (off > lim) {
             uint32_t which = 0u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) which |= fabsf(r[i]) > lim ? 1u << i : 0u;
+            for (int i = 0; i < 8; ++i) which |= r[i] > lim ? 1u << i : 0u;
+            if (BF16) {
+                uint32_t ties = 0u;
+                float least = m == 0.f ? s : fabsf(m);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    ties |= r[i] == half ? 1u << i : 0u;
+                    least = fminf(least, fabsf(x[i]));
+                }
+                if (least >= s * 0x1p-12f) which &= ~ties;
+            }
 #pragma unroll 1
             for (; which; which &= which - 1u) {
                 const int i = __ffs((int)which) - 1;
@@ -165,7 +174,7 @@ __device__ __forceinline__ void kv4_store32(unsigned char* tile, int dh, int whi
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[8 * c + i];
-        const uint32_t codes = kv4_codes8(y, params);
+        const uint32_t codes = kv4_codes8<true>(y, params);
         if (which == 0) {
             *(uint32_t*)(tile + kv4_k_at(dh, r, w, c)) = codes;
         } else {

@@ -610,3 +610,29 @@ def test_many_columns_on_two_streams_and_in_graphs():
         t.cuda.synchronize()
         assert t.equal(o, f.cache.attention(f.q, f.rows, n_q=61))
         assert bool((o.view(3, 61, -1)[2] == 0).all()) and bool((o.view(3, 61, -1)[1, :60] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["halves", "eighths", "spread", "tiny beside large", "nearly ties"])
+def test_codes_of_values_beside_ties(dtype, kind):
+    """Half a million values of which many are ties, or a last bit away from one: the codes are those of exact arithmetic."""
+    t = _torch()
+    g = t.Generator(device="cuda").manual_seed(7)
+    shape = (1024, 4, 128)
+    x = t.randn(shape, device="cuda", generator=g)
+    if kind == "halves":
+        x = t.randint(0, 31, shape, device="cuda", generator=g).float() * 0.5
+    elif kind == "eighths":
+        x = (x * 8).round() / 8
+    elif kind == "spread":
+        x = x * t.exp2(t.randint(-20, 20, shape, device="cuda", generator=g).float())
+    elif kind == "tiny beside large":
+        x = t.where(t.rand(shape, device="cuda", generator=g) < 0.5, x * 1e-6, x)
+    else:
+        x = t.randint(-60, 61, shape, device="cuda", generator=g).float() * 2.0 ** -3 + x * 2.0 ** -14 * (t.rand(shape, device="cuda", generator=g) < 0.3)
+    x = x.to(t.bfloat16 if dtype == "bf16" else t.float32)
+    cache = _cache(1, 4, 128, 1024)
+    cache.append(x, x, [0, 1024], _ints([0]))
+    k, v = cache.read([0, 1024], _ints([0]))
+    want = ref.values(*ref.quantise(_np(x))).astype(np.float32)
+    assert np.array_equal(k.cpu().numpy(), want) and np.array_equal(v.cpu().numpy(), want)
