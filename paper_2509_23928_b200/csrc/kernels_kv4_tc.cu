@@ -13,10 +13,10 @@
 // Keys are scaled by a power of two of their row (which the row's scores undo), values by one of the CTA, R, so that fp16's range
 // holds them; probabilities are written for a running maximum that is raised once a score is above it by 2^8.
 //
-// What bounds it: 64 sequences x 4 KV heads x 56 columns of 4096 rows take 139 us, 216 TFLOP/s, and 64 columns as long as 17: about 3500
+// What bounds it: 64 sequences x 4 KV heads x 56 columns of 4096 rows take 136 us, 222 TFLOP/s, and 64 columns as long as 17: about 3500
 // cycles go by for 128 rows, of which the codes' warps (two to a scheduler) are busy all the time and the others two thirds.  Shared memory
-// is in use for half of them: values and probabilities are written once (640 cycles) and read by the products at 128 bytes a cycle (16 of
-// 6 KB: 790).  What was measured on the way: one group of eight warps that does everything in turn 238 us; two groups 161; keys' codes as
+// is in use for some 2500 of them: values and probabilities are written (640), read by the products at 128 bytes a cycle (16 of
+// 6 KB: 790), codes, parameters and columns' scales read by the warps.  What was measured on the way: one group of eight warps that does everything in turn 238 us; two groups 161; keys' codes as
 // subnormal factors and all loads before all stores 152; sums of weights added up beside the probabilities instead of a product with ones,
 // and two steps' P and V in shared memory, 134; stores without bank conflicts 131; values' codes as whole numbers, for rows far below the
 // largest, 137.  Products started by other warps than now are no help: by the probabilities' 142, by warps of their own, which leave the
