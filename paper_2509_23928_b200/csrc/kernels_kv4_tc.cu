@@ -352,8 +352,8 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                         kt_mma<true>(tmem + KT_S + (n & 1) * KT_COLS, kt_desc(smem + M::K + kb * 16384) + 2 * k, kt_desc(smem + M::Q + kb * 8192) + 2 * k, kb | k ? 1u : 0u);
                 kt_commit(bar_s + 8 * (n & 1));
                 kt_arrive(bar_s + 8 * (n & 1));
-                // the step before this one's codes have been read
-                if (n > 0 && t + (KT_STAGES - 1) * S < nstep) fetch(t + (KT_STAGES - 1) * S, stage == 0 ? KT_STAGES - 1 : stage - 1);
+                // the step before this one's codes have been read (if they have not come, their barrier takes no second arrival)
+                if (ok && n > 0 && t + (KT_STAGES - 1) * S < nstep) fetch(t + (KT_STAGES - 1) * S, stage == 0 ? KT_STAGES - 1 : stage - 1);
             }
             __syncwarp();
             // (of eight pairs of rows, four start with the odd one: no bank twice)
