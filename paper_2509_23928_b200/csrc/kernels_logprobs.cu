@@ -30,6 +30,7 @@ struct LogprobArgs {
     long long ld;
     int n_rows, V;
     float scale;                  // log2(e) / T
+    uint32_t low;                 // bf16: a pair of the number that stands for -infinity in the sums
     const int32_t* ids;           // nullable
     int n_ids, top_n;
     float *out_lp, *out_h, *out_top_lp;     // nullable
@@ -110,15 +111,16 @@ __device__ __forceinline__ float lp_most(const uint4 (&v)[U]) {
         return m;
     }
 }
-// The sums of some vectors' logits.  A logit of -infinity counts as one of -1e30, so that 2^y y is 0 and no NaN.
+// The sums of some vectors' logits.  y stays finite, so that 2^y y of a logit of -infinity is 0 and no NaN: a clamp of y, and for bf16 of
+// the logits, two at a time, to a number `low` that is without mass at any reference (lp_low).
 template <typename T, int U>
-__device__ __forceinline__ void lp_add(LpSum& s, const uint4 (&v)[U], float scale) {
+__device__ __forceinline__ void lp_add(LpSum& s, const uint4 (&v)[U], float scale, uint32_t low2) {
     constexpr int N = LpVec<T>::N;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         float x[N];
         if constexpr (sizeof(T) == 2) {
-            const __nv_bfloat162 low = __float2bfloat162_rn(-1e30f);
+            const __nv_bfloat162 low = lp_bf2(low2);
             const uint4 t = make_uint4(lp_w(__hmax2_nan(lp_bf2(v[u].x), low)), lp_w(__hmax2_nan(lp_bf2(v[u].y), low)),
                                        lp_w(__hmax2_nan(lp_bf2(v[u].z), low)), lp_w(__hmax2_nan(lp_bf2(v[u].w), low)));
             lp_values<T>(t, x);
@@ -238,7 +240,7 @@ __global__ void __launch_bounds__(LpVec<T>::THREADS, 1024 / LpVec<T>::THREADS) l
             lp_lower(s.z, s.w, c - s.c);
             s.c = c;
         }
-        lp_add<T>(s, v, a.scale);
+        lp_add<T>(s, v, a.scale, a.low);
     }
     // ---- the CTA's sums
     {
@@ -406,6 +408,15 @@ __global__ void __launch_bounds__(LpVec<T>::THREADS, 1024 / LpVec<T>::THREADS) l
     if (S > 1) cluster.sync();
 }
 
+// For bf16: the logit that takes -infinity's place, as a pair.  scale * low has to be finite (1e37) and so far below every reference, which is
+// -LP_FAR at least, that 2^y is 0: at the smallest scale that is taken (T below 1e30) -3.3e38 comes to -4.7e8, LP_FAR is 2.7e8.  A finite
+// logit below it is as far from the largest one, or its CTA goes over its part again relative to that one.
+static uint32_t lp_low(float scale) {
+    const double most = 1e37 / (double)scale;
+    const uint32_t b = __bfloat16_as_ushort(__float2bfloat16((float)(most < 3.3e38 ? -most : -3.3e38)));
+    return b << 16 | b;
+}
+
 template <typename T, bool TOP>
 static cudaError_t lp_launch(LogprobArgs& a, int dev, int num_sms, cudaStream_t st) {
     auto kernel = logprob_kernel<T, TOP>;
@@ -455,6 +466,7 @@ extern "C" int hivis_logprobs(int n_rows, int vocab, const void* logits, int log
     memset(&a, 0, sizeof(a));
     a.logits = logits; a.ld = ld; a.n_rows = n_rows; a.V = vocab;
     a.scale = (float)(1.4426950408889634 / (double)temperature);
+    a.low = lp_low(a.scale);
     a.ids = ids; a.n_ids = n_ids; a.top_n = top_n;
     a.out_lp = n_ids > 0 ? out_logprobs : nullptr; a.out_h = out_entropy; a.out_top = out_top_ids; a.out_top_lp = out_top_logprobs;
     int dev = 0, sms = 0;

@@ -234,3 +234,62 @@ def test_tensors_that_do_not_fit_are_refused():
     for kw in (dict(top_n=33), dict(temperature=0.0), dict(entropy=False)):
         with pytest.raises(HivisError):
             logprobs(x, **kw)
+
+
+# ------------------------------------------------------------------------------------------- every temperature that is taken
+def _check_far(x, ids, temperature, top_n, out):
+    """As _check, with bounds that go by a token's own distance from the row's largest logit: log2(e) / T is rounded to 2^-24 of itself, and
+    so is y, its distance in powers of two; the sums, of terms good to 2^-22, to 2^-19.  The entropy moves by that factor's error times
+    the variance of log p, which the mean of its square bounds."""
+    x = x.double().cpu().numpy()
+    # (distances from the largest logit first: beside x / T of 1e60 a logarithm is lost even in 64 bits)
+    top = np.where(np.isneginf(x).all(-1, keepdims=True), 0.0, x.max(-1, keepdims=True))
+    T = float(np.float32(temperature))
+    lp, h, tid, tlp = _want(x - top, ids.cpu().numpy(), T, top_n)
+    with np.errstate(all="ignore"):
+        for got, want in ((out.logprobs, lp), (out.top_logprobs, tlp)):
+            g = got.double().cpu().numpy()
+            below = want < -3.5e38                                   # beyond fp32's range, or without mass
+            assert np.all(np.isneginf(g[below])) and not np.isnan(g).any()
+            d = np.abs(g - want)[~below]
+            assert np.all(d <= 2.0 ** -19 + 2.0 ** -21 * np.abs(want[~below])), float(d.max())
+        got = out.entropy.double().cpu().numpy()
+        for r in range(x.shape[0]):
+            ok = x[r] > -np.inf
+            y = x[r, ok] / T
+            y = y - y.max() if ok.any() else y
+            p = np.exp(y) / np.exp(y).sum() if ok.any() else y
+            square = (p[p > 0] * np.log(p[p > 0]) ** 2).sum()
+            assert abs(got[r] - h[r]) <= 2.0 ** -18 * (1 + h[r]) + 2.0 ** -22 * square, (r, got[r], h[r])
+    assert np.array_equal(out.top_ids.cpu().numpy(), tid)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("temperature", [1.1e-30, 1e-29, 1e-20, 1e-12, 1e-9, 3e-9, 1e-3, 1e3, 1e8, 1e20, 1e22, 1e25, 1e28, 1e29, 9e29])
+@pytest.mark.parametrize("V,ld", [(200, 200), (5031, 6001), (50257, 50257)])
+def test_banned_tokens_at_any_temperature(dtype, temperature, V, ld):
+    """Rows whose largest logit is 0, next to 0 or far from it, with tokens at -infinity or at finite values as low."""
+    from paper_2509_23928_b200 import logprobs
+    t = _torch()
+    rng = np.random.default_rng(V)
+    lowest = float(t.finfo(t.bfloat16 if dtype == "bf16" else t.float32).min)
+    x = rng.standard_normal((12, ld)) * 4
+    x[:8] -= x[:8, :V].max(-1, keepdims=True)                        # rows of log-probabilities, nearly
+    some = rng.random(ld) < 0.4
+    x[0, some] = -np.inf
+    x[1, :V // 2] = -np.inf                                          # whole threads and whole CTAs without a token
+    x[2, V // 2:] = -np.inf
+    x[3, some] = lowest
+    x[4, some] = -1e30
+    x[5, 1::2] = -np.inf
+    x[6, 3:] = -np.inf                                               # three tokens are left
+    x[7, :V - 1] = -np.inf                                           # the last one alone
+    x[7, V - 1] = 0.05
+    x[8, some] = -np.inf
+    x[9] = -np.inf
+    x[10] = lowest                                                   # a row of the lowest value alone is flat
+    d = _to(x, dtype)
+    d[11, V // 2:] = lowest
+    d = d[:, :V]
+    ids = t.from_numpy(np.concatenate([rng.integers(0, V, (12, 3)), np.full((12, 1), V - 1), np.zeros((12, 1))], 1).astype(np.int32)).cuda()
+    _check_far(d, ids, temperature, 7, logprobs(d, ids, temperature=temperature, top_n=7))
