@@ -483,6 +483,11 @@ def _dtype(t) -> int:
     return _DTYPES[t.dtype]
 
 
+def _aligned(t):
+    """A tensor that is only read, starting on 16 bytes as the library wants it: itself, or a copy of a view that starts elsewhere."""
+    return t if t.data_ptr() % 16 == 0 else t.new_empty(t.shape).copy_(t)
+
+
 def _slots(slots, B):
     if slots is None:
         return None
@@ -499,7 +504,8 @@ def _raw_stream(index: int) -> int:
 
 class Kv4Cache:
     """A key/value cache held in 4 bits (include/hivis.h: hivis_kv4_cache) for `n_slots` sequences of up to `max_len` rows
-    (rounded up to a multiple of 32).  Rows hold [n_kv_heads, head_dim] keys and values."""
+    (rounded up to a multiple of 32).  Rows hold [n_kv_heads, head_dim] keys and values.  Keys, values, queries and outputs start on 16 bytes;
+    lists of counts and masks may start anywhere (a view that does not start on 16 bytes is copied)."""
 
     def __init__(self, n_slots: int, n_kv_heads: int, head_dim: int, max_len: int, device=None):
         import torch
@@ -537,7 +543,7 @@ class Kv4Cache:
     def _counts(self, t, B, name):
         if t.dtype is not self.torch.int32 or t.shape != (B,) or (B > 1 and t.stride(0) != 1):
             raise ValueError(f"{name} must be a contiguous int32 tensor of {B} entries")
-        return t.data_ptr()
+        return _aligned(t)
 
     def append(self, k, v, cu_seqlens, start_rows, slots=None):
         """Rows [cu_seqlens[b], cu_seqlens[b + 1]) of k and v ([total, n_kv_heads, head_dim], bf16 or fp32) become rows
@@ -549,7 +555,8 @@ class Kv4Cache:
         ld = self._row_stride(k, self.n_kv_heads, total, "k")
         if self._row_stride(v, self.n_kv_heads, total, "v") != ld or v.dtype is not k.dtype:
             raise ValueError("k and v must have the same type and row stride")
-        _check(lib.hivis_kv4_append(self._ref, B, _slots(slots, B), _ints(cu_seqlens), self._counts(start_rows, B, "start_rows"), k.data_ptr(),
+        first = self._counts(start_rows, B, "start_rows")
+        _check(lib.hivis_kv4_append(self._ref, B, _slots(slots, B), _ints(cu_seqlens), first.data_ptr(), k.data_ptr(),
                                     v.data_ptr(), _dtype(k), ld, _raw_stream(self.dev.index)))
 
     def read(self, cu_seqlens, start_rows, slots=None):
@@ -561,7 +568,8 @@ class Kv4Cache:
         shape = (int(cu_seqlens[-1]), self.n_kv_heads, self.head_dim)
         k = t.empty(shape, dtype=t.float32, device=self.dev)
         v = k.new_empty(shape)
-        _check(lib.hivis_kv4_read(self._ref, B, _slots(slots, B), _ints(cu_seqlens), self._counts(start_rows, B, "start_rows"), k.data_ptr(),
+        first = self._counts(start_rows, B, "start_rows")
+        _check(lib.hivis_kv4_read(self._ref, B, _slots(slots, B), _ints(cu_seqlens), first.data_ptr(), k.data_ptr(),
                                   v.data_ptr(), _raw_stream(self.dev.index)))
         return k, v
 
@@ -578,7 +586,9 @@ class Kv4Cache:
         if mask is not None:
             if mask.dtype is not t.int32 or tuple(mask.shape) != (B, n_q, (mask_rows + 31) // 32) or not mask.is_contiguous():
                 raise ValueError("mask must be a contiguous int32 tensor [B, n_q, ceil(mask_rows / 32)]")
+            mask = _aligned(mask)
             mask_ptr = mask.data_ptr()
+        counts = self._counts(rows, B, "rows")
         if out is None:
             out = q.new_empty(q.shape)
             out_ld = heads * self.head_dim
@@ -586,7 +596,7 @@ class Kv4Cache:
             if out.dtype is not q.dtype:
                 raise ValueError("out must have the type of q")
             out_ld = self._row_stride(out, heads, B * n_q, "out")
-        _check(lib.hivis_kv4_attention(self._ref, B, _slots(slots, B), self._counts(rows, B, "rows"), n_q, heads, q.data_ptr(), _dtype(q), q_ld,
+        _check(lib.hivis_kv4_attention(self._ref, B, _slots(slots, B), counts.data_ptr(), n_q, heads, q.data_ptr(), _dtype(q), q_ld,
                                        self._scale if scale is None else scale, mask_ptr, mask_rows, out.data_ptr(), out_ld,
                                        _raw_stream(self.dev.index)))
         return out
@@ -602,7 +612,8 @@ class Logprobs(NamedTuple):
 
 def logprobs(logits, ids=None, temperature: float = 1.0, top_n: int = 0, entropy: bool = True) -> Logprobs:
     """Log-probabilities of `ids` (int32 [n_rows, n_ids]) under softmax(logits / temperature), the rows' entropy and their
-    `top_n` most probable tokens; logits [n_rows, vocab], bf16 or fp32, rows may lie apart.  include/hivis.h: hivis_logprobs."""
+    `top_n` most probable tokens; logits [n_rows, vocab], bf16 or fp32, rows may lie apart.  include/hivis.h: hivis_logprobs.
+    Views may start anywhere; one that does not start on 16 bytes (logits[1:] of an odd vocabulary, say) is copied first."""
     import torch
     shape, stride, index = logits.shape, logits.stride(), logits.get_device()
     if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
@@ -618,6 +629,9 @@ def logprobs(logits, ids=None, temperature: float = 1.0, top_n: int = 0, entropy
         if ids.dtype is not torch.int32 or ids.dim() != 2 or ids.shape[0] != n or ids.get_device() != index or not ids.is_contiguous():
             raise ValueError("ids must be a contiguous int32 tensor [n_rows, n_ids] beside the logits")
         n_ids = ids.shape[1]
+        ids = _aligned(ids)
+    logits = _aligned(logits)
+    stride = logits.stride()
     lp = h = top = top_lp = None
     p_lp = p_h = p_top = p_top_lp = None
     f32 = torch.float32

@@ -636,3 +636,22 @@ def test_codes_of_values_beside_ties(dtype, kind):
     k, v = cache.read([0, 1024], _ints([0]))
     want = ref.values(*ref.quantise(_np(x))).astype(np.float32)
     assert np.array_equal(k.cpu().numpy(), want) and np.array_equal(v.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("n_q", [1, 33])
+def test_counts_and_masks_that_start_anywhere(n_q):
+    t = _torch()
+    f = Filled("bf16", 128, 2, 2, [70, 33, 100], n_q, seed=61)
+    f.put()
+    again = _cache(3, 2, 128, 100)
+    zeros = t.zeros(5, dtype=t.int32, device="cuda")
+    again.append(f.k, f.v, _starts(f.lens), zeros[1:4])
+    for a, b in zip(again.read([0, 70, 103, 203], zeros[2:]), f.cache.read([0, 70, 103, 203], _ints([0, 0, 0]))):
+        assert t.equal(a, b)
+    wide = _ints([7] + f.lens)
+    assert t.equal(again.attention(f.q, wide[1:], n_q=n_q), f.cache.attention(f.q, f.rows, n_q=n_q))
+    mask = f.rng.random((3, n_q, 40)) < 0.5
+    words = t.zeros(1 + 3 * n_q * 2, dtype=t.int32, device="cuda")
+    words[1:] = _words(mask).view(-1)
+    out = again.attention(f.q, wide[1:], n_q=n_q, mask=words[1:].view(3, n_q, 2), mask_rows=40)
+    assert t.equal(out, f.cache.attention(f.q, f.rows, n_q=n_q, mask=_words(mask), mask_rows=40))

@@ -293,3 +293,17 @@ def test_banned_tokens_at_any_temperature(dtype, temperature, V, ld):
     d = d[:, :V]
     ids = t.from_numpy(np.concatenate([rng.integers(0, V, (12, 3)), np.full((12, 1), V - 1), np.zeros((12, 1))], 1).astype(np.int32)).cuda()
     _check_far(d, ids, temperature, 7, logprobs(d, ids, temperature=temperature, top_n=7))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_views_that_start_anywhere(dtype):
+    """A prompt is scored: the rows of one position, the tokens of the next; rows and tokens from the second one on."""
+    from paper_2509_23928_b200 import logprobs
+    t = _torch()
+    rng = np.random.default_rng(4)
+    V = 50257
+    x = _to(rng.standard_normal((6, V)) * 3, dtype)
+    tokens = t.from_numpy(rng.integers(0, V, 6).astype(np.int32)).cuda()
+    for logits, ids in ((x[:-1], tokens[1:].view(-1, 1)), (x[1:], tokens[1:].view(-1, 1)), (x[3:], tokens[3:].view(-1, 1)),
+                        (x.view(2, 3, V)[:, -1], tokens[2:4].view(-1, 1)), (x[:, 5:1000], tokens[:6].view(-1, 1) % 995)):
+        _check(logits, ids, 1.0, 4, logprobs(logits, ids, top_n=4))

@@ -24,3 +24,15 @@ def test_bad_arguments_are_refused(kw, code):
 
 def test_no_rows_need_no_gpu():
     assert _call(n=0, logits=None) == 0
+
+
+@pytest.mark.parametrize("first", range(8))
+def test_views_that_start_anywhere_are_copied_to_where_the_library_reads(first):
+    import torch
+    from paper_2509_23928_b200.binding import _aligned
+    whole = torch.arange(8 * 40, dtype=torch.int32).view(8, 40)
+    for t in (whole.view(-1)[first:first + 9], whole[:, first:first + 21], whole.bfloat16()[1:, first:], whole[:0, first:]):
+        a = _aligned(t)
+        assert a.data_ptr() % 16 == 0 and a.dtype is t.dtype and a.shape == t.shape and bool((a == t).all())
+        assert a.numel() == 0 or a[0].is_contiguous()
+        assert (a is t) == (t.data_ptr() % 16 == 0)
