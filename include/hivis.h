@@ -406,7 +406,7 @@ int hivis_kv4_read(const hivis_kv4_cache* cache, int B, const int* seq_slots_hos
  *   mask NULL: causal.  The queries sit on the last n_q rows: query i sees rows [0, rows[b] - n_q + i].
  *   mask (uint32 [B, n_q, ceil(mask_rows / 32)]): a draft tree, or anything else over the last mask_rows rows: query i sees
  *   rows [0, rows[b] - mask_rows), and row rows[b] - mask_rows + j iff bit j % 32 of word j / 32 is set.
- * scale: positive, below 1e38.  A query that sees no row gets zeros.  Rows that a query does not see do not touch its result, whatever they hold.
+ * scale: positive, below 1e38; scores may have any size that fp32 holds.  A query that sees no row gets zeros.  Rows that a query does not see do not touch its result, whatever they hold.
  * q [B * n_q, n_q_heads * head_dim] and out likewise in `dtype` (HIVIS_F32 | HIVIS_BF16), q_ld and out_ld elements from one
  * row to the next.  The result does not depend on anything but the arguments: sums are made in one order.
  * Rows' values as m + s n, sums in fp32; fp32: queries and weights to 22 bits.  bf16: weights to 11 bits, and in calls of many

@@ -407,11 +407,14 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (EDGE)
-                    if (!sight(row + 16 * u + g + (e < 2 ? 0 : 8), min((j0 + 8 * n + 2 * c + (e & 1)) / G, sight.n_q - 1))) s[u][n][e] = -INFINITY;
-                p[u][n][e] = fmaf(s[u][n][e], st.fq[n][e & 1], -st.m[n][e & 1]);
-                top = fmaxf(top, p[u][n][e]);
+            for (int e = 0; e < 4; e += 2) {
+                if constexpr (EDGE) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (!sight(row + 16 * u + g + 4 * e, min((j0 + 8 * n + 2 * c + i) / G, sight.n_q - 1))) s[u][n][e + i] = -INFINITY;
+                }
+                kv4_above(s[u][n][e], s[u][n][e + 1], st.fq[n][0], st.fq[n][1], kv4_pack2(-st.m[n][0], -st.m[n][1]), p[u][n][e], p[u][n][e + 1]);
+                top = fmaxf(top, fmaxf(p[u][n][e], p[u][n][e + 1]));
             }
     if (__any_sync(0xffffffffu, top > KV4_LAZY)) {
 #pragma unroll
@@ -426,8 +429,8 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
                 st.m[n][e] = m;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    p[u][n][e] = fmaf(s[u][n][e], st.fq[n][e], -m);
-                    p[u][n][e + 2] = fmaf(s[u][n][e + 2], st.fq[n][e], -m);
+                    p[u][n][e] = __fadd_rn(__fmul_rn(s[u][n][e], st.fq[n][e]), -m);
+                    p[u][n][e + 2] = __fadd_rn(__fmul_rn(s[u][n][e + 2], st.fq[n][e]), -m);
                 }
                 st.l[n][e] *= f;
 #pragma unroll

@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     // rows' codes; of even and odd steps: S^T is there (and what goes with it); V is there; O^T is there, P and V may be overwritten
     __shared__ u64 bars[KT_STAGES + 6];
     __shared__ uint32_t s_tmem, s_poison[KT_COLS], s_nan[2][KT_ROWS];
-    __shared__ __align__(16) float2 s_fm[KT_COLS];                     // what a column's scores are to be multiplied with; its maximum less KT_LIFT
+    __shared__ __align__(16) float s_f[KT_COLS], s_m[KT_COLS];         // what a column's scores are to be multiplied with; KT_LIFT less its maximum
     __shared__ float2 s_part[KT_CLUSTER][KT_COLS];
     __shared__ float s_rk[2][KT_ROWS], s_fade[2], s_top[4][KT_COLS], s_fall[KT_COLS], s_inv[KT_COLS];
     __shared__ uint32_t s_max[8];
@@ -227,7 +227,10 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         const int e = mx > 0.f ? min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 100) : 0;
         const float up = kv4_pow2(14 - e);
-        if (c == 0) s_fm[col] = make_float2(kv4_pow2(e + 2) * a.scale_log2, KV4_NOTHING);     // (2^-14 of the queries' scaling, 2^16 of the keys')
+        if (c == 0) {
+            s_f[col] = kv4_pow2(e + 2) * a.scale_log2;                 // (2^-14 of the queries' scaling, 2^16 of the keys')
+            s_m[col] = -KV4_NOTHING;
+        }
 #pragma unroll
         for (int w = 0; w < Q; ++w) {
             const float* y = x[w];
@@ -411,10 +414,14 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 uint32_t raw[32];
                 kt_ld32(my_tmem + KT_S + (n & 1) * KT_COLS, raw);
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    const float4 f = *(const float4*)(s_fm + half * 32 + i);
-                    y[i] = fmaf(__uint_as_float(raw[i]) * rk, f.x, -f.y);
-                    y[i + 1] = fmaf(__uint_as_float(raw[i + 1]) * rk, f.z, -f.w);
+                for (int i = 0; i < 32; i += 4) {
+                    const float4 f = *(const float4*)(s_f + half * 32 + i);
+                    const ulonglong2 m = *(const ulonglong2*)(s_m + half * 32 + i);
+                    float t[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) t[k] = __uint_as_float(raw[i + k]) * rk;
+                    kv4_above(t[0], t[1], f.x, f.y, m.x, y[i], y[i + 1]);
+                    kv4_above(t[2], t[3], f.z, f.w, m.y, y[i + 2], y[i + 3]);
                 }
             }
             if (t >= nfull) {
@@ -436,7 +443,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 float x[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    y[i] = __uint_as_float(raw[i]) * rk * s_fm[half * 32 + i].x;
+                    y[i] = __fmul_rn(__uint_as_float(raw[i]) * rk, s_f[half * 32 + i]);
                     if (!(see >> i & 1u)) y[i] = -INFINITY;
                     x[i] = y[i];
                 }
@@ -454,13 +461,13 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 kt_sync<2>();
                 if (tid < KT_GROUP + KT_COLS) {
                     const int c = tid - KT_GROUP;
-                    const float old = s_fm[c].y, m = fmaxf(old, fmaxf(fmaxf(s_top[0][c], s_top[1][c]), fmaxf(s_top[2][c], s_top[3][c])) - KT_LIFT);
-                    s_fm[c].y = m;
+                    const float old = -s_m[c], m = fmaxf(old, fmaxf(fmaxf(s_top[0][c], s_top[1][c]), fmaxf(s_top[2][c], s_top[3][c])) - KT_LIFT);
+                    s_m[c] = -m;
                     s_fall[c] = kv4_exp2(old - m);
                 }
                 kt_sync<2>();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) y[i] -= s_fm[half * 32 + i].y;
+                for (int i = 0; i < 32; ++i) y[i] += s_m[half * 32 + i];
                 if (n > 0) {
                     if (ok) ok = kv4_wait(bar_o + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
                     kt_fence_after();
@@ -541,7 +548,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     if (tid < S * KT_COLS) {
         const int col = tid % KT_COLS;
         const float l = ok ? (s_top[0][col] + s_top[1][col]) + (s_top[2][col] + s_top[3][col]) : __uint_as_float(0x7FC00000u);
-        *(S > 1 ? cluster.map_shared_rank(&s_part[rank][col], tid / KT_COLS) : &s_part[0][col]) = make_float2(s_fm[col].y, l);
+        *(S > 1 ? cluster.map_shared_rank(&s_part[rank][col], tid / KT_COLS) : &s_part[0][col]) = make_float2(-s_m[col], l);
         if (tid < KT_COLS) s_inv[col] = l == 0.f ? 0.f : 1.f / l;      // nothing visible: zeros
     }
     __syncthreads();

@@ -109,7 +109,16 @@ __device__ __forceinline__ void kv4_put(const Kv4AttnArgs& a, int b, int h, int 
     }
 }
 
-#define KV4_NOTHING -1e30f     // the running maximum of a column that has seen no row
+// The running maximum of a column that has seen no row: fp32's lowest number, as good a reference as any for scores next to it, and a
+// difference with it is never NaN.
+#define KV4_NOTHING -3.402823466e38f
+
+// Two columns' scores above their maxima.  The product is rounded before the difference, as the maxima are: by one fused operation the
+// largest score itself would be off its maximum by what the product lost, whole powers of two from 2^25 on.
+// (Single products: the compiler fuses a pair's with the sum.)
+__device__ __forceinline__ void kv4_above(float s0, float s1, float f0, float f1, u64 minus_m, float& y0, float& y1) {
+    kv4_unpack2(kv4_add2(kv4_pack2(__fmul_rn(s0, f0), __fmul_rn(s1, f1)), minus_m), y0, y1);
+}
 
 // How far the maximum may fall behind: p < 2^8, so that p s R < 2^14 stays inside fp16.
 #define KV4_LAZY 8.f

@@ -655,3 +655,36 @@ def test_counts_and_masks_that_start_anywhere(n_q):
     words[1:] = _words(mask).view(-1)
     out = again.attention(f.q, wide[1:], n_q=n_q, mask=words[1:].view(3, n_q, 2), mask_rows=40)
     assert t.equal(out, f.cache.attention(f.q, f.rows, n_q=n_q, mask=_words(mask), mask_rows=40))
+
+
+def _check_weights(f, out, see):
+    """Results whose weights are the same for every row of see [sequence][n_q, rows]: the values' share of Filled.check's bounds alone."""
+    got, cu = _np(out).reshape(len(f.lens), f.n_q, f.Hkv * f.G, f.dh), _starts(f.lens)
+    for b, n in enumerate(f.lens):
+        kq, vq = ref.quantise(_np(f.k[cu[b]:cu[b + 1]])), ref.quantise(_np(f.v[cu[b]:cu[b + 1]]))
+        want, reach, _ = ref.attention(np.zeros((f.n_q, f.Hkv * f.G, f.dh)), kq, vq, 1.0, see[b])
+        tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * reach if f.dtype == "bf16" else 2.0 ** -20 * reach
+        d = np.abs(got[b] - want)
+        assert np.all(d <= tol), (b, float((d / np.maximum(tol, 1e-300)).max()))
+
+
+@pytest.mark.parametrize("dtype,n_q", [("bf16", 1), ("bf16", 61), ("f32", 1), ("f32", 20)])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("size,sign", [(1e3, 1), (1e5, -1), (1e5, 1), (1e8, 1), (1e12, -1), (1e16, -1), (1e18, -1), (1e18, 1)])
+def test_scores_far_from_zero(dtype, n_q, dh, size, sign):
+    """Scores of 1e7 to 1e37 are scores like any other: equal ones share the weight; one that is half as high has none, or all if they are below zero."""
+    f = Filled(dtype, dh, 2, 1, [300, 3], n_q, seed=63)
+    f.q.fill_(1.37 * size)
+    f.k.fill_(sign * 1.71 * size)
+    f.put()
+    see = [ref.visible(n, n_q, None, 0) for n in f.lens]
+    _check_weights(f, f.cache.attention(f.q, f.rows, n_q=n_q), see)
+    for b, r in ((0, 280), (1, 1)):
+        f.k[_starts(f.lens)[b] + r] *= 0.5
+        s, other = see[b], np.arange(f.lens[b]) != r
+        if sign < 0:
+            s[s[:, r]] = ~other
+        else:
+            s[s[:, other].any(-1), r] = False
+    f.put()
+    _check_weights(f, f.cache.attention(f.q, f.rows, n_q=n_q), see)
