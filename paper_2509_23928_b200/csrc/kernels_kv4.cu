@@ -622,8 +622,8 @@ __device__ __forceinline__ void kv4_load_queries(Kv4Warp<DH, NT, Kv4Io<T>::SPLIT
         }
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        // the row's largest number to 2^14 .. 2^15 (a row of zeros, or below 2^-100, or beyond 2^100, as far as that goes)
-        const int e = mx > 0.f ? min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 100) : 0;
+        // the row's largest number to 2^14 .. 2^15 (a row of zeros, or below 2^-100, as far as that goes)
+        const int e = mx > 0.f ? min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 127) : 0;
         const float up = kv4_pow2(14 - e);
         float sum[Q];
 #pragma unroll
@@ -656,7 +656,7 @@ __device__ __forceinline__ void kv4_load_queries(Kv4Warp<DH, NT, Kv4Io<T>::SPLIT
         if constexpr (!SPLIT) {
             kv4_sum_parts<Q>(sum, c, st.qm[n]);
         }
-        const float f = kv4_pow2(e - 14) * (1.f / UNIT) * a.scale_log2;
+        const float f = kv4_factor(e - 14 + (SPLIT ? 0 : 24), a.scale_log2);       // (the unit of the products in it)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int from = (2 * c + s) * 4;                     // a lane with lane / 4 = 2 c + s

@@ -225,10 +225,10 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
         }
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        const int e = mx > 0.f ? min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 100) : 0;
+        const int e = mx > 0.f ? min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 127) : 0;
         const float up = kv4_pow2(14 - e);
         if (c == 0) {
-            s_f[col] = kv4_pow2(e + 2) * a.scale_log2;                 // (2^-14 of the queries' scaling, 2^16 of the keys')
+            s_f[col] = kv4_factor(e + 2, a.scale_log2);                // (2^-14 of the queries' scaling, 2^16 of the keys')
             s_m[col] = -KV4_NOTHING;
         }
 #pragma unroll

@@ -68,6 +68,11 @@ __device__ __forceinline__ float kv4_exp2(float x) {
 }
 // 2^e, -126 <= e <= 127
 __device__ __forceinline__ float kv4_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// What a column's scores are multiplied with, 2^e f (e may lie beyond fp32's exponents): neither 0 nor infinite, so that a score of
+// -infinity (a row that is not seen) stays one and a score of 0 stays 0.
+__device__ __forceinline__ float kv4_factor(int e, float f) {
+    return fminf(fmaxf(f * kv4_pow2(e / 2) * kv4_pow2(e - e / 2), __uint_as_float(1u)), 3.402823466e38f);
+}
 
 // Nibbles 0 and 4 of a word as n, nibbles 1 and 5 as 16 n, two fp16 numbers: subnormal ones (of 2^-24) by a mask alone, or whole ones.
 // The tensor core lines products up by their factors' exponent fields, and a subnormal's is ten bits above its value: sums of

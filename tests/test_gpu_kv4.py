@@ -688,3 +688,19 @@ def test_scores_far_from_zero(dtype, n_q, dh, size, sign):
             s[s[:, other].any(-1), r] = False
     f.put()
     _check_weights(f, f.cache.attention(f.q, f.rows, n_q=n_q), see)
+
+
+@pytest.mark.parametrize("dtype,n_q", [("bf16", 4), ("bf16", 61), ("f32", 4), ("f32", 20)])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_scales_that_are_tiny_or_huge(dtype, n_q, dh):
+    """Queries and a scale so small that all scores are next to 0, rows that are not seen among them; and so large that only a 0 is one."""
+    f = Filled(dtype, dh, 2, 1, [300, 3, 70], n_q, seed=65)
+    f.q *= 1e-30
+    f.put()
+    see = [ref.visible(n, n_q, None, 0) for n in f.lens]
+    _check_weights(f, f.cache.attention(f.q, f.rows, n_q=n_q, scale=1e-20), see)
+    f.q *= 1e30
+    f.q *= 1e30
+    f.k.zero_()
+    f.put()
+    _check_weights(f, f.cache.attention(f.q, f.rows, n_q=n_q, scale=9e37), see)
