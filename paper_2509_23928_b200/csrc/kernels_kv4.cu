@@ -488,7 +488,7 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
                 }
             }
         fin = __reduce_max_sync(0xffffffffu, fin);
-        const int e = min(max((int)(fin >> 7) - 127, -114), 114);           // scales are below 2^(e + 1)
+        const int e = max((int)(fin >> 7) - 127, -114);                     // scales are below 2^(e + 1)
         const float R = kv4_pow2(5 - e);
         if (R < st.R) {
             const float f = R / st.R;
@@ -758,7 +758,7 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
     __syncthreads();                                // every ring is used up
 
     // ---- this warp's columns to shared memory: maximum, sum, output
-    const float down = (1.f / UNIT) / st.R;
+    const float down = 1.f / st.R;                  // (the unit apart: values next to fp32's ends pass through numbers of their own size)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -777,7 +777,8 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
                 const float x1 = st.o[n][2 * w][2 + s], y1 = st.o[n][2 * w + 1][2 + s];
                 const float x0 = st.o[n][2 * w][s] - (SPLIT ? 0.f : x1), y0 = st.o[n][2 * w + 1][s] - (SPLIT ? 0.f : y1);
                 *(float4*)(sO + (warp * NB + col) * LDO + 32 * w + 4 * g) =
-                    make_float4(fmaf(x0, down, m), fmaf(x1, down * 0.0625f, m), fmaf(y0, down, m), fmaf(y1, down * 0.0625f, m));
+                    make_float4(fmaf(x0 * down, 1.f / UNIT, m), fmaf(x1 * down, 0.0625f / UNIT, m), fmaf(y0 * down, 1.f / UNIT, m),
+                                fmaf(y1 * down, 0.0625f / UNIT, m));
             }
         }
     __syncthreads();

@@ -704,3 +704,16 @@ def test_scales_that_are_tiny_or_huge(dtype, n_q, dh):
     f.k.zero_()
     f.put()
     _check_weights(f, f.cache.attention(f.q, f.rows, n_q=n_q, scale=9e37), see)
+
+
+@pytest.mark.parametrize("dtype,n_q", [("bf16", 1), ("f32", 1), ("bf16", 2)])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("scale_v", [1e33, 1e34, 5e34])
+def test_values_next_to_the_end_of_the_range(dtype, n_q, dh, scale_v):
+    """2^8 |v| summed over the rows stays below 2^127: so far values are taken."""
+    f = Filled(dtype, dh, 1, 1, [3, 1], n_q, seed=67)
+    f.v.clamp_(-4.0, 4.0).mul_(scale_v)
+    assert 256.0 * 3 * 4.0 * scale_v < 2.0 ** 127
+    f.k.zero_()
+    f.put()
+    _check_weights(f, f.cache.attention(f.q, f.rows, n_q=n_q), [ref.visible(n, n_q, None, 0) for n in f.lens])
