@@ -291,6 +291,9 @@ cudaError_t launch_kv4_put(const Kv4View& c, int n, const float* kv, int ld, int
 // is rounded there); probabilities are rounded to fp16's 11 bits, 2^-12 of each, which the 2^-9 of the bf16 result hides.  fp32
 // queries and their probabilities go in as two fp16 numbers (22 bits), the codes as whole numbers, and the products of 16 rows are
 // added up in fp32 outside the tensor core.
+// Weights meet the values' scales in fp16, p s R.  R is a column's own power of two and follows the largest p s that the column has met
+// (as its maximum follows its scores), between 2^5 and 2^15 of it: rows that it does not see, and rows whose weight is next to nothing,
+// take no bits from the others, whatever they hold.  What a warp does for one column depends on that column's rows alone, to the bit.
 //
 // A cluster of up to 16 CTAs shares one (sequence, KV head, block of columns); a warp takes every (warps of the cluster)-th step of
 // 16 or 32 rows, which bulk copies bring into its own ring, and keeps its own maximum, sum and output.  They are joined in
@@ -334,8 +337,8 @@ struct Kv4Warp {
     float m[NT][2], l[NT][2];                   // l: this lane's rows only
     float o[NT][2 * Q][4];                      // V^T P^T, scaled by R and the codes' unit
     float mn[NT][Q][2];                         // sum of p m per group, this lane's rows only
-    float R;                                    // power of two that brings the values' scales below 2^6
-    uint32_t r_limit;                           // the bf16 scale from which on R is too large
+    float R[NT][2];                             // powers of two that bring those columns' p s below 2^15
+    uint32_t r_limit;                           // the bf16 scale from which on one of them may be too large
 };
 
 __device__ __forceinline__ float kv4_max_rows(float x) {       // over the lanes that hold other rows of the same columns
@@ -402,6 +405,7 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
     }
     // ---- scores above the running maximum, in powers of two
     float p[U][NT][4], top = -INFINITY;
+    uint32_t risen = 0u;                                              // columns whose maximum is raised: bits 2 n + e
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -421,11 +425,18 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float m = -INFINITY;
+                // (a column's own scores decide; raised by whole powers of two, which R takes from the outputs' scale)
+                float z = -INFINITY;
 #pragma unroll
-                for (int u = 0; u < U; ++u) m = fmaxf(m, fmaxf(s[u][n][e] * st.fq[n][e], s[u][n][e + 2] * st.fq[n][e]));
-                m = fmaxf(st.m[n][e], kv4_max_rows(m));
-                const float f = kv4_exp2(st.m[n][e] - m);
+                for (int u = 0; u < U; ++u) z = fmaxf(z, fmaxf(__fmul_rn(s[u][n][e], st.fq[n][e]), __fmul_rn(s[u][n][e + 2], st.fq[n][e])));
+                z = kv4_max_rows(z);
+                const float old = st.m[n][e], above = z - old;
+                if (above > KV4_LAZY) risen |= 1u << (2 * n + e);
+                const float m = !(above > KV4_LAZY) ? old : above < 0x1p20f && fabsf(old) < 0x1p22f ? old + floorf(above) : z;
+                const float f = kv4_exp2(old - m);
+                const int was = (int)(__float_as_uint(st.R[n][e]) >> 23), now = min(was + __float2int_rn(fminf(m - old, 300.f)), 127 + 119);
+                const float fo = kv4_exp2((old - m) + (float)(now - was));
+                st.R[n][e] = __uint_as_float((uint32_t)now << 23);
                 st.m[n][e] = m;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -436,11 +447,12 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
 #pragma unroll
                 for (int w = 0; w < Q; ++w) {
                     st.mn[n][w][e] *= f;
-                    st.o[n][2 * w][e] *= f; st.o[n][2 * w][e + 2] *= f;
-                    st.o[n][2 * w + 1][e] *= f; st.o[n][2 * w + 1][e + 2] *= f;
+                    st.o[n][2 * w][e] *= fo; st.o[n][2 * w][e + 2] *= fo;
+                    st.o[n][2 * w + 1][e] *= fo; st.o[n][2 * w + 1][e + 2] *= fo;
                 }
             }
         }
+        st.r_limit = 0u;                                            // (R has grown)
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -473,34 +485,45 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
 #pragma unroll
         for (int w = 0; w < Q; ++w) big = __vmaxu2(big, __vmaxu2(a0[u][w], a1[u][w]));
     }
-    // R follows the largest scale, by halves of words (no scale is negative; a NaN's is above all)
+    // R follows a column's own p s: what it does not see, or gives no weight, has no part in it.  While every scale is below r_limit (by
+    // halves of words; no scale is negative, a NaN's is above all) and p below 2^8, no p s R reaches 2^15.
     if (__any_sync(0xffffffffu, max(big >> 16, big & 0xFFFFu) >= st.r_limit)) {
-        uint32_t fin = 0u;                                          // (rows that hold a NaN decide nothing)
+        float s0[U], s1[U];                                         // the rows' largest scales (those of groups that hold a NaN decide nothing)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            uint32_t x0 = 0u, x1 = 0u;
 #pragma unroll
             for (int w = 0; w < Q; ++w) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const uint32_t u0 = (a0[u][w] >> (16 * t)) & 0xFFFFu, u1 = (a1[u][w] >> (16 * t)) & 0xFFFFu;
-                    if (u0 < 0x7F80u) fin = max(fin, u0);
-                    if (u1 < 0x7F80u) fin = max(fin, u1);
-                }
+                const uint32_t y0 = __byte_perm(a0[u][w], 0u, mine) >> 16, y1 = __byte_perm(a1[u][w], 0u, mine) >> 16;
+                if (y0 < 0x7F80u) x0 = max(x0, y0);
+                if (y1 < 0x7F80u) x1 = max(x1, y1);
             }
-        fin = __reduce_max_sync(0xffffffffu, fin);
-        const int e = max((int)(fin >> 7) - 127, -114);                     // scales are below 2^(e + 1)
-        const float R = kv4_pow2(5 - e);
-        if (R < st.R) {
-            const float f = R / st.R;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 2 * Q; ++i)
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) st.o[n][i][t] *= f;
-            st.R = R;
-            st.r_limit = (uint32_t)(e + 1 + 127) << 7;
+            s0[u] = __uint_as_float(x0 << 16);
+            s1[u] = __uint_as_float(x1 << 16);
         }
+        float R = 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float t = 0.f;
+#pragma unroll
+                for (int u = 0; u < U; ++u) t = fmaxf(t, fmaxf(p[u][n][e] * s0[u], p[u][n][e + 2] * s1[u]));
+                t = kv4_max_rows(t);
+                if (t * st.R[n][e] >= (risen >> (2 * n + e) & 1u ? 0x1p6f : 0x1p15f)) {
+                    const float r = kv4_pow2(127 + 5 - (int)(__float_as_uint(t) >> 23)), f = r / st.R[n][e];   // (t >= 2^-113)
+                    st.R[n][e] = r;
+#pragma unroll
+                    for (int i = 0; i < 2 * Q; ++i) {
+                        st.o[n][i][e] *= f;
+                        st.o[n][i][e + 2] *= f;
+                    }
+                }
+                R = fmaxf(R, st.R[n][e]);
+            }
+        R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, 1));
+        R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, 2));
+        st.r_limit = (uint32_t)(127 + 127 + 7 - (int)(__float_as_uint(R) >> 23)) << 7;       // 2^7 / R
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -511,7 +534,7 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pr[n][e] = p[u][n][e] * st.R;
+            for (int e = 0; e < 4; ++e) pr[n][e] = p[u][n][e] * st.R[n][e & 1];
         uint32_t q0[Q], q1[Q];                                      // m likewise
         kv4_lds<Q>(tile + u * TB + 18 * DH + (g >> 1) * (DH / 4) + CH, q0);
         kv4_lds<Q>(tile + u * TB + 19 * DH + (g >> 1) * (DH / 4) + CH, q1);
@@ -722,6 +745,7 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
         for (int s = 0; s < 2; ++s) {
             st.m[n][s] = KV4_NOTHING;
             st.l[n][s] = 0.f;
+            st.R[n][s] = 0x1p119f;
 #pragma unroll
             for (int w = 0; w < Q; ++w) st.mn[n][w][s] = 0.f;
         }
@@ -730,8 +754,7 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
 #pragma unroll
             for (int s = 0; s < 4; ++s) st.o[n][i][s] = 0.f;
     }
-    st.R = 0x1p119f;
-    st.r_limit = (uint32_t)(127 - 113) << 7;
+    st.r_limit = 0u;
 
     bool ok = true;
     uint32_t stage = 0, parity = 0;
@@ -758,12 +781,12 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
     __syncthreads();                                // every ring is used up
 
     // ---- this warp's columns to shared memory: maximum, sum, output
-    const float down = 1.f / st.R;                  // (the unit apart: values next to fp32's ends pass through numbers of their own size)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int col = 8 * n + 2 * c + s;
+            const float down = 1.f / st.R[n][s];    // (the unit apart: values next to fp32's ends pass through numbers of their own size)
             const float l = kv4_sum_rows(st.l[n][s]);
             if (g == 0) {
                 sM[warp * NB + col] = st.m[n][s];

@@ -125,7 +125,7 @@ __device__ __forceinline__ void kv4_above(float s0, float s1, float f0, float f1
     kv4_unpack2(kv4_add2(kv4_pack2(__fmul_rn(s0, f0), __fmul_rn(s1, f1)), minus_m), y0, y1);
 }
 
-// How far the maximum may fall behind: p < 2^8, so that p s R < 2^14 stays inside fp16.
+// How far the maximum may fall behind: p < 2^8.
 #define KV4_LAZY 8.f
 
 struct Kv4Sight {              // which rows the columns see

@@ -717,3 +717,99 @@ def test_values_next_to_the_end_of_the_range(dtype, n_q, dh, scale_v):
     f.k.zero_()
     f.put()
     _check_weights(f, f.cache.attention(f.q, f.rows, n_q=n_q), [ref.visible(n, n_q, None, 0) for n in f.lens])
+
+
+def _unseen(f, size, hidden):
+    """Rows `hidden` [sequence][...] of f with keys and values of about `size`, or zeros."""
+    g = _torch().Generator(device="cuda").manual_seed(5)
+    for b, rows in enumerate(hidden):
+        i = [_starts(f.lens)[b] + r for r in rows]
+        for x in (f.k, f.v):
+            x[i] = (x[i].float().normal_(0.0, 1.0, generator=g) * size).to(x.dtype)
+    f.put()
+
+
+UNSEEN = [("bf16", 64, 1, 4), ("bf16", 128, 1, 4), ("bf16", 128, 2, 5), ("f32", 64, 1, 4), ("f32", 128, 3, 6)]
+
+
+@pytest.mark.parametrize("dtype,dh,G,n_q", UNSEEN)
+@pytest.mark.parametrize("size", [1e4, 1e8, 1e12, 1e30, 1e-20])
+def test_rows_that_are_not_seen_may_hold_anything(dtype, dh, G, n_q, size):
+    """Finite rows far larger (or smaller) than the others, hidden from all queries by a mask, from some, and by the causal edge: to the bit what
+    the same call gives where those rows are zero, and within the bounds."""
+    t = _torch()
+    lens, T = [300, 70, 45], 40
+    f = Filled(dtype, dh, 2, G, lens, n_q, seed=71)
+    mask = f.rng.random((3, n_q, T)) < 0.6
+    everywhere, half = [3, 4, 17, 30], [8, 20, 33]                   # of the last T rows: hidden from all, from the first queries
+    mask[:, :, everywhere] = False
+    mask[:, :n_q // 2, half] = False
+    mask[:, n_q // 2:, half] = True
+    got = []
+    for s in (0.0, size):
+        _unseen(f, s, [[n - T + j for j in everywhere + half] for n in lens])
+        got.append(f.cache.attention(f.q, f.rows, n_q=n_q, mask=_words(mask), mask_rows=T).view(3, n_q, -1))
+        if s == 0.0:
+            f.check(got[0], mask, T)
+    assert bool(t.isfinite(got[1]).all())
+    assert t.equal(got[0][:, :n_q // 2], got[1][:, :n_q // 2])
+    got = []
+    for s in (0.0, size):
+        _unseen(f, s, [[n - 1] for n in lens])                       # the last query alone sees it
+        got.append(f.cache.attention(f.q, f.rows, n_q=n_q).view(3, n_q, -1))
+    assert bool(t.isfinite(got[1]).all())
+    assert t.equal(got[0][:, :n_q - 1], got[1][:, :n_q - 1])
+
+
+@pytest.mark.parametrize("dtype,dh,G,n_q", UNSEEN)
+@pytest.mark.parametrize("fill", [0xFF, 0xFE, 0x7F, 0x7E, 0x80, "random"])
+def test_rows_that_were_never_written_may_be_masked(dtype, dh, G, n_q, fill):
+    """A padded tree over a buffer with anything in it: the mask leaves the padding out."""
+    t = _torch()
+    f = Filled(dtype, dh, 2, G, [40, 21], n_q, seed=73, max_len=96)
+    mask = np.zeros((2, n_q, 64), bool)
+    want = None
+    for b, n in enumerate(f.lens):
+        mask[b, :, :n] = f.rng.random((n_q, n)) < 0.7                # the rows [rows - 64, rows) = [0, 64): n of them written
+    rows = _ints([64, 64])
+    outs = []
+    for what in (0, fill):
+        if what == "random":
+            g = t.Generator(device="cuda").manual_seed(9)
+            f.cache.data.random_(0, 256, generator=g)
+        else:
+            f.cache.data.fill_(what)
+        f.put()
+        outs.append(f.cache.attention(f.q, rows, n_q=n_q, mask=_words(mask), mask_rows=64))
+    assert bool(t.isfinite(outs[0]).all()) and t.equal(outs[0], outs[1])
+
+
+@pytest.mark.parametrize("dtype,dh,G,n_q", UNSEEN)
+@pytest.mark.parametrize("size", [1e4, 1e12, 1e30])
+@pytest.mark.parametrize("first", [True, False])
+def test_rows_that_are_seen_without_weight_take_no_bits(dtype, dh, G, n_q, size, first):
+    """A far larger row whose score is 400 below the others (their scores: within 200): seen before them, or after."""
+    f = Filled(dtype, dh, 1, G, [400, 33], n_q, seed=75)
+    f.q.copy_(f.q.abs() + 0.5)
+    f.k.copy_((f.k.float() * 0.05).to(f.k.dtype))
+    cu = _starts(f.lens)
+    got = []
+    for s in (0.0, size):
+        for b in range(2):
+            i = slice(cu[b], cu[b] + 3) if first else slice(cu[b + 1] - n_q - 3, cu[b + 1] - n_q)
+            f.k[i] = -400.0
+            f.v[i] = (f.v[i].float().sign() * s).to(f.v.dtype)
+        f.put()
+        got.append(f.cache.attention(f.q, f.rows, n_q=n_q))
+        f.v[:] = f.v.where(f.v != 0, 1.0)
+    assert _torch().equal(got[0], got[1])
+
+
+@pytest.mark.parametrize("dtype,dh,G,n_q", UNSEEN)
+def test_groups_of_channels_of_other_magnitudes(dtype, dh, G, n_q):
+    """Neighbouring groups of 32 channels whose values differ by 1e4: every channel has the precision of its own group."""
+    f = Filled(dtype, dh, 2, G, [300, 20], n_q, seed=77)
+    f.v[:, :, 32:64] *= 1e-4
+    f.q *= 0.3
+    f.put()
+    f.check(f.cache.attention(f.q, f.rows, n_q=n_q))
