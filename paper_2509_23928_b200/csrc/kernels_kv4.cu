@@ -291,9 +291,9 @@ cudaError_t launch_kv4_put(const Kv4View& c, int n, const float* kv, int ld, int
 // is rounded there); probabilities are rounded to fp16's 11 bits, 2^-12 of each, which the 2^-9 of the bf16 result hides.  fp32
 // queries and their probabilities go in as two fp16 numbers (22 bits), the codes as whole numbers, and the products of 16 rows are
 // added up in fp32 outside the tensor core.
-// Weights meet the values' scales in fp16, p s R.  R is a column's own power of two and follows the largest p s that the column has met
-// (as its maximum follows its scores), between 2^5 and 2^15 of it: rows that it does not see, and rows whose weight is next to nothing,
-// take no bits from the others, whatever they hold.  What a warp does for one column depends on that column's rows alone, to the bit.
+// Weights meet the values' scales in fp16, p s R.  R is a column's own power of two and follows the largest p s that the column has met,
+// which it keeps between 2^3 and 2^15, as the maximum follows the scores: rows that a column does not see, and rows whose weight is next to
+// nothing, take no bits from the others, whatever they hold.  What a warp does for one column depends on that column's rows alone, to the bit.
 //
 // A cluster of up to 16 CTAs shares one (sequence, KV head, block of columns); a warp takes every (warps of the cluster)-th step of
 // 16 or 32 rows, which bulk copies bring into its own ring, and keeps its own maximum, sum and output.  They are joined in
@@ -405,7 +405,6 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
     }
     // ---- scores above the running maximum, in powers of two
     float p[U][NT][4], top = -INFINITY;
-    uint32_t risen = 0u;                                              // columns whose maximum is raised: bits 2 n + e
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -420,50 +419,7 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
                 kv4_above(s[u][n][e], s[u][n][e + 1], st.fq[n][0], st.fq[n][1], kv4_pack2(-st.m[n][0], -st.m[n][1]), p[u][n][e], p[u][n][e + 1]);
                 top = fmaxf(top, fmaxf(p[u][n][e], p[u][n][e + 1]));
             }
-    if (__any_sync(0xffffffffu, top > KV4_LAZY)) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                // (a column's own scores decide; raised by whole powers of two, which R takes from the outputs' scale)
-                float z = -INFINITY;
-#pragma unroll
-                for (int u = 0; u < U; ++u) z = fmaxf(z, fmaxf(__fmul_rn(s[u][n][e], st.fq[n][e]), __fmul_rn(s[u][n][e + 2], st.fq[n][e])));
-                z = kv4_max_rows(z);
-                const float old = st.m[n][e], above = z - old;
-                if (above > KV4_LAZY) risen |= 1u << (2 * n + e);
-                const float m = !(above > KV4_LAZY) ? old : above < 0x1p20f && fabsf(old) < 0x1p22f ? old + floorf(above) : z;
-                const float f = kv4_exp2(old - m);
-                const int was = (int)(__float_as_uint(st.R[n][e]) >> 23), now = min(was + __float2int_rn(fminf(m - old, 300.f)), 127 + 119);
-                const float fo = kv4_exp2((old - m) + (float)(now - was));
-                st.R[n][e] = __uint_as_float((uint32_t)now << 23);
-                st.m[n][e] = m;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    p[u][n][e] = __fadd_rn(__fmul_rn(s[u][n][e], st.fq[n][e]), -m);
-                    p[u][n][e + 2] = __fadd_rn(__fmul_rn(s[u][n][e + 2], st.fq[n][e]), -m);
-                }
-                st.l[n][e] *= f;
-#pragma unroll
-                for (int w = 0; w < Q; ++w) {
-                    st.mn[n][w][e] *= f;
-                    st.o[n][2 * w][e] *= fo; st.o[n][2 * w][e + 2] *= fo;
-                    st.o[n][2 * w + 1][e] *= fo; st.o[n][2 * w + 1][e + 2] *= fo;
-                }
-            }
-        }
-        st.r_limit = 0u;                                            // (R has grown)
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[u][n][e] = kv4_exp2(p[u][n][e]);
-            st.l[n][0] += p[u][n][0] + p[u][n][2];
-            st.l[n][1] += p[u][n][1] + p[u][n][3];
-        }
-    // ---- the values
+    // ---- the values' scales
     uint32_t a0[U][Q], a1[U][Q];                                    // s of the lane's rows' pairs, a word a group
     const uint32_t mine = g & 1 ? 0x3244u : 0x1044u;                // the lane's rows are the even or the odd ones of their pairs
     uint32_t big = 0u;
@@ -485,10 +441,11 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
 #pragma unroll
         for (int w = 0; w < Q; ++w) big = __vmaxu2(big, __vmaxu2(a0[u][w], a1[u][w]));
     }
-    // R follows a column's own p s: what it does not see, or gives no weight, has no part in it.  While every scale is below r_limit (by
-    // halves of words; no scale is negative, a NaN's is above all) and p below 2^8, no p s R reaches 2^15.
-    if (__any_sync(0xffffffffu, max(big >> 16, big & 0xFFFFu) >= st.r_limit)) {
-        float s0[U], s1[U];                                         // the rows' largest scales (those of groups that hold a NaN decide nothing)
+    // ---- The columns' maxima and their R, by what each of them sees: a maximum is raised by whole powers of two, which R takes from the
+    // outputs' scale, once a score is above it by KV4_LAZY, R lowered once a p s R may reach 2^15.  Neither can be while no score is so far up
+    // and every scale is below r_limit = 2^7 / (the largest R) - compared by halves of words; no scale is negative, a NaN's is above all.
+    if (__any_sync(0xffffffffu, top > KV4_LAZY || max(big >> 16, big & 0xFFFFu) >= st.r_limit)) {
+        float s0[U], s1[U];                                         // the rows' scales are below 2^s0, 2^s1 (those of groups that hold a NaN decide nothing)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             uint32_t x0 = 0u, x1 = 0u;
@@ -498,33 +455,57 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
                 if (y0 < 0x7F80u) x0 = max(x0, y0);
                 if (y1 < 0x7F80u) x1 = max(x1, y1);
             }
-            s0[u] = __uint_as_float(x0 << 16);
-            s1[u] = __uint_as_float(x1 << 16);
+            s0[u] = x0 ? (float)((int)(x0 >> 7) - 126) : -INFINITY;
+            s1[u] = x1 ? (float)((int)(x1 >> 7) - 126) : -INFINITY;
         }
-        float R = 0.f;
+        int most = -200;                                            // the largest R's exponent
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float t = 0.f;
+                float z = -INFINITY, t = -INFINITY;
 #pragma unroll
-                for (int u = 0; u < U; ++u) t = fmaxf(t, fmaxf(p[u][n][e] * s0[u], p[u][n][e + 2] * s1[u]));
-                t = kv4_max_rows(t);
-                if (t * st.R[n][e] >= (risen >> (2 * n + e) & 1u ? 0x1p6f : 0x1p15f)) {
-                    const float r = kv4_pow2(127 + 5 - (int)(__float_as_uint(t) >> 23)), f = r / st.R[n][e];   // (t >= 2^-113)
-                    st.R[n][e] = r;
+                for (int u = 0; u < U; ++u) z = fmaxf(z, fmaxf(__fmul_rn(s[u][n][e], st.fq[n][e]), __fmul_rn(s[u][n][e + 2], st.fq[n][e])));
+                z = kv4_max_rows(z);
+                const float old = st.m[n][e], above = z - old;
+                const bool rise = above > KV4_LAZY;
+                const float m = !rise ? old : above < 0x1p20f && fabsf(old) < 0x1p22f ? old + floorf(above) : z;
 #pragma unroll
-                    for (int i = 0; i < 2 * Q; ++i) {
-                        st.o[n][i][e] *= f;
-                        st.o[n][i][e + 2] *= f;
-                    }
+                for (int u = 0; u < U; ++u) {
+                    p[u][n][e] = __fadd_rn(__fmul_rn(s[u][n][e], st.fq[n][e]), -m);
+                    p[u][n][e + 2] = __fadd_rn(__fmul_rn(s[u][n][e + 2], st.fq[n][e]), -m);
+                    t = fmaxf(t, fmaxf(p[u][n][e] + s0[u], p[u][n][e + 2] + s1[u]));
                 }
-                R = fmaxf(R, st.R[n][e]);
+                t = kv4_max_rows(t);                                // the step's p s are below 2^t
+                const int was = (int)(__float_as_uint(st.R[n][e]) >> 23) - 127;
+                int now = min(was + (rise ? __float2int_rn(fminf(m - old, 300.f)) : 0), 119);
+                if (t + (float)now > (rise ? 6.f : 15.f)) now = max(5 - (int)ceilf(t), -125);
+                const float f = kv4_exp2(old - m), fo = kv4_exp2((old - m) + (float)(now - was));
+                st.m[n][e] = m;
+                st.R[n][e] = kv4_pow2(now);
+                most = max(most, now);
+                st.l[n][e] *= f;
+#pragma unroll
+                for (int w = 0; w < Q; ++w) {
+                    st.mn[n][w][e] *= f;
+                    st.o[n][2 * w][e] *= fo; st.o[n][2 * w][e + 2] *= fo;
+                    st.o[n][2 * w + 1][e] *= fo; st.o[n][2 * w + 1][e + 2] *= fo;
+                }
             }
-        R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, 1));
-        R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, 2));
-        st.r_limit = (uint32_t)(127 + 127 + 7 - (int)(__float_as_uint(R) >> 23)) << 7;       // 2^7 / R
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        st.r_limit = (uint32_t)(127 + 7 - most) << 7;
     }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[u][n][e] = kv4_exp2(p[u][n][e]);
+            st.l[n][0] += p[u][n][0] + p[u][n][2];
+            st.l[n][1] += p[u][n][1] + p[u][n][3];
+        }
+    // ---- the values
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         uint32_t v0[Q], v1[Q];
@@ -786,7 +767,8 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS) kv4_attn_kernel(const __grid
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int col = 8 * n + 2 * c + s;
-            const float down = 1.f / st.R[n][s];    // (the unit apart: values next to fp32's ends pass through numbers of their own size)
+            // 1 / R (the unit apart: values next to fp32's ends pass through numbers of their own size)
+            const float down = __uint_as_float((254u << 23) - __float_as_uint(st.R[n][s]));
             const float l = kv4_sum_rows(st.l[n][s]);
             if (g == 0) {
                 sM[warp * NB + col] = st.m[n][s];
