@@ -10,16 +10,20 @@
 // that row, the channels of a group in the order of the nibbles, and the queries' in the same.  Two words of V codes have four channels
 // each of two neighbouring rows: 16 bytes of either row, channels of two groups side by side; V^T and P^T are read transposed, a row
 // of the cache to 128 bytes, and the results' channels put in order when they leave.
-// Keys are scaled by a power of two of their row (which the row's scores undo), values by one of the CTA, R, so that fp16's range
-// holds them; probabilities are written for a running maximum that is raised once a score is above it by 2^8.
+// Keys are scaled by a power of two of their row (which the row's scores undo), so that fp16's range holds them; probabilities are written
+// for a running maximum that is raised once a score is above it by 2^8.  Values share one power of two, that of rows up to 2^KT_SPAN times
+// as large as the smallest the CTA met first.  A row that lies outside (far larger or smaller than most, or not seen at all and holding
+// anything) gets one of its own, 2^-d of that: its probabilities are written 2^d times as large, and a column in which that leaves fp16's range has all
+// its probabilities, and its outputs, scaled by 2^c.  Steps with such a row cost a second exponential and maximum.
+// What is done for one column depends on the rows that it sees and gives weight, to the bit.
 //
-// What bounds it: 64 sequences x 4 KV heads x 56 columns of 4096 rows take 136 us, 222 TFLOP/s, and 64 columns as long as 17: about 3500
+// What bounds it: 64 sequences x 4 KV heads x 56 columns of 4096 rows take 140 us, 214 TFLOP/s, and 64 columns as long as 17: about 3600
 // cycles go by for 128 rows, of which the codes' warps (two to a scheduler) are busy all the time and the others two thirds.  Shared memory
 // is in use for some 2500 of them: values and probabilities are written (640), read by the products at 128 bytes a cycle (16 of
 // 6 KB: 790), codes, parameters and columns' scales read by the warps.  What was measured on the way: one group of eight warps that does everything in turn 238 us; two groups 161; keys' codes as
 // subnormal factors and all loads before all stores 152; sums of weights added up beside the probabilities instead of a product with ones,
 // and two steps' P and V in shared memory, 134; stores without bank conflicts 131; values' codes as whole numbers, for rows far below the
-// largest, 137.  Products started by other warps than now are no help: by the probabilities' 142, by warps of their own, which leave the
+// largest, 137; scales and maxima that go by what a column sees 140.  Products started by other warps than now are no help: by the probabilities' 142, by warps of their own, which leave the
 // others fewer registers, 139 instead of 131.
 #include <cstring>
 
@@ -35,6 +39,8 @@ constexpr int KT_COLS = 64, KT_ROWS = 128, KT_GROUP = 256, KT_THREADS = 2 * KT_G
 constexpr uint32_t KT_TMEM = 256;                                     // columns: S^T of two steps, O^T
 // Probabilities are held as 2^KT_LIFT p, below 2^15: fp16 has them to 2^-31 of a column's largest.
 #define KT_LIFT 7.f
+// Values' exponents: the rows that share a scale lie in (base - KT_WINDOW, base], base = KT_SPAN above the smallest of the first step with any.
+constexpr int KT_SPAN = 10, KT_WINDOW = 16, KT_LEAST = -98, KT_MOST = 131;
 constexpr uint32_t KT_S = 0, KT_O = 128;
 
 // Shared memory, every block 1024-byte aligned.  K: [64 channels a block][128 rows][128 bytes], Q: [64 channels a block][64][128 bytes];
@@ -145,10 +151,11 @@ __device__ __forceinline__ uint32_t kt_window(const Kv4Sight& s, int r0, int i) 
     const int n = end - r0;
     return n >= 32 ? w : n <= 0 ? 0u : w & ((1u << n) - 1u);
 }
-// The largest of |m| and 16 s over halves of words (bf16); NaNs are above everything.
-// Below 2^(e + 1), keys are scaled by 2^-(e + 6): they stay below 2^-4, s 2^24 below 2^15, and a rounding is 2^-20 of its row's largest at
-// most, or half a step of its own.  Values, whose scale R all rows of a CTA share, by 2^(13 - e): below 2^15, roundings 2^-38 of the largest.
+// The larger of |m| and 16 s over halves of words (bf16; 0x0200 where both are 0).
+// Keys: below 2^(e + 1), they are scaled by 2^-(e + 6) and stay below 2^-4, s 2^24 below 2^15; a rounding is 2^-20 of its row's largest at
+// most, or half a step of its own.  Values: by 2^(13 - e), below 2^15, roundings 2^-38 of the largest.
 __device__ __forceinline__ uint32_t kt_reach(uint32_t s, uint32_t m) { return __vmaxu2(m & 0x7FFF7FFFu, s + 0x02000200u); }
+#define KT_ZERO 0x0200u
 
 template <int DH>
 __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_constant__ Kv4AttnArgs a) {
@@ -160,9 +167,9 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     __shared__ uint32_t s_tmem, s_poison[KT_COLS], s_nan[2][KT_ROWS];
     __shared__ __align__(16) float s_f[KT_COLS], s_m[KT_COLS];         // what a column's scores are to be multiplied with; KT_LIFT less its maximum
     __shared__ float2 s_part[KT_CLUSTER][KT_COLS];
-    __shared__ float s_rk[2][KT_ROWS], s_fade[2], s_top[4][KT_COLS], s_fall[KT_COLS], s_inv[KT_COLS];
-    __shared__ uint32_t s_max[8];
-    __shared__ int s_has_nan[2], s_eV;
+    // of the rows: what undoes their keys' scale, d; of the columns: c, what their sums and their outputs are multiplied with
+    __shared__ float s_rk[2][KT_ROWS], s_d[2][KT_ROWS], s_top[4][KT_COLS], s_c[KT_COLS], s_fall[KT_COLS], s_fall_o[KT_COLS], s_inv[KT_COLS];
+    __shared__ int s_least[8], s_has_nan[2], s_apart[2], s_base;
     unsigned char* sm = (unsigned char*)(((uintptr_t)kt_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t smem = kv4_saddr(sm), bar = kv4_saddr(bars), bar_s = bar + 8 * KT_STAGES, bar_v = bar_s + 16, bar_o = bar_v + 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -174,7 +181,10 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async;" ::: "memory");
-    if (tid < KT_COLS) s_poison[tid] = 0u;
+    if (tid < KT_COLS) {
+        s_poison[tid] = 0u;
+        s_c[tid] = 0.f;
+    }
     if (warp == 0) {
         __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(kv4_saddr(&s_tmem)), "r"(KT_TMEM) : "memory");
@@ -246,7 +256,8 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     int n = 0;                             // steps taken
     if (warp < KT_GROUP / 32) {
         // ================ codes into values
-        int eV = -99;                                                  // |m| and 16 s of the values stay below 2^(eV + 1) (the same in all threads)
+        int base = KT_LEAST;                                           // |m| and 16 s of a row in the window are below 2^(base + 1)
+        uint32_t above = 0u, below = 0u;                               // its ends in kt_reach's numbers (above 0: no row has had values yet)
         int stage = 0;
         uint32_t parity = 0;
         const __half2 sixteenth = __floats2half2_rn(0.0625f, 0.0625f);
@@ -305,35 +316,53 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
                 for (int w = 0; w < Q; ++w) { sw[w] &= keep; mw[w] &= keep; }
             }
+            uint32_t signs = 0u;                                       // (of scales: of rows that were never written)
 #pragma unroll
-            for (int w = 0; w < Q; ++w) big = w ? __vmaxu2(big, kt_reach(sw[w], mw[w])) : kt_reach(sw[w], mw[w]);
+            for (int w = 0; w < Q; ++w) {
+                big = w ? __vmaxu2(big, kt_reach(sw[w], mw[w])) : kt_reach(sw[w], mw[w]);
+                signs |= sw[w];
+            }
             kt_fence_smem();
-            float fade = 1.f;
-            const bool smaller = kt_sync_or<1>(max(big >> 16, big & 0xFFFFu) >= (uint32_t)(eV + 1 + 127) << 7);
-            if (smaller) {
-                uint32_t fin = 0u, nan = 0u;                           // groups of the pair's rows that hold a NaN: bits w and 4 + w
+            // (of eight pairs of rows, four start with the odd one: no bank twice)
+            const int flip = pr >> 2 & 1;
+            float R0 = kv4_pow2(13 - base), R1 = R0;                   // of the pair's rows, in that order
+            bool apart = false;
+            // (an infinite or NaN parameter, or a row outside the window)
+            const uint32_t b0 = big & 0xFFFFu, b1 = big >> 16;
+            const bool unusual = kt_sync_or<1>((signs & 0x80008000u) != 0u || max(b0, b1) >= above || b0 - (KT_ZERO + 1u) < below || b1 - (KT_ZERO + 1u) < below);
+            if (unusual) {
+                uint32_t nan = 0u, x0 = 0u, x1 = 0u;                   // groups of the pair's rows that hold a NaN: bits w and 4 + w
 #pragma unroll
                 for (int w = 0; w < Q; ++w)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const uint32_t x = (sw[w] >> (16 * i)) & 0xFFFFu, y = (mw[w] >> (16 * i)) & 0x7FFFu;
-                        if (x < 0x7F80u) fin = max(fin, max(x + 0x0200u, y));
+                        if (x < 0x7F80u && y < 0x7F80u) (i ? x1 : x0) = max(i ? x1 : x0, max(x + 0x0200u, y));
                         else nan |= 1u << (4 * i + w);
                     }
-                fin = __reduce_max_sync(0xffffffffu, fin);
-                if (lane == 0) s_max[warp] = fin;
+                const int e0 = max((int)(x0 >> 7) - 127, KT_LEAST), e1 = max((int)(x1 >> 7) - 127, KT_LEAST);
+                if (above == 0u) {
+                    int least = __reduce_min_sync(0xffffffffu, min(x0 > KT_ZERO ? e0 : KT_MOST + 1, x1 > KT_ZERO ? e1 : KT_MOST + 1));
+                    if (lane == 0) s_least[warp] = least;
+                    kt_sync<1>();
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) least = min(least, s_least[w]);
+                    if (least <= KT_MOST) {
+                        base = min(least + KT_SPAN, KT_MOST);
+                        above = min((uint32_t)(base + 1 + 127) << 7, 0x7F80u);
+                        below = base - KT_WINDOW < KT_LEAST ? 0u : ((uint32_t)(base - KT_WINDOW + 1 + 127) << 7) - (KT_ZERO + 1u);
+                    }
+                }
+                const int d0 = x0 <= KT_ZERO || (e0 <= base && e0 > base - KT_WINDOW) ? 0 : e0 - base, d1 = x1 <= KT_ZERO || (e1 <= base && e1 > base - KT_WINDOW) ? 0 : e1 - base;
+                R0 = kv4_pow2(13 - base - (flip ? d1 : d0));
+                R1 = kv4_pow2(13 - base - (flip ? d0 : d1));
                 if (part == 0) {
                     s_nan[n & 1][2 * pr] = nan & 15u;
                     s_nan[n & 1][2 * pr + 1] = nan >> 4;
+                    s_d[n & 1][2 * pr] = (float)d0;
+                    s_d[n & 1][2 * pr + 1] = (float)d1;
                 }
-                kt_sync<1>();
-#pragma unroll
-                for (int w = 0; w < 8; ++w) fin = max(fin, s_max[w]);
-                const int e = min(max((int)(fin >> 7) - 127, -98), 130);
-                if (e > eV) {
-                    fade = e - eV > 126 ? 0.f : kv4_pow2(eV - e);
-                    eV = e;
-                }
+                apart = kt_sync_or<1>(d0 != 0 || d1 != 0);
                 if (edge && nan) {
                     // columns that do not see the row take nothing of it: left out here, put in where the probabilities are
 #pragma unroll
@@ -345,8 +374,8 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 }
             }
             if (warp == 0 && kt_elect()) {
-                s_fade[n & 1] = fade;
-                s_has_nan[n & 1] = smaller && edge;
+                s_apart[n & 1] = apart;
+                s_has_nan[n & 1] = unusual && edge;
                 kt_fence_after();
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
@@ -359,22 +388,19 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 if (ok && n > 0 && t + (KT_STAGES - 1) * S < nstep) fetch(t + (KT_STAGES - 1) * S, stage == 0 ? KT_STAGES - 1 : stage - 1);
             }
             __syncwarp();
-            // (of eight pairs of rows, four start with the odd one: no bank twice)
-            const int flip = pr >> 2 & 1;
 #pragma unroll
             for (int w = 0; w < Q; ++w) {
                 sw[w] = __byte_perm(sw[w], 0u, flip ? 0x1032 : 0x3210);
                 mw[w] = __byte_perm(mw[w], 0u, flip ? 0x1032 : 0x3210);
             }
             // ---- values: four channels of a group and of its neighbour, of two rows
-            const float R = kv4_pow2(13 - eV);
             __half2 s1[2][H], m1[2][H];
 #pragma unroll
             for (int w = 0; w < H; ++w) {
-                s1[0][w] = __floats2half2_rn(bf16_lo(sw[2 * w]) * R, bf16_lo(sw[2 * w + 1]) * R);
-                s1[1][w] = __floats2half2_rn(bf16_hi(sw[2 * w]) * R, bf16_hi(sw[2 * w + 1]) * R);
-                m1[0][w] = __floats2half2_rn(bf16_lo(mw[2 * w]) * R, bf16_lo(mw[2 * w + 1]) * R);
-                m1[1][w] = __floats2half2_rn(bf16_hi(mw[2 * w]) * R, bf16_hi(mw[2 * w + 1]) * R);
+                s1[0][w] = __floats2half2_rn(bf16_lo(sw[2 * w]) * R0, bf16_lo(sw[2 * w + 1]) * R0);
+                s1[1][w] = __floats2half2_rn(bf16_hi(sw[2 * w]) * R1, bf16_hi(sw[2 * w + 1]) * R1);
+                m1[0][w] = __floats2half2_rn(bf16_lo(mw[2 * w]) * R0, bf16_lo(mw[2 * w + 1]) * R0);
+                m1[1][w] = __floats2half2_rn(bf16_hi(mw[2 * w]) * R1, bf16_hi(mw[2 * w + 1]) * R1);
             }
             unsigned char* to = sm + M::V + (n & 1) * KB * 16384;
 #pragma unroll
@@ -395,7 +421,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
             if (lane == 0) kt_arrive(bar_v + 8 * (n & 1));
             if (++stage == KT_STAGES) { stage = 0; parity ^= 1u; }
         }
-        if (tid == 0) s_eV = eV;
+        if (tid == 0) s_base = base;
     } else {
         // ================ scores into probabilities
         const int quarter = warp & 3, half = (warp - KT_GROUP / 32) >> 2;
@@ -404,11 +430,29 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
         float l[32];                                                   // sums of this row's weights, every 128th row's
 #pragma unroll
         for (int i = 0; i < 32; ++i) l[i] = 0.f;
+        bool scaled = false;                                           // some column's c is not 0 (the same in all of these threads)
+        // the columns' largest of the rows' x: lane L of the warp gets that of its column L, by halving what each lane has to compare
+        auto largest = [&](float (&x)[32]) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const bool high = (lane & o) != 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i < o) {
+                        const float keep = high ? x[i + o] : x[i], give = high ? x[i] : x[i + o];
+                        x[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, o));
+                    }
+            }
+            s_top[quarter][half * 32 + lane] = x[0];
+            kt_sync<2>();
+        };
         for (int t = rank; t < nstep; t += S, ++n) {
             if (ok) ok = kv4_wait(bar_s + 8 * (n & 1), (n >> 1) & 1);
             kt_fence_after();
-            const float rk = s_rk[n & 1][row], fade = s_fade[n & 1];
+            const bool apart = s_apart[n & 1] || scaled;
+            const float rk = s_rk[n & 1][row];
             float y[32], top = -INFINITY;                              // by how much scores are above the columns' maxima
+            float counts = 1.f;                                        // what the probabilities written count for in the sums
             uint32_t see = 0xFFFFFFFFu;
             {
                 uint32_t raw[32];
@@ -419,7 +463,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                     const ulonglong2 m = *(const ulonglong2*)(s_m + half * 32 + i);
                     float t[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) t[k] = __uint_as_float(raw[i + k]) * rk;
+                    for (int k = 0; k < 4; k += 2) kv4_unpack2(kv4_mul2(kv4_pack2(__uint_as_float(raw[i + k]), __uint_as_float(raw[i + k + 1])), kv4_pack2(rk, rk)), t[k], t[k + 1]);
                     kv4_above(t[0], t[1], f.x, f.y, m.x, y[i], y[i + 1]);
                     kv4_above(t[2], t[3], f.z, f.w, m.y, y[i + 2], y[i + 3]);
                 }
@@ -436,8 +480,7 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
             for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
             if (ok && n > 1) ok = kv4_wait(bar_o + 8 * (n & 1), ((n >> 1) - 1) & 1);       // P may be overwritten
-            if (kt_sync_or<2>(top > KV4_LAZY + KT_LIFT || fade != 1.f)) {
-                // the columns' maxima: lane L of the warp gets that of its column L, by halving what each lane has to compare
+            if (kt_sync_or<2>(top > KV4_LAZY + KT_LIFT || apart)) {
                 uint32_t raw[32];
                 kt_ld32(my_tmem + KT_S + (n & 1) * KT_COLS, raw);
                 float x[32];
@@ -447,27 +490,39 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                     if (!(see >> i & 1u)) y[i] = -INFINITY;
                     x[i] = y[i];
                 }
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    const bool high = (lane & o) != 0;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (i < o) {
-                            const float keep = high ? x[i + o] : x[i], give = high ? x[i] : x[i + o];
-                            x[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, o));
-                        }
-                }
-                s_top[quarter][half * 32 + lane] = x[0];
-                kt_sync<2>();
-                if (tid < KT_GROUP + KT_COLS) {
-                    const int c = tid - KT_GROUP;
-                    const float old = -s_m[c], m = fmaxf(old, fmaxf(fmaxf(s_top[0][c], s_top[1][c]), fmaxf(s_top[2][c], s_top[3][c])) - KT_LIFT);
+                largest(x);
+                float d = 0.f, old = 0.f, m = 0.f;                     // old, m: of the column that this thread looks after, if any
+                const int c = tid - KT_GROUP;
+                if (c < KT_COLS) {
+                    // (a column's own scores decide)
+                    const float z = fmaxf(fmaxf(s_top[0][c], s_top[1][c]), fmaxf(s_top[2][c], s_top[3][c]));
+                    old = -s_m[c];
+                    m = z - old > KV4_LAZY + KT_LIFT ? z - KT_LIFT : old;
                     s_m[c] = -m;
-                    s_fall[c] = kv4_exp2(old - m);
+                    s_fall[c] = s_fall_o[c] = kv4_exp2(old - m);
                 }
                 kt_sync<2>();
 #pragma unroll
                 for (int i = 0; i < 32; ++i) y[i] += s_m[half * 32 + i];
+                if (apart) {
+                    // what the rows' 2^d does to the probabilities: below 2^15, and not next to nothing where the maximum has been raised
+                    d = s_apart[n & 1] ? s_d[n & 1][row] : 0.f;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = y[i] + d;
+                    largest(x);
+                    bool some = false;
+                    if (c < KT_COLS) {
+                        const float z = fmaxf(fmaxf(s_top[0][c], s_top[1][c]), fmaxf(s_top[2][c], s_top[3][c])), was = s_c[c];
+                        float now = was;
+                        if (z + was > 15.f) now = KT_LIFT - ceilf(z);
+                        else if (m > old && z + was < 0.f) now = fminf(KT_LIFT - ceilf(z), was + floorf(fminf(m - old, 300.f)));
+                        now = fminf(now, 300.f);
+                        s_c[c] = now;
+                        s_fall_o[c] = kv4_exp2((old - m) + (now - was));
+                        some = now != 0.f;
+                    }
+                    scaled = kt_sync_or<2>(some);
+                }
                 if (n > 0) {
                     if (ok) ok = kv4_wait(bar_o + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
                     kt_fence_after();
@@ -475,11 +530,19 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                     kt_ld32(my_tmem + KT_O, o);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        const float f = s_fall[half * 32 + i];
-                        l[i] *= f;
-                        o[i] = __float_as_uint(__uint_as_float(o[i]) * (f * fade));
+                        l[i] *= s_fall[half * 32 + i];
+                        o[i] = __float_as_uint(__uint_as_float(o[i]) * s_fall_o[half * 32 + i]);
                     }
                     kt_st32(my_tmem + KT_O, o);
+                }
+                if (apart) {
+                    // the sums take the weights themselves
+                    counts = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        l[i] += kv4_exp2(y[i]);
+                        y[i] += d + s_c[half * 32 + i];
+                    }
                 }
             }
             // ---- probabilities
@@ -489,8 +552,8 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float p0 = kv4_exp2(y[i + 2 * k]), p1 = kv4_exp2(y[i + 2 * k + 1]);
-                    l[i + 2 * k] += p0;
-                    l[i + 2 * k + 1] += p1;
+                    l[i + 2 * k] = fmaf(p0, counts, l[i + 2 * k]);
+                    l[i + 2 * k + 1] = fmaf(p1, counts, l[i + 2 * k + 1]);
                     v[k] = kv4_half2(p0, p1);
                 }
                 const int chunk = half * 4 + i / 8;
@@ -559,14 +622,16 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
     } else {
         // a warp has a quarter of the lanes, 16 columns
         const int quarter = warp & 3, col = (warp >> 2) * 16;
-        const float down = kv4_pow2(s_eV - 13);
         uint32_t o[16];
         if (quarter * 32 < DH) {
             kt_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + col + KT_O, o);
             const int at = quarter * 32 + lane, w = at % (4 * Q) / 8 * 2 + (at & 1), ch = 32 * w + at / (4 * Q) * 4 + (at >> 1 & 3);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                sO[(col + i) * LDO + ch + APART * w] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u) : __uint_as_float(o[i]) * s_inv[col + i] * down;
+            for (int i = 0; i < 16; ++i) {
+                const int e = min(max(s_base - 13 - (int)s_c[col + i], -250), 250);
+                sO[(col + i) * LDO + ch + APART * w] = s_poison[col + i] >> w & 1u ? __uint_as_float(0x7FC00000u)
+                                                                                  : __uint_as_float(o[i]) * s_inv[col + i] * kv4_pow2(e / 2) * kv4_pow2(e - e / 2);
+            }
         }
     }
     kt_fence_before();

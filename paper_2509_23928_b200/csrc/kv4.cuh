@@ -80,6 +80,11 @@ __device__ __forceinline__ u64 kv4_pack2(float x, float y) {
     return r;
 }
 __device__ __forceinline__ void kv4_unpack2(u64 v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ u64 kv4_mul2(u64 a, u64 b) {
+    u64 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 __device__ __forceinline__ u64 kv4_add2(u64 a, u64 b) {
     u64 r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
