@@ -410,7 +410,8 @@ int hivis_kv4_read(const hivis_kv4_cache* cache, int B, const int* seq_slots_hos
  * q [B * n_q, n_q_heads * head_dim] and out likewise in `dtype` (HIVIS_F32 | HIVIS_BF16), q_ld and out_ld elements from one
  * row to the next.  The result does not depend on anything but the arguments: sums are made in one order.
  * Rows' values as m + s n, sums in fp32; fp32: queries and weights to 22 bits.  bf16: weights to 11 bits, and in calls of many
- * queries x query heads per KV head (over 16, head_dim 64: over 48) the rows' values too.  Sums of 2^8 |v| over a sequence's
+ * queries x query heads per KV head (over 16, head_dim 64: over 48) the rows' values too.  A weight times the scale of its row and group
+ * counts to 2^-24 (fp32: 2^-39) of the largest such product of its query and head.  Sums of 2^8 |v| over a sequence's
  * rows are to stay below 2^127.
  * Errors: ARG, SHAPE (n_q_heads not a multiple of n_kv_heads, q_ld or out_ld not a multiple of 8), DTYPE, CAPACITY (B, n_q >
  * HIVIS_KV4_MAX_QUERIES, mask_rows > HIVIS_KV4_MAX_MASK), CUDA; the text is available from hivis_last_error(NULL).    */

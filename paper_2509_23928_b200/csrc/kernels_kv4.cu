@@ -553,17 +553,20 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
                 const uint32_t b0 = kv4_transpose(h0), b1 = kv4_transpose(h1);
                 if constexpr (SPLIT) {
                     const float2 w0 = kv4_unhalf2(h0), w1 = kv4_unhalf2(h1);
-                    const uint32_t c0 = kv4_transpose(kv4_half2(ps[0] - w0.x, ps[1] - w0.y)), c1 = kv4_transpose(kv4_half2(ps[2] - w1.x, ps[3] - w1.y));
-                    float d[4], f[4];
-                    kv4_mma0(d, f0, f1, f2, f3, c0, c1);
-                    kv4_mma(d, f0, f1, f2, f3, b0, b1);
-                    kv4_mma0(f, g0, g1, g2, g3, c0, c1);
-                    kv4_mma(f, g0, g1, g2, g3, b0, b1);
+                    // (what the first rounding left, 2^11 times: as far from fp16's smallest number as the first part)
+                    const uint32_t c0 = kv4_transpose(kv4_half2((ps[0] - w0.x) * 0x1p11f, (ps[1] - w0.y) * 0x1p11f));
+                    const uint32_t c1 = kv4_transpose(kv4_half2((ps[2] - w1.x) * 0x1p11f, (ps[3] - w1.y) * 0x1p11f));
+                    auto add = [](float (&o)[4], const float (&hi)[4], const float (&lo)[4]) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        st.o[n][2 * w][e] += d[e];
-                        st.o[n][2 * w + 1][e] += f[e];
-                    }
+                        for (int e = 0; e < 4; ++e) o[e] += fmaf(lo[e], 0x1p-11f, hi[e]);
+                    };
+                    float d[4], f[4];
+                    kv4_mma0(d, f0, f1, f2, f3, b0, b1);
+                    kv4_mma0(f, f0, f1, f2, f3, c0, c1);
+                    add(st.o[n][2 * w], d, f);
+                    kv4_mma0(d, g0, g1, g2, g3, b0, b1);
+                    kv4_mma0(f, g0, g1, g2, g3, c0, c1);
+                    add(st.o[n][2 * w + 1], d, f);
                 } else {
                     kv4_mma(st.o[n][2 * w], f0, f1, f2, f3, b0, b1);
                     kv4_mma(st.o[n][2 * w + 1], g0, g1, g2, g3, b0, b1);

@@ -836,3 +836,14 @@ def test_values_and_scores_that_change_together(dtype, dh, G, n_q, step, rising)
         f.v[i] = (f.v[i].double() * step ** (r // 70 % 4).double()).to(f.v.dtype)
     f.put()
     _check_any(f, f.cache.attention(f.q, f.rows, n_q=n_q))
+
+
+@pytest.mark.parametrize("dh,G,n_q", [(64, 1, 1), (128, 1, 1), (64, 4, 5), (128, 2, 8)])
+@pytest.mark.parametrize("ratio", [1e-2, 1e-4, 1e-5])
+def test_fp32_weights_keep_22_bits_in_every_group(dh, G, n_q, ratio):
+    """A group of channels far smaller than its neighbour, few rows with scores around 0: the bounds of its own values."""
+    f = Filled("f32", dh, 2, G, [3, 40, 2, 20], n_q, seed=81)
+    f.v[:, :, 32:64] *= ratio
+    f.k *= 0.1
+    f.put()
+    f.check(f.cache.attention(f.q, f.rows, n_q=n_q))
