@@ -17,13 +17,13 @@
 // its probabilities, and its outputs, scaled by 2^c.  Steps with such a row cost a second exponential and maximum.
 // What is done for one column depends on the rows that it sees and gives weight, to the bit.
 //
-// What bounds it: 64 sequences x 4 KV heads x 56 columns of 4096 rows take 140 us, 214 TFLOP/s, and 64 columns as long as 17: about 3600
+// What bounds it: 64 sequences x 4 KV heads x 56 columns of 4096 rows take 139 us, 217 TFLOP/s, and 64 columns as long as 17: about 3500
 // cycles go by for 128 rows, of which the codes' warps (two to a scheduler) are busy all the time and the others two thirds.  Shared memory
 // is in use for some 2500 of them: values and probabilities are written (640), read by the products at 128 bytes a cycle (16 of
 // 6 KB: 790), codes, parameters and columns' scales read by the warps.  What was measured on the way: one group of eight warps that does everything in turn 238 us; two groups 161; keys' codes as
 // subnormal factors and all loads before all stores 152; sums of weights added up beside the probabilities instead of a product with ones,
 // and two steps' P and V in shared memory, 134; stores without bank conflicts 131; values' codes as whole numbers, for rows far below the
-// largest, 137; scales and maxima that go by what a column sees 140.  Products started by other warps than now are no help: by the probabilities' 142, by warps of their own, which leave the
+// largest, 137; scales and maxima that go by what a column sees 139 (138 without).  Products started by other warps than now are no help: by the probabilities' 142, by warps of their own, which leave the
 // others fewer registers, 139 instead of 131.
 #include <cstring>
 
@@ -309,10 +309,11 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                 }
             }
             // ---- the values' parameters
+            uint32_t keep = 0xFFFFFFFFu;
             if (edge) {
                 // nothing was fetched behind `end`
                 const int r = t * KT_ROWS + 2 * pr;
-                const uint32_t keep = r + 1 < end ? 0xFFFFFFFFu : r < end ? 0xFFFFu : 0u;
+                keep = r + 1 < end ? 0xFFFFFFFFu : r < end ? 0xFFFFu : 0u;
 #pragma unroll
                 for (int w = 0; w < Q; ++w) { sw[w] &= keep; mw[w] &= keep; }
             }
@@ -327,9 +328,10 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
             const int flip = pr >> 2 & 1;
             float R0 = kv4_pow2(13 - base), R1 = R0;                   // of the pair's rows, in that order
             bool apart = false;
-            // (an infinite or NaN parameter, or a row outside the window)
+            // (an infinite or NaN parameter, or a row outside the window; behind `end` there is none)
+            if (edge) big = (big & keep) | (below << 16 | below) & ~keep;
             const uint32_t b0 = big & 0xFFFFu, b1 = big >> 16;
-            const bool unusual = kt_sync_or<1>((signs & 0x80008000u) != 0u || max(b0, b1) >= above || b0 - (KT_ZERO + 1u) < below || b1 - (KT_ZERO + 1u) < below);
+            const bool unusual = kt_sync_or<1>((signs & 0x80008000u) != 0u || max(b0, b1) >= above || min(b0, b1) < below);
             if (unusual) {
                 uint32_t nan = 0u, x0 = 0u, x1 = 0u;                   // groups of the pair's rows that hold a NaN: bits w and 4 + w
 #pragma unroll
@@ -350,12 +352,15 @@ __global__ void __launch_bounds__(KT_THREADS, 1) kv4_tc_kernel(const __grid_cons
                     if (least <= KT_MOST) {
                         base = min(least + KT_SPAN, KT_MOST);
                         above = min((uint32_t)(base + 1 + 127) << 7, 0x7F80u);
-                        below = base - KT_WINDOW < KT_LEAST ? 0u : ((uint32_t)(base - KT_WINDOW + 1 + 127) << 7) - (KT_ZERO + 1u);
+                        below = base - KT_WINDOW < KT_LEAST ? KT_ZERO + 1u : (uint32_t)(base - KT_WINDOW + 1 + 127) << 7;
                     }
                 }
-                const int d0 = x0 <= KT_ZERO || (e0 <= base && e0 > base - KT_WINDOW) ? 0 : e0 - base, d1 = x1 <= KT_ZERO || (e1 <= base && e1 > base - KT_WINDOW) ? 0 : e1 - base;
+                int d0 = e0 <= base && e0 > base - KT_WINDOW ? 0 : e0 - base, d1 = e1 <= base && e1 > base - KT_WINDOW ? 0 : e1 - base;
                 R0 = kv4_pow2(13 - base - (flip ? d1 : d0));
                 R1 = kv4_pow2(13 - base - (flip ? d0 : d1));
+                // (rows of zeros have weight and no values: a column does not go by them)
+                if (x0 <= KT_ZERO) d0 = keep & 0xFFFFu ? -300 : 0;
+                if (x1 <= KT_ZERO) d1 = keep >> 16 ? -300 : 0;
                 if (part == 0) {
                     s_nan[n & 1][2 * pr] = nan & 15u;
                     s_nan[n & 1][2 * pr + 1] = nan >> 4;

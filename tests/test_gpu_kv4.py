@@ -847,3 +847,18 @@ def test_fp32_weights_keep_22_bits_in_every_group(dh, G, n_q, ratio):
     f.k *= 0.1
     f.put()
     f.check(f.cache.attention(f.q, f.rows, n_q=n_q))
+
+
+@pytest.mark.parametrize("dtype,dh,G,n_q", UNSEEN)
+@pytest.mark.parametrize("at", [0, 130, 299])
+def test_a_row_of_zeros_that_takes_the_weight(dtype, dh, G, n_q, at):
+    """Where a row without values has all the weight but 1e-12, what the others add to its zeros is held like any result."""
+    f = Filled(dtype, dh, 2, G, [300, 100], n_q, seed=83, q_std=0.5)
+    f.q.copy_(f.q.abs() + 0.1)
+    f.k.copy_((f.k.float() * 0.1).to(f.k.dtype))
+    for b in range(2):
+        r = _starts(f.lens)[b] + min(at, f.lens[b] - n_q)
+        f.v[r] = 0.0
+        f.k[r] = 60.0 / (float(f.q.float().mean()) * dh ** 0.5)
+    f.put()
+    _check_any(f, f.cache.attention(f.q, f.rows, n_q=n_q))
