@@ -352,6 +352,14 @@ __device__ __forceinline__ float kv4_sum_rows(float x) {
     return x + __shfl_xor_sync(0xffffffffu, x, 16);
 }
 
+// A score above its column's maximum.  Products are rounded first, as for two (kv4_above); fp32 keeps what a fused operation has of them where
+// the maximum is small enough for that to be a fraction.
+template <bool SPLIT>
+__device__ __forceinline__ float kv4_above1(float s, float f, float m) {
+    const float y = __fadd_rn(__fmul_rn(s, f), -m);
+    return SPLIT && fabsf(m) < 0x1p22f ? fmaf(s, f, -m) : y;
+}
+
 // U tiles of 16 rows from `row` on.  EDGE: some of the rows are not for every column, or not there at all.  Two tiles at a time: the
 // chain from a tile's codes to its output is a thousand cycles long, and one tile alone leaves a warp waiting for most of them.
 template <int DH, int NT, bool SPLIT, int U, bool EDGE>
@@ -416,7 +424,12 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
                     for (int i = 0; i < 2; ++i)
                         if (!sight(row + 16 * u + g + 4 * e, min((j0 + 8 * n + 2 * c + i) / G, sight.n_q - 1))) s[u][n][e + i] = -INFINITY;
                 }
-                kv4_above(s[u][n][e], s[u][n][e + 1], st.fq[n][0], st.fq[n][1], kv4_pack2(-st.m[n][0], -st.m[n][1]), p[u][n][e], p[u][n][e + 1]);
+                if constexpr (SPLIT) {
+                    p[u][n][e] = kv4_above1<true>(s[u][n][e], st.fq[n][0], st.m[n][0]);
+                    p[u][n][e + 1] = kv4_above1<true>(s[u][n][e + 1], st.fq[n][1], st.m[n][1]);
+                } else {
+                    kv4_above(s[u][n][e], s[u][n][e + 1], st.fq[n][0], st.fq[n][1], kv4_pack2(-st.m[n][0], -st.m[n][1]), p[u][n][e], p[u][n][e + 1]);
+                }
                 top = fmaxf(top, fmaxf(p[u][n][e], p[u][n][e + 1]));
             }
     // ---- the values' scales
@@ -465,15 +478,15 @@ __device__ __forceinline__ void kv4_rows(Kv4Warp<DH, NT, SPLIT>& st, const unsig
             for (int e = 0; e < 2; ++e) {
                 float z = -INFINITY, t = -INFINITY;
 #pragma unroll
-                for (int u = 0; u < U; ++u) z = fmaxf(z, fmaxf(__fmul_rn(s[u][n][e], st.fq[n][e]), __fmul_rn(s[u][n][e + 2], st.fq[n][e])));
+                for (int u = 0; u < U; ++u) z = fmaxf(z, fmaxf(s[u][n][e], s[u][n][e + 2]));
                 z = kv4_max_rows(z);
-                const float old = st.m[n][e], above = z - old;
+                const float old = st.m[n][e], above = kv4_above1<SPLIT>(z, st.fq[n][e], old);
                 const bool rise = above > KV4_LAZY;
-                const float m = !rise ? old : above < 0x1p20f && fabsf(old) < 0x1p22f ? old + floorf(above) : z;
+                const float m = !rise ? old : above < 0x1p20f && fabsf(old) < 0x1p22f ? old + floorf(above) : __fmul_rn(z, st.fq[n][e]);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    p[u][n][e] = __fadd_rn(__fmul_rn(s[u][n][e], st.fq[n][e]), -m);
-                    p[u][n][e + 2] = __fadd_rn(__fmul_rn(s[u][n][e + 2], st.fq[n][e]), -m);
+                    p[u][n][e] = kv4_above1<SPLIT>(s[u][n][e], st.fq[n][e], m);
+                    p[u][n][e + 2] = kv4_above1<SPLIT>(s[u][n][e + 2], st.fq[n][e], m);
                     t = fmaxf(t, fmaxf(p[u][n][e] + s0[u], p[u][n][e + 2] + s1[u]));
                 }
                 t = kv4_max_rows(t);                                // the step's p s are below 2^t
@@ -862,10 +875,14 @@ static cudaError_t kv4_launch_attn_n(Kv4AttnArgs& a, int dev, int num_sms, cudaS
         if (a.ncol <= 8) return kv4_launch_attn<DH, 1, T, 1, 4, 2>(a, dev, num_sms, st);
         return kv4_launch_attn<DH, 2, T, 1, 4, 2>(a, dev, num_sms, st);
     } else {
-        // Blocks of 64 columns, whose codes are taken apart once (kernels_kv4_tc.cu), or of 16 here.  64 sequences x 4 KV heads of 4096 rows,
-        // head_dim 128: 16 columns 124 there, 95 us here, 17 to 32 131 and 152, 64 134 and 242; 32 heads of 2240 rows: 17 columns 19.7 and
-        // 18.3, 64 20.3 and 26.5; 4 heads of 2048 rows: 13.2 and 11.1, 13.8 and 13.4.  head_dim 64, where taking apart is half the work,
-        // 32 x 8 of 2048 rows: 48 columns 65 and 57, 64 67 and 75.
+        // Blocks of 64 columns, whose codes are taken apart once (kernels_kv4_tc.cu), or of 16 here.  The rule is set for large batches of long
+        // caches: 64 sequences x 4 KV heads of 4096 rows, head_dim 128, 16 columns take 132 us there and 95 here, 17 to 32 133 and 155 to 159,
+        // 64 136 and 249; head_dim 64, where taking apart is half the work, 32 x 8 of 2048 rows: 48 columns 71 and 56, 49 71 and 74.  Where a
+        // CTA has less to do it costs more than it saves, most of all with many short sequences, whose units of one step pay a CTA's
+        // set-up each: 64 x 32 of 32 rows, 17 columns 166 there and 95 here, 64 191 and 183; of 512 rows 257 and 178, 275 and 378; one
+        // sequence of 32 heads x 2240 rows 20.5 and 19.0, 21.0 and 27.3, of 4 heads x 2048 rows 14.9 and 11.8, 15.4 and 14.1; head_dim 64,
+        // 64 x 32 of 64 rows, 49 columns 155 and 107.
+        // Registers: head_dim 128 spills, by ptxas, 32 bytes a thread at eight columns and four CTAs to an SM, 104 (bf16) and 60 (fp32) at sixteen.
         if (std::is_same<T, bf16>::value && a.ncol > (DH == 128 ? 16 : 48)) return launch_kv4_attn_tc(a, dev, num_sms, st);
         if (a.ncol > 8) return kv4_launch_attn<DH, 2, T, 1, 4, 3>(a, dev, num_sms, st);
         // Few (sequence, KV head) pairs do not fill the GPU with clusters of 16: a warp then gets more registers (nothing spilled)
