@@ -65,8 +65,9 @@ typedef struct {
                              /* HIVIS_BF16_KV4: as HIVIS_BF16, with the KV cache held in 4 */
                              /* bits (the format under hivis_kv4_cache, below): 0.3125 of  */
                              /* the memory.  Rows are rounded to bf16 and then quantised,  */
-                             /* the step's own row before it is attended to.  Draft steps  */
-                             /* run as a few launches each; no draft trees (SHAPE)         */
+                             /* the step's own row before it is attended to; a step's      */
+                             /* queries and weights are held to 11 bits.  Draft steps run  */
+                             /* as a few launches each; no draft trees (SHAPE)             */
     int d;                   /* model width; multiple of 8                                 */
     int n_q_heads, n_kv_heads;   /* n_q_heads % n_kv_heads == 0                            */
     int head_dim;            /* 64 or 128                                                  */
@@ -294,7 +295,8 @@ enum { HIVIS_OPT_CHAIN_KERNEL = 0, HIVIS_OPT_TC_KERNEL = 1, HIVIS_OPT_WAIT_LIMIT
 int hivis_set_option(hivis_ctx* ctx, int option, int value);
 
 /* Where the time of a draft step goes: synchronises `stream` and copies the time stamps of the LAST hivis_draft
- * that ran the tensor-core chain kernel with HIVIS_OPT_PHASE_TIMES on.  out_host[(s * HIVIS_PHASE_EVENTS + e) *
+ * that ran the tensor-core chain kernel with HIVIS_OPT_PHASE_TIMES on (a context of dtype HIVIS_BF16_KV4 records
+ * nothing: its steps are several launches).  out_host[(s * HIVIS_PHASE_EVENTS + e) *
  * grid + cta] = time in ns (the GPU's global timer) of event e of draft step s on CTA cta; 0 where the event did
  * not occur (a CTA without work in a phase).  Events:
  *   0..7   the CTA's arrival on the grid barrier after: embedding gather, fusion FC, QKV, attention, O, gate/up,

@@ -560,7 +560,8 @@ class Kv4Cache:
                                     v.data_ptr(), _dtype(k), ld, _raw_stream(self.dev.index)))
 
     def read(self, cu_seqlens, start_rows, slots=None):
-        """-> (k, v) fp32 [total, n_kv_heads, head_dim]: what rows start_rows[b].. of the slots stand for."""
+        """-> (k, v) fp32 [total, n_kv_heads, head_dim]: what rows start_rows[b].. of the slots stand for.  (Places whose row would lie
+        outside the cache are not written: they hold what the allocator left there.)"""
         if self._elsewhere(start_rows):
             with self.torch.cuda.device(self.dev):
                 return self.read(cu_seqlens, start_rows, slots)

@@ -426,8 +426,10 @@ static cudaError_t lp_launch(LogprobArgs& a, int dev, int num_sms, cudaStream_t 
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < HIVIS_MAX_DEVICES) attr_set[dev] = true;
     }
-    // CTAs per row: half of what the GPU holds, each with a few thousand logits at least.  A CTA costs some microseconds beside its logits: 56 rows of
-    // 152064 take 12.3 us with 8 CTAs each, 14.4 with 4, 16.4 with 16; 1021 rows of 50257 take 45 with one, 58 with two.
+    // CTAs per row: the first power of two that comes to half of what the GPU holds at once, each with a few thousand logits at least.  A CTA
+    // costs some microseconds beside its logits.  Rows of 152064, in a graph: 56 of fp32 take 8.3 us with 16 CTAs each (which this gives
+    // them; 16 CTAs of 128 threads are as many warps as 8 of 256), 8.2 with 8, 10.3 with 4; 56 of bf16 8.9 with 8 (this), 7.7 with 4, 11.9 with
+    // 16; 512 of bf16 with 20 alternatives 43 with one (this), 46 with two; 1021 fp32 rows of 50257 38 with one (this), 45 with two.
     int S = 1;
     while (S < LP_MAX_CLUSTER && (long long)a.n_rows * S < (long long)num_sms * 512 / LpVec<T>::THREADS && a.V / (2 * S) >= 8 * LpVec<T>::THREADS) S *= 2;
     a.slice = ((a.V + 8 + S - 1) / S + 7) / 8 * 8;
