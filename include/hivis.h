@@ -431,7 +431,7 @@ int hivis_kv4_attention(const hivis_kv4_cache* cache, int B, const int* seq_slot
  *   out_top_ids int32, out_top_logprobs fp32 [n_rows, top_n] (with top_n > 0): the most probable tokens, largest logit
  *   first, the lowest id among equals; -1 and -infinity where no token with mass is left.
  * A row without any mass (every logit -infinity): log-probabilities -infinity, entropy 0, no alternatives.  A row that holds
- * a NaN or +infinity: NaN; its alternatives are tokens that are not NaN.  Sums are made in one order.
+ * a NaN or +infinity: NaN for every id; its alternatives are tokens that are not NaN.  Sums are made in one order.
  * Errors: CAPACITY (n_ids > HIVIS_LOGPROBS_MAX_IDS, top_n > HIVIS_LOGPROBS_MAX_TOP), SHAPE (vocab, ld), DTYPE, ARG, CUDA; the
  * text is available from hivis_last_error(NULL).                                                                     */
 #define HIVIS_LOGPROBS_MAX_IDS 32

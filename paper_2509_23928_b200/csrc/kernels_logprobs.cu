@@ -392,7 +392,8 @@ __global__ void __launch_bounds__(LpVec<T>::THREADS, 1024 / LpVec<T>::THREADS) l
         d.w = __shfl_sync(0xffffffffu, d.w, 0);
         const bool mass = !(d.z == 0.f);                      // (a NaN counts as mass: it has to come out)
         const double ln2 = 0.69314718055994531, log_z = log2((double)d.z), scale = (double)a.scale;
-        auto logprob = [&](float x) { return !mass || x == -INFINITY ? -INFINITY : (float)((scale * (double)x - c - log_z) * ln2); };
+        // (-infinity - log Z: -infinity, or NaN in a row that is)
+        auto logprob = [&](float x) { return !mass ? -INFINITY : (float)((scale * (double)x - c - log_z) * ln2); };
         if (a.out_lp && lane < a.n_ids) a.out_lp[(long long)r * a.n_ids + lane] = logprob(asked);
         if (a.out_h && lane == 0) a.out_h[r] = mass ? (float)((log_z - (double)d.w / (double)d.z) * ln2) : 0.f;
         if (TOP) {

@@ -307,3 +307,20 @@ def test_views_that_start_anywhere(dtype):
     for logits, ids in ((x[:-1], tokens[1:].view(-1, 1)), (x[1:], tokens[1:].view(-1, 1)), (x[3:], tokens[3:].view(-1, 1)),
                         (x.view(2, 3, V)[:, -1], tokens[2:4].view(-1, 1)), (x[:, 5:1000], tokens[:6].view(-1, 1) % 995)):
         _check(logits, ids, 1.0, 4, logprobs(logits, ids, top_n=4))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [300, 20000, 152064])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_every_answer_of_a_row_that_is_not_finite_is_nan(dtype, V, bad):
+    """Tokens without mass too, and ids outside the vocabulary; in the rows beside it those are -infinity."""
+    from paper_2509_23928_b200 import logprobs
+    t = _torch()
+    x = _to(np.random.default_rng(6).standard_normal((3, V)), dtype)
+    x[:, 7] = -math.inf
+    x[1, V - 3] = bad
+    ids = t.tensor([[7, -1, V, 5]] * 3, dtype=t.int32, device="cuda")
+    out = logprobs(x, ids, top_n=2)
+    assert bool(out.logprobs[1].isnan().all()) and bool(out.entropy[1].isnan()) and bool(out.top_logprobs[1].isnan().all())
+    for r in (0, 2):
+        assert bool(out.logprobs[r, :3].isneginf().all()) and bool(t.isfinite(out.logprobs[r, 3])) and bool(t.isfinite(out.top_logprobs[r]).all())
