@@ -585,6 +585,8 @@ class Kv4Cache:
         q_ld = self._row_stride(q, heads, B * n_q, "q")
         mask_ptr = None
         if mask is not None:
+            if mask_rows < 1:
+                raise ValueError("a mask covers at least one row: mask_rows says how many")
             if mask.dtype is not t.int32 or tuple(mask.shape) != (B, n_q, (mask_rows + 31) // 32) or not mask.is_contiguous():
                 raise ValueError("mask must be a contiguous int32 tensor [B, n_q, ceil(mask_rows / 32)]")
             mask = _aligned(mask)

@@ -862,3 +862,13 @@ def test_a_row_of_zeros_that_takes_the_weight(dtype, dh, G, n_q, at):
         f.k[r] = 60.0 / (float(f.q.float().mean()) * dh ** 0.5)
     f.put()
     _check_any(f, f.cache.attention(f.q, f.rows, n_q=n_q))
+
+
+@pytest.mark.parametrize("mask_rows", [0, -1])
+def test_a_mask_of_no_rows_is_refused(mask_rows):
+    """An empty tensor has no address: without the refusal the call would be a causal one."""
+    t = _torch()
+    f = Filled("bf16", 64, 1, 2, [20, 20], 3, seed=85)
+    f.put()
+    with pytest.raises(ValueError, match="mask_rows"):
+        f.cache.attention(f.q, f.rows, n_q=3, mask=t.zeros((2, 3, 0), dtype=t.int32, device="cuda"), mask_rows=mask_rows)
