@@ -16,7 +16,8 @@
 // anything) gets one of its own, 2^-d of that: its probabilities are written 2^d times as large, and a column in which that leaves fp16's range has all
 // its probabilities, and its outputs, scaled by 2^c.  Steps with such a row cost a second maximum and exponential, and the outputs' way
 // through registers: where every step has one, 64 sequences x 4 KV heads x 56 columns of 4096 rows take 278 us, where none has, 135 to 139.
-// What is done for one column depends on the rows that it sees and gives weight, to the bit.
+// So a column gets what the rows that it sees and gives weight make of it; others can move the scale that most rows share, which shifts
+// roundings at most.
 // (ptxas: 128 registers, 14 bytes spilled at head_dim 128, 8 at 64.)
 //
 // What bounds it: 64 sequences x 4 KV heads x 56 columns of 4096 rows take 139 us, 217 TFLOP/s, and 64 columns as long as 17: about 3500
